@@ -354,6 +354,125 @@ int lordba_fit_scales(const float *target, int64_t ld, const uint32_t *packed_A,
                       float *s_in, float *s_r, float *s_out, int64_t d_in, int64_t d_out, int r, int sweeps,
                       int axes, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * ---- The frozen base projection in 8-bit integers ------------------------------------------------
+ *
+ * y[t,n] = s_x[t] * s_w[n] * sum_k x[t,k] w[n,k]: x holds a token's activations as integers with one
+ * scale a token, w a weight matrix (d_out x d_in row-major, the contraction contiguous) with one scale
+ * an output channel.  The sum is exact in 32-bit integers (d_in <= LORDBA_INT8_MAX_DIN, all values
+ * -128 ... 127 allowed); float32(sum) * s_x * s_w is rounded once to the type of y.  y is overwritten:
+ * this is the base output of Eq. 2, to which the adapter forward then adds its term.
+ *
+ * lordba_int8_quantize_rows makes x and s_x from activations: s_x[t] = max_k |x[t,k]| / 127 and
+ * q = rint(x * (127 / max)), ties to even.  A row whose largest magnitude is below 2^-120 (zero rows
+ * among them) becomes zeros with scale 0; a row that holds an infinity or a NaN becomes zeros with
+ * scale NaN, so that its outputs are NaN and no other row's are touched.
+ *
+ * The gradient to x of a frozen projection is the same product with w transposed (laid out once) and
+ * dy * s_w quantised per token.
+ *
+ * dtype: the type of y (and of the activations that are quantised): LORDBA_BF16, LORDBA_F16 or
+ * LORDBA_F32.  Any sizes, pitches and alignments are taken; operands whose base or pitch is not a
+ * multiple of 16 bytes are first copied into the workspace.  T = 0 is a no-op.
+ */
+#define LORDBA_INT8_MAX_DIN 131071
+typedef struct lordba_int8_proj {
+    const int8_t *x;            /* [device] T x d_in, pitch ldx                 */
+    const float  *s_x;          /* [device] T                                   */
+    const int8_t *w;            /* [device] d_out x d_in, pitch ldw             */
+    const float  *s_w;          /* [device] d_out                               */
+    void         *y;            /* [device] T x d_out, pitch ldy, overwritten   */
+    int64_t d_in, d_out, ldx, ldw, ldy;      /* pitches in elements              */
+} lordba_int8_proj;
+
+int lordba_int8_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scale, int64_t T,
+                              int64_t d, int dtype, void *stream);
+/* Bytes of workspace the call needs: [device], 256-byte aligned; 0 when every operand is aligned (the
+ * workspace may then be NULL).  LORDBA_EINVAL from the call when the workspace given is shorter. */
+size_t lordba_int8_linear_workspace_bytes(const lordba_int8_proj *p, int64_t T);
+int lordba_int8_linear(const lordba_int8_proj *p, int64_t T, int dtype, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
+/*
+ * ---- The gated feed-forward block -----------------------------------------------------------------
+ *
+ *     g = x w_gate^T + gate_add        u = x w_up^T + up_add        h = act(g) * u
+ *
+ * both projections, the activation and the product in one kernel.  x is T x d_in, w_gate and w_up are
+ * d_hidden x d_in (contraction contiguous), h is T x d_hidden.  gate_add / up_add (both or neither) are
+ * added to the sums in float32: the terms that the adapters of the two projections put into zeroed
+ * buffers.  gate / up (both or neither) receive g and u rounded once, which is what the backward pass
+ * takes; they may be the buffers of gate_add / up_add.  h is computed from the unrounded g and u.
+ *
+ * act: LORDBA_ACT_SILU  act(g) = g s(g), s the logistic function;
+ *      LORDBA_ACT_GELU_TANH  act(g) = g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.
+ *
+ * dtype: LORDBA_BF16 or LORDBA_F16, the type of every matrix.  With LORDBA_GATED_INT8 in flags x, w_gate
+ * and w_up are int8 and s_x (T), s_gate, s_up (d_hidden) their scales, as in lordba_int8_linear; dtype is
+ * then the type of the other matrices.  LORDBA_F32 is LORDBA_EUNSUPPORTED.  Workspace as above.
+ */
+typedef enum { LORDBA_ACT_SILU = 0, LORDBA_ACT_GELU_TANH = 1 } lordba_activation;
+#define LORDBA_GATED_INT8 1
+typedef struct lordba_gated {
+    const void  *x, *w_gate, *w_up;          /* [device] pitches ldx, ldw, ldw                        */
+    const float *s_x, *s_gate, *s_up;        /* [device] scales, LORDBA_GATED_INT8 only, else NULL    */
+    const void  *gate_add, *up_add;          /* [device] T x d_hidden, pitch ld_add, or both NULL     */
+    void        *gate, *up;                  /* [device] T x d_hidden, pitch ld_pre, or both NULL     */
+    void        *h;                          /* [device] T x d_hidden, pitch ldh                      */
+    int64_t d_in, d_hidden, ldx, ldw, ld_add, ld_pre, ldh;
+    int32_t act, flags;
+} lordba_gated;
+
+size_t lordba_gated_workspace_bytes(const lordba_gated *g, int64_t T);
+int lordba_gated_forward(const lordba_gated *g, int64_t T, int dtype, void *workspace, size_t workspace_bytes,
+                         void *stream);
+
+/*
+ * Backward pass of lordba_gated_forward from the gradient dh of h and the stored gate / up:
+ *
+ *     dgate = dh * up * act'(gate)           dup = dh * act(gate)
+ *     dx = dgate w_gate + dup w_up           dw_gate = dgate^T x       dw_up = dup^T x
+ *
+ * dgate and dup (T x d_hidden) are always written: they are the gradients of gate_add and up_add, where
+ * the adapters' own gradients start.  dx is skipped when its pointer is NULL (w_gate and w_up are then
+ * not read), dw_gate / dw_up when both of theirs are (x is then not read).  Every sum is float32; dgate
+ * and dup enter the products in the matrices' type, because that is what the tensor cores take.  The
+ * result is the same from run to run.  T = 0 writes zeros into dw_gate and dw_up.
+ * dtype: LORDBA_BF16 or LORDBA_F16.
+ */
+typedef struct lordba_gated_grad {
+    const void *dh, *gate, *up;              /* [device] T x d_hidden, pitches ld_dh, ld_pre, ld_pre  */
+    const void *x;                           /* [device] T x d_in, pitch ldx                          */
+    const void *w_gate, *w_up;               /* [device] d_hidden x d_in, pitch ldw                   */
+    void       *dgate, *dup;                 /* [device] T x d_hidden, pitch ld_dpre                  */
+    void       *dx;                          /* [device] T x d_in, pitch ld_dx, or NULL               */
+    void       *dw_gate, *dw_up;             /* [device] d_hidden x d_in, pitch ld_dw, or both NULL   */
+    int64_t d_in, d_hidden, ld_dh, ld_pre, ldx, ldw, ld_dpre, ld_dx, ld_dw;
+    int32_t act, flags;                      /* flags: 0                                              */
+} lordba_gated_grad;
+
+size_t lordba_gated_backward_workspace_bytes(const lordba_gated_grad *g, int64_t T);
+int lordba_gated_backward(const lordba_gated_grad *g, int64_t T, int dtype, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/*
+ * ---- Dropout --------------------------------------------------------------------------------------
+ *
+ * out[t,c] = residual[t,c] + (keep(t,c) ? x[t,c] * 65536 / (65536 - n) : 0),  n = rint(65536 p)
+ *
+ * keep is a function of (t, c, seed, offset) alone and is never stored: the sixteen-bit number of
+ * element (t,c) is at least n.  The numbers are those of Philox4x32-10 (Salmon, Moraes, Dror and Shaw, SC
+ * 2011) with key (seed low, seed high) and counter (c / 8, t, offset low, offset high): the 128-bit
+ * output holds the numbers of columns 8 (c/8) ... 8 (c/8) + 7, lowest bits first.  So the backward pass is
+ * the same call on the gradient (residual NULL), whatever the pitches.  0 <= p <= 1; the probability is
+ * taken to the nearest 1/65536.  A dropped element contributes an exact zero, also where x is not finite.
+ *
+ * residual may be NULL; out may be x or residual (same pitch), nothing else may overlap it.  dtype: all
+ * three matrices.  T < 2^32, d < 2^34.  One rounding, of the sum.  T = 0 is a no-op.
+ */
+int lordba_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr, void *out, int64_t ldo, int64_t T,
+                   int64_t d, float p, uint64_t seed, uint64_t offset, int dtype, void *stream);
+
 /* Storage of one adapter in bits, Eq. 5: r(d_in+d_out) + 16 ell (d_in+r+d_out). */
 int64_t lordba_adapter_bits(int64_t d_in, int64_t d_out, int r, int ell);
 

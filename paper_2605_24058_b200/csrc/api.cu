@@ -110,16 +110,6 @@ int LaunchSink::emit(LaunchRec rec, const void *arg0, const void *arg1)
 
 namespace {
 
-bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-
-bool overlaps(const void *a, size_t na, const void *b, size_t nb)
-{
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    return a0 < b0 + nb && b0 < a0 + na;
-}
-
-bool known_dtype(int dtype) { return dtype == LORDBA_F32 || dtype == LORDBA_BF16 || dtype == LORDBA_F16; }
-
 int validate_proj(const lordba_proj &p, int64_t T, int dtype)
 {
     if (!known_dtype(dtype)) return LORDBA_EUNSUPPORTED;

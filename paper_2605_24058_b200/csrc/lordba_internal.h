@@ -113,6 +113,59 @@ bool mma_supported(const lordba_proj &p, int64_t T, int dtype);
 int launch_forward_mma(const lordba_proj *projs, const int64_t *tokens, int64_t T, int n, const FamilySelector &sel,
                        LaunchSink &sink, bool batch_checked, int *launches);
 
+// --- elementwise.cu ----------------------------------------------------------
+int launch_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scale, int64_t T, int64_t d,
+                         int dtype, cudaStream_t stream);
+int launch_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr, void *out, int64_t ldo, int64_t T,
+                   int64_t d, int cut, uint64_t seed, uint64_t offset, int dtype, cudaStream_t stream);
+int launch_gated_grad(const lordba_gated_grad &g, int64_t T, int dtype, cudaStream_t stream);
+// dst (pitch ld_dst bytes, a multiple of 16) = src, rows x cols bytes, any alignment of src
+int launch_repack(const void *src, int64_t ld_src, void *dst, int64_t ld_dst, int64_t rows, int64_t cols,
+                  cudaStream_t stream);
+
+// --- product.cu --------------------------------------------------------------
+// D[m,n] = sum_k A[m,k] B[n,k], then an epilogue.  An operand is a row-major matrix; its rows run along m
+// (n) with the contraction contiguous, or, mn_major, along the contraction with m (n) contiguous.
+struct Operand {
+    const void *p;
+    int64_t ld;          // pitch in elements
+    bool mn_major;
+};
+
+enum ProductKind { kProductBf16, kProductF16, kProductInt8 };
+
+struct Product {
+    ProductKind kind;
+    int64_t M, N, K;
+    Operand a[2], b[2];
+    // kSingle: D = A0 B0.  kSum: D = A0 B0 + A1 B1.  kGated: gate = A0 B0, up = A0 B1.
+    // kPair: two products A0 B0 and A1 B0 with an output each.
+    enum Form { kSingle, kSum, kGated, kPair } form;
+    // epilogue
+    void *out[2];                 // [1]: kPair only
+    int64_t ldo;
+    int dtype;                    // of out, add and pre
+    const float *s_row, *s_col[2];    // int8 only: scales per row and per column (of gate and up)
+    const void *add[2];           // kGated only: addends of gate and up, or null
+    void *pre[2];                 // kGated only: where gate and up go, or null
+    int64_t ld_add, ld_pre;
+    int act;
+};
+
+size_t product_workspace_bytes(const Product &p);
+int launch_product(const Product &p, void *workspace, cudaStream_t stream);
+
+// --- argument checks -----------------------------------------------------------
+inline bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+inline bool overlaps(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+    return a0 < b0 + nb && b0 < a0 + na;
+}
+
+inline bool known_dtype(int dtype) { return dtype == LORDBA_F32 || dtype == LORDBA_BF16 || dtype == LORDBA_F16; }
+
 inline int64_t rows_of(const int64_t *tokens, int64_t T, int i) { return tokens ? tokens[i] : T; }
 
 }  // namespace lordba

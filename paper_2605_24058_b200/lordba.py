@@ -24,6 +24,9 @@ PROJ_X_READY = 4
 MAX_ELL = 8
 MAX_PROJS = 4096
 FIT_ALPHA, FIT_BETA, FIT_GAMMA, FIT_ALL = 1, 2, 4, 7
+ACT_SILU, ACT_GELU_TANH = 0, 1
+GATED_INT8 = 1
+INT8_MAX_DIN = 131071
 
 
 def proj_ell(ell: int) -> int:
@@ -45,6 +48,26 @@ class Proj(ctypes.Structure):
     _fields_ = [("x", _vp), ("packed_A", _vp), ("packed_B", _vp), ("s_in", _vp), ("s_r", _vp),
                 ("s_out", _vp), ("y", _vp), ("d_in", _i64), ("d_out", _i64), ("ldx", _i64),
                 ("ldy", _i64), ("r", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class Int8Proj(ctypes.Structure):
+    """Mirror of ``lordba_int8_proj``."""
+    _fields_ = [("x", _vp), ("s_x", _vp), ("w", _vp), ("s_w", _vp), ("y", _vp), ("d_in", _i64), ("d_out", _i64),
+                ("ldx", _i64), ("ldw", _i64), ("ldy", _i64)]
+
+
+class Gated(ctypes.Structure):
+    """Mirror of ``lordba_gated``."""
+    _fields_ = [(n, _vp) for n in ("x", "w_gate", "w_up", "s_x", "s_gate", "s_up", "gate_add", "up_add", "gate", "up", "h")] + [
+        (n, _i64) for n in ("d_in", "d_hidden", "ldx", "ldw", "ld_add", "ld_pre", "ldh")] + [
+        ("act", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class GatedGrad(ctypes.Structure):
+    """Mirror of ``lordba_gated_grad``."""
+    _fields_ = [(n, _vp) for n in ("dh", "gate", "up", "x", "w_gate", "w_up", "dgate", "dup", "dx", "dw_gate", "dw_up")] + [
+        (n, _i64) for n in ("d_in", "d_hidden", "ld_dh", "ld_pre", "ldx", "ldw", "ld_dpre", "ld_dx", "ld_dw")] + [
+        ("act", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
 _SIGNATURES = {
@@ -77,6 +100,15 @@ _SIGNATURES = {
     "lordba_fit_workspace_bytes": (ctypes.c_size_t, [_i64, _i64, ctypes.c_int]),
     "lordba_fit_scales": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, ctypes.c_int, ctypes.c_int,
                                          ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "lordba_int8_quantize_rows": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, ctypes.c_int, _vp]),
+    "lordba_int8_linear_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Int8Proj), _i64]),
+    "lordba_int8_linear": (ctypes.c_int, [ctypes.POINTER(Int8Proj), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "lordba_gated_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Gated), _i64]),
+    "lordba_gated_forward": (ctypes.c_int, [ctypes.POINTER(Gated), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "lordba_gated_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(GatedGrad), _i64]),
+    "lordba_gated_backward": (ctypes.c_int, [ctypes.POINTER(GatedGrad), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "lordba_dropout": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, ctypes.c_float, ctypes.c_uint64,
+                                      ctypes.c_uint64, ctypes.c_int, _vp]),
     "lordba_adapter_bits": (_i64, [_i64, _i64, ctypes.c_int, ctypes.c_int]),
     "lordba_set_variant": (ctypes.c_int, [ctypes.c_int]),
     "lordba_get_variant": (ctypes.c_int, []),
@@ -406,6 +438,234 @@ def fit_scales(target, packed_A, packed_B, s_in, s_r, s_out, r: int, sweeps: int
                                   s_r.data_ptr(), s_out.data_ptr(), d_in, d_out, r, sweeps, axes,
                                   workspace.data_ptr(), workspace.numel(), _stream(stream))
     _check(rc, "lordba_fit_scales")
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
+    """Check a 2-D operand with contiguous rows on the current device; its row pitch in elements."""
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError("%s must be on the current CUDA device" % what)
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError("%s must be (%d, %d), got %s" % (what, rows, cols, tuple(t.shape)))
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError("rows of %s must be contiguous" % what)
+    if rows <= 1:
+        return max(cols, ld)          # a single row has no pitch of its own
+    if ld < cols:
+        raise ValueError("rows of %s overlap" % what)
+    return ld
+
+
+def _vector(t: torch.Tensor, n: int, what: str) -> None:
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise TypeError("%s must be %d contiguous float32 values" % (what, n))
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError("%s must be on the current CUDA device" % what)
+
+
+def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """A new tensor that belongs to the stream the call runs on: its memory is free for that stream's work."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rows(rows: int, cols: int, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """A new rows x cols matrix whose rows start on 16-byte boundaries (what the copy engine takes)."""
+    step = 16 // dtype.itemsize
+    pitch = (cols + step - 1) // step * step
+    out = _empty((rows, pitch), dtype, device, stream)
+    return out if pitch == cols else out[:, :cols]
+
+
+def _workspace(nbytes: int, given: Optional[torch.Tensor], device, stream) -> Optional[torch.Tensor]:
+    """The workspace of a call: the caller's, or one made here."""
+    if given is not None:
+        _need_cuda(given)
+        return given
+    return _empty(nbytes, torch.uint8, device, stream) if nbytes else None
+
+
+def _ws_args(ws: Optional[torch.Tensor]):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def int8_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, stream=None):
+    """Activations (T, d) in bfloat16, float16 or float32 -> (q, scale): int8 rows and one float32 scale a row,
+    scale = max|row| / 127, q = round(row * 127 / max|row|) (ties to even).  q and scale are made here if absent
+    (q with rows on 16-byte boundaries, as int8_linear likes them best) and belong, like all tensors that the calls
+    below make, to the stream the call runs on."""
+    if x.dim() != 2:
+        raise ValueError("x must be (T, d)")
+    T, d = x.shape
+    dtype = _dtype_code(x)
+    ldx = _matrix(x, T, d, x.dtype, "x")
+    if q is None:
+        q = _rows(T, d, torch.int8, x.device, stream)
+    if scale is None:
+        scale = _empty(T, torch.float32, x.device, stream)
+    ldq = _matrix(q, T, d, torch.int8, "q")
+    _vector(scale, T, "scale")
+    _check(load().lordba_int8_quantize_rows(x.data_ptr(), ldx, q.data_ptr(), ldq, scale.data_ptr(), T, d, dtype,
+                                            _stream(stream)), "lordba_int8_quantize_rows")
+    return q, scale
+
+
+def int8_linear(x, s_x, w, s_w, y: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """y[t, n] = s_x[t] s_w[n] sum_k x[t, k] w[n, k] for int8 x (T, d_in) and w (d_out, d_in): the frozen base
+    projection that an adapter's term is added to.  y (of its own type, or of ``dtype`` when made here) is
+    overwritten and returned.  workspace: a uint8 CUDA tensor of lordba_int8_linear_workspace_bytes(), made here
+    if absent; only operands off 16-byte boundaries need one."""
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x must be (T, d_in) and w (d_out, d_in)")
+    T, d_in = x.shape
+    d_out = w.shape[0]
+    if y is None:
+        y = _rows(T, d_out, dtype, x.device, stream)
+    code = _dtype_code(y)
+    _vector(s_x, T, "s_x")
+    _vector(s_w, d_out, "s_w")
+    p = Int8Proj(x.data_ptr(), s_x.data_ptr(), w.data_ptr(), s_w.data_ptr(), y.data_ptr(), d_in, d_out,
+                 _matrix(x, T, d_in, torch.int8, "x"), _matrix(w, d_out, d_in, torch.int8, "w"),
+                 _matrix(y, T, d_out, y.dtype, "y"))
+    lib = load()
+    ref = ctypes.byref(p)
+    ws = _workspace(lib.lordba_int8_linear_workspace_bytes(ref, T), workspace, x.device, stream)
+    _check(lib.lordba_int8_linear(ref, T, code, *_ws_args(ws), _stream(stream)), "lordba_int8_linear")
+    return y
+
+
+def _pair(a, b, what: str):
+    if (a is None) != (b is None):
+        raise ValueError("%s come together" % what)
+    return a is not None
+
+
+def _pair_ld(a, b, rows: int, cols: int, dtype, what: str) -> int:
+    """The pitch that both matrices of a pair have."""
+    ld, ld_b = _matrix(a, rows, cols, dtype, what), _matrix(b, rows, cols, dtype, what)
+    if ld != ld_b:
+        raise ValueError("%s must have one row pitch" % what)
+    return ld
+
+
+def gated_forward(x, w_gate, w_up, h: Optional[torch.Tensor] = None, act: int = ACT_SILU, scales=None,
+                  dtype: Optional[torch.dtype] = None, gate_add=None, up_add=None, gate=None, up=None, save: bool = False,
+                  workspace: Optional[torch.Tensor] = None, stream=None):
+    """(h, gate, up) with g = x w_gate^T + gate_add, u = x w_up^T + up_add, h = act(g) u, in one kernel.
+
+    x (T, d_in), w_gate and w_up (d_hidden, d_in): bfloat16 or float16, or int8 with ``scales`` = (s_x, s_gate,
+    s_up) and ``dtype`` the type of the rest (bfloat16 if not given).  gate_add / up_add: what the adapters of the
+    two projections add.  save=True (or gate and up given) stores g and u for gated_backward; otherwise gate and
+    up come back as None."""
+    if x.dim() != 2 or w_gate.dim() != 2:
+        raise ValueError("x must be (T, d_in), w_gate and w_up (d_hidden, d_in)")
+    T, d_in = x.shape
+    d_hidden = w_gate.shape[0]
+    int8 = x.dtype == torch.int8
+    if int8 != (scales is not None):
+        raise ValueError("int8 operands come with scales = (s_x, s_gate, s_up), others without")
+    if h is not None:
+        dtype = h.dtype
+    elif dtype is None or not int8:
+        dtype = torch.bfloat16 if int8 else x.dtype
+    p = Gated()
+    p.ldx = _matrix(x, T, d_in, x.dtype, "x")
+    p.ldw = _pair_ld(w_gate, w_up, d_hidden, d_in, x.dtype, "w_gate and w_up")
+    if h is None:
+        h = _rows(T, d_hidden, dtype, x.device, stream)
+    code = _dtype_code(h)
+    p.ldh = _matrix(h, T, d_hidden, dtype if int8 else x.dtype, "h")
+    if int8:
+        s_x, s_gate, s_up = scales
+        _vector(s_x, T, "s_x")
+        _vector(s_gate, d_hidden, "s_gate")
+        _vector(s_up, d_hidden, "s_up")
+        p.s_x, p.s_gate, p.s_up, p.flags = s_x.data_ptr(), s_gate.data_ptr(), s_up.data_ptr(), GATED_INT8
+    if _pair(gate_add, up_add, "gate_add and up_add"):
+        p.ld_add = _pair_ld(gate_add, up_add, T, d_hidden, dtype, "gate_add and up_add")
+        p.gate_add, p.up_add = gate_add.data_ptr(), up_add.data_ptr()
+    if not _pair(gate, up, "gate and up") and save:
+        gate, up = (_rows(T, d_hidden, dtype, x.device, stream) for _ in range(2))
+    if gate is not None:
+        p.ld_pre = _pair_ld(gate, up, T, d_hidden, dtype, "gate and up")
+        p.gate, p.up = gate.data_ptr(), up.data_ptr()
+    p.x, p.w_gate, p.w_up, p.h = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr()
+    p.d_in, p.d_hidden, p.act = d_in, d_hidden, act
+    lib = load()
+    ref = ctypes.byref(p)
+    ws = _workspace(lib.lordba_gated_workspace_bytes(ref, T), workspace, x.device, stream)
+    _check(lib.lordba_gated_forward(ref, T, code, *_ws_args(ws), _stream(stream)), "lordba_gated_forward")
+    return h, gate, up
+
+
+def gated_backward(dh, gate, up, x=None, w_gate=None, w_up=None, dgate=None, dup=None, dx=None, dw_gate=None, dw_up=None,
+                   act: int = ACT_SILU, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dgate, dup, dx, dw_gate, dw_up) from the gradient dh of h and the gate / up that gated_forward stored.
+
+    dgate and dup (the gradients of gate_add and up_add) are always made.  dx is made when w_gate and w_up are
+    given, dw_gate and dw_up when x is given (None: frozen weights); what is not made comes back as None."""
+    if dh.dim() != 2:
+        raise ValueError("dh must be (T, d_hidden)")
+    T, d_hidden = dh.shape
+    dtype, code = dh.dtype, _dtype_code(dh)
+    p = GatedGrad()
+    p.ld_dh = _matrix(dh, T, d_hidden, dtype, "dh")
+    p.ld_pre = _pair_ld(gate, up, T, d_hidden, dtype, "gate and up")
+    if not _pair(dgate, dup, "dgate and dup"):
+        dgate, dup = (_rows(T, d_hidden, dtype, dh.device, stream) for _ in range(2))
+    p.ld_dpre = _pair_ld(dgate, dup, T, d_hidden, dtype, "dgate and dup")
+    p.dh, p.gate, p.up, p.dgate, p.dup = dh.data_ptr(), gate.data_ptr(), up.data_ptr(), dgate.data_ptr(), dup.data_ptr()
+    d_in = 1
+    if _pair(w_gate, w_up, "w_gate and w_up"):
+        d_in = w_gate.shape[1]
+        p.ldw = _pair_ld(w_gate, w_up, d_hidden, d_in, dtype, "w_gate and w_up")
+        if dx is None:
+            dx = _rows(T, d_in, dtype, dh.device, stream)
+        p.ld_dx = _matrix(dx, T, d_in, dtype, "dx")
+        p.w_gate, p.w_up, p.dx = w_gate.data_ptr(), w_up.data_ptr(), dx.data_ptr()
+    elif dx is not None:
+        raise ValueError("dx needs w_gate and w_up")
+    if x is not None:
+        if w_gate is not None and x.shape[1] != d_in:
+            raise ValueError("x must be (T, d_in)")
+        d_in = x.shape[1]
+        p.ldx = _matrix(x, T, d_in, dtype, "x")
+        if not _pair(dw_gate, dw_up, "dw_gate and dw_up"):
+            dw_gate, dw_up = (_rows(d_hidden, d_in, dtype, dh.device, stream) for _ in range(2))
+        p.ld_dw = _pair_ld(dw_gate, dw_up, d_hidden, d_in, dtype, "dw_gate and dw_up")
+        p.x, p.dw_gate, p.dw_up = x.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr()
+    elif dw_gate is not None or dw_up is not None:
+        raise ValueError("dw_gate and dw_up need x")
+    p.d_in, p.d_hidden, p.act = d_in, d_hidden, act
+    lib = load()
+    ref = ctypes.byref(p)
+    ws = _workspace(lib.lordba_gated_backward_workspace_bytes(ref, T), workspace, dh.device, stream)
+    _check(lib.lordba_gated_backward(ref, T, code, *_ws_args(ws), _stream(stream)), "lordba_gated_backward")
+    return dgate, dup, dx, dw_gate, dw_up
+
+
+def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out: Optional[torch.Tensor] = None,
+            stream=None) -> torch.Tensor:
+    """out = residual + (keep ? x / (1 - p) : 0), p to the nearest 1/65536; keep follows from (row, column, seed,
+    offset), so the same call on the gradient (without a residual) is the backward pass.  out may be x or residual."""
+    if x.dim() != 2:
+        raise ValueError("x must be (T, d)")
+    T, d = x.shape
+    ldx = _matrix(x, T, d, x.dtype, "x")
+    code = _dtype_code(x)
+    if out is None:
+        out = _rows(T, d, x.dtype, x.device, stream)
+    ldo = _matrix(out, T, d, x.dtype, "out")
+    rp, ldr = (None, 0) if residual is None else (residual.data_ptr(), _matrix(residual, T, d, x.dtype, "residual"))
+    mask = (1 << 64) - 1
+    _check(load().lordba_dropout(x.data_ptr(), ldx, rp, ldr, out.data_ptr(), ldo, T, d, p, seed & mask, offset & mask, code,
+                                 _stream(stream)), "lordba_dropout")
+    return out
 
 
 def adapter_bits(d_in: int, d_out: int, r: int, ell: int = 1) -> int:
