@@ -1,140 +1,110 @@
-// Products with an epilogue: the 8-bit base projection, the gated block and its gradients.
-//
-// One kernel for every form, type, size, pitch and alignment: 64 x 64 outputs a block, the operands
-// staged in shared memory 16 contraction steps at a time as 32-bit values, sums in 32-bit integers (int8)
-// or floats.
-#include "block_common.cuh"
+// Products with an epilogue: the 8-bit base projection, the gated block and its gradients.  Operands that the
+// copy engine cannot take are copied into the workspace first; the number of rows chooses the kernel.
+#include <mutex>
+
+#include "product_internal.cuh"
 
 namespace lordba {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiledFn encode_fn()
+{
+    static EncodeTiledFn fn = []() -> EncodeTiledFn {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            return nullptr;
+        return reinterpret_cast<EncodeTiledFn>(p);
+    }();
+    return fn;
+}
+
+bool encode_map(CUtensorMap *map, const void *p, int64_t rows, int64_t cols, int64_t ld, int e, int box_rows)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * e};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / e), (cuuint32_t)box_rows}, step[2] = {1, 1};
+    // 16-bit elements keep their bits whatever they are called here
+    return fn(map, e == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(p), dims,
+              strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int sm_count()
+{
+    static std::mutex mu;
+    static int count[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+    std::lock_guard<std::mutex> lock(mu);
+    if (count[dev] == 0 && (cudaDeviceGetAttribute(&count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || count[dev] < 1))
+        count[dev] = 148;
+    return count[dev];
+}
+
 namespace {
 
-constexpr int kTile = 64, kStep = 16;
+int elt_of(const Product &p) { return p.kind == kProductInt8 ? 1 : 2; }
 
-struct Side {
-    const void *p;
-    int64_t ld;
-    int mn_major;
-};
+// Rows and columns of an operand as it lies in memory.
+int64_t rows_of(const Operand &o, int64_t mn, int64_t k) { return o.mn_major ? k : mn; }
+int64_t cols_of(const Operand &o, int64_t mn, int64_t k) { return o.mn_major ? mn : k; }
 
-struct SimpleArgs {
-    Side a[2], b[2];
-    int64_t M, N, K;
-    int form, kind;
-    void *out[2];
-    int64_t ldo;
-    int dtype;
-    const float *s_row, *s_col[2];
-    const void *add[2];
-    void *pre[2];
-    int64_t ld_add, ld_pre;
-    int act;
-};
+bool taken_as_is(const Operand &o, int e) { return !o.p || (aligned(o.p, 16) && (o.ld * e) % 16 == 0); }
 
-__device__ __forceinline__ float load_any(const void *p, int64_t i, int dtype)
+size_t packed_pitch(const Operand &o, int64_t mn, int64_t k, int e) { return ((size_t)cols_of(o, mn, k) * e + 15) / 16 * 16; }
+
+size_t packed_bytes(const Operand &o, int64_t mn, int64_t k, int e)
 {
-    if (dtype == LORDBA_F32) return static_cast<const float *>(p)[i];
-    if (dtype == LORDBA_BF16) return to_float(static_cast<const __nv_bfloat16 *>(p)[i]);
-    return to_float(static_cast<const __half *>(p)[i]);
+    return taken_as_is(o, e) ? 0 : (packed_pitch(o, mn, k, e) * (size_t)rows_of(o, mn, k) + 255) / 256 * 256;
 }
 
-__device__ __forceinline__ void store_any(void *p, int64_t i, int dtype, float v)
-{
-    if (dtype == LORDBA_F32) static_cast<float *>(p)[i] = v;
-    else if (dtype == LORDBA_BF16) static_cast<__nv_bfloat16 *>(p)[i] = from_float<__nv_bfloat16>(v);
-    else static_cast<__half *>(p)[i] = from_float<__half>(v);
-}
-
-template <typename Acc>
-__device__ __forceinline__ Acc element(const Side &s, int kind, int64_t mn, int64_t k)
-{
-    const int64_t i = s.mn_major ? k * s.ld + mn : mn * s.ld + k;
-    if (kind == kProductInt8) return (Acc) static_cast<const int8_t *>(s.p)[i];
-    return (Acc)load_any(s.p, i, kind == kProductBf16 ? LORDBA_BF16 : LORDBA_F16);
-}
-
-template <typename Acc>
-__global__ void __launch_bounds__(256)
-product_kernel(const SimpleArgs P)
-{
-    __shared__ Acc As[kStep][kTile + 1], Bs[2][kStep][kTile + 1];
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    const int64_t n0 = (int64_t)blockIdx.x * kTile;
-    const int problem = P.form == Product::kPair ? blockIdx.z : 0;
-    const int parts = P.form == Product::kSum ? 2 : 1, cols = P.form == Product::kGated ? 2 : 1;
-    grid_wait();
-    grid_release();
-    for (int64_t m0 = (int64_t)blockIdx.y * kTile; m0 < P.M; m0 += (int64_t)gridDim.y * kTile) {
-        Acc acc[2][4][4] = {};
-        for (int part = 0; part < parts; ++part) {
-            const Side &a = P.a[P.form == Product::kPair ? problem : part];
-            for (int64_t k0 = 0; k0 < P.K; k0 += kStep) {
-                __syncthreads();
-                for (int e = threadIdx.x; e < kTile * kStep; e += 256) {
-                    const int am = a.mn_major ? e % kTile : e / kStep, ak = a.mn_major ? e / kTile : e % kStep;
-                    As[ak][am] = m0 + am < P.M && k0 + ak < P.K ? element<Acc>(a, P.kind, m0 + am, k0 + ak) : (Acc)0;
-                    for (int c = 0; c < cols; ++c) {
-                        const Side &b = P.b[cols == 2 ? c : part];
-                        const int bn = b.mn_major ? e % kTile : e / kStep, bk = b.mn_major ? e / kTile : e % kStep;
-                        Bs[c][bk][bn] = n0 + bn < P.N && k0 + bk < P.K ? element<Acc>(b, P.kind, n0 + bn, k0 + bk) : (Acc)0;
-                    }
-                }
-                __syncthreads();
-#pragma unroll
-                for (int k = 0; k < kStep; ++k)
-                    for (int c = 0; c < cols; ++c)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) acc[c][i][j] += As[k][ty + 16 * i] * Bs[c][k][tx + 16 * j];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-                if (m >= P.M || n >= P.N) continue;
-                float v[2] = {(float)acc[0][i][j], (float)acc[1][i][j]};
-                for (int c = 0; c < cols; ++c) {
-                    if (P.kind == kProductInt8) v[c] = v[c] * P.s_row[m] * P.s_col[c][n];
-                    if (P.add[c]) v[c] += load_any(P.add[c], m * P.ld_add + n, P.dtype);
-                    if (P.pre[c]) store_any(P.pre[c], m * P.ld_pre + n, P.dtype, v[c]);
-                }
-                if (cols == 2)
-                    v[0] = (P.act == LORDBA_ACT_SILU ? act_gate<LORDBA_ACT_SILU>(v[0]) : act_gate<LORDBA_ACT_GELU_TANH>(v[0])) * v[1];
-                store_any(P.out[problem], m * P.ldo + n, P.dtype, v[0]);
-            }
-    }
-}
+bool rows_vec(const void *p, int64_t ld, size_t e) { return aligned(p, 16) && ((size_t)ld * e) % 16 == 0; }
 
 }  // namespace
 
 size_t product_workspace_bytes(const Product &p)
 {
-    (void)p;
-    return 0;
+    size_t n = 0;
+    for (int i = 0; i < 2; ++i) n += packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + packed_bytes(p.b[i], p.N, p.K, elt_of(p));
+    return n;
 }
 
-int launch_product(const Product &p, void *workspace, cudaStream_t stream)
+int launch_product(const Product &given, void *workspace, cudaStream_t stream)
 {
-    (void)workspace;
-    SimpleArgs a = {};
-    for (int i = 0; i < 2; ++i) {
-        a.a[i] = Side{p.a[i].p, p.a[i].ld, p.a[i].mn_major};
-        a.b[i] = Side{p.b[i].p, p.b[i].ld, p.b[i].mn_major};
-        a.out[i] = p.out[i];
-        a.s_col[i] = p.s_col[i];
-        a.add[i] = p.add[i];
-        a.pre[i] = p.pre[i];
+    Product p = given;
+    const int e = elt_of(p);
+    uint8_t *next = static_cast<uint8_t *>(workspace);
+    for (int i = 0; i < 4; ++i) {
+        Operand &o = i < 2 ? p.a[i] : p.b[i - 2];
+        const int64_t mn = i < 2 ? p.M : p.N;
+        if (taken_as_is(o, e)) continue;
+        const int64_t pitch = (int64_t)packed_pitch(o, mn, p.K, e);
+        const int rc = launch_repack(o.p, o.ld * e, next, pitch, rows_of(o, mn, p.K), cols_of(o, mn, p.K) * e, stream);
+        if (rc != LORDBA_OK) return rc;
+        const size_t bytes = packed_bytes(o, mn, p.K, e);
+        o.p = next;
+        o.ld = pitch / e;
+        next += bytes;
     }
-    a.M = p.M; a.N = p.N; a.K = p.K;
-    a.form = p.form; a.kind = p.kind;
-    a.ldo = p.ldo; a.dtype = p.dtype; a.s_row = p.s_row;
-    a.ld_add = p.ld_add; a.ld_pre = p.ld_pre; a.act = p.act;
-    const int64_t gy = (p.M + kTile - 1) / kTile;
-    const dim3 grid((unsigned)((p.N + kTile - 1) / kTile), (unsigned)(gy < 65535 ? gy : 65535), p.form == Product::kPair ? 2 : 1);
-    return p.kind == kProductInt8 ? launch_kernel(product_kernel<int>, grid, 256, 0, stream, a)
-                                  : launch_kernel(product_kernel<float>, grid, 256, 0, stream, a);
+    Finish f = {};
+    for (int i = 0; i < 2; ++i) {
+        f.out[i] = p.out[i]; f.s_col[i] = p.s_col[i]; f.add[i] = p.add[i]; f.pre[i] = p.pre[i];
+    }
+    f.ldo = p.ldo; f.s_row = p.s_row; f.ld_add = p.ld_add; f.ld_pre = p.ld_pre;
+    f.M = p.M; f.N = p.N; f.dtype = p.dtype; f.act = p.act;
+    const size_t eo = p.dtype == LORDBA_F32 ? 4 : 2;
+    f.vec_out = rows_vec(p.out[0], p.ldo, eo) && aligned(p.out[1], 16);
+    f.vec_add = rows_vec(p.add[0], p.ld_add, eo) && aligned(p.add[1], 16);
+    f.vec_pre = rows_vec(p.pre[0], p.ld_pre, eo) && aligned(p.pre[1], 16);
+    if (p.form != Product::kPair && p.M <= 256) return launch_product_stream(p, f, stream);
+    return launch_product_tile(p, f, stream);
 }
 
 }  // namespace lordba

@@ -1,0 +1,308 @@
+// The product kernel for many rows: 256 x 256 outputs a CTA pair on tcgen05 (cta_group::2), persistent.
+//
+//   D[m,n] = sum_k A[m,k] B[n,k]; 16-bit operands with sums in float32, int8 with sums in int32.
+//
+// Bound: the tensor core.  A pair's two SMs each hold 128 rows of A and 128 of the 256 rows of B (of the
+// gated form: one the gate's, the other up's 128 rows, so that g and u of the same outputs land in the
+// same thread), 128 bytes of the contraction a stage: 32 KB of loads per 128 x 256 x 64 products (16-bit),
+// half of what two lone SMs would load, in a ring of six stages.  An accumulator is 256 of the 512 TMEM
+// columns: while the epilogue drains one, the next tile is summed into the other.
+//
+//   warp 0      copies: both CTAs' producers fill their own halves; every copy completes on the leader's barrier
+//   warp 1      the leader's issues all MMAs (one thread) and frees stages and accumulators in both CTAs
+//   warps 4-11  epilogue: two warps per TMEM lane quadrant, each half of the columns
+//
+// Operands come contraction-contiguous or (gradients) m- or n-contiguous: then a stage holds 64 contraction
+// steps as rows of 64 columns and the MMA reads it transposed.
+#include <cstring>
+#include <mutex>
+
+#include "product_internal.cuh"
+
+namespace lordba {
+namespace {
+
+using namespace sm100;
+
+constexpr int kStages = 6;
+constexpr int kHalf = 128 * 128;                   // bytes of one CTA's half of an operand in a stage
+constexpr int kStageBytes = 2 * kHalf;
+constexpr int kTileM = 256;
+constexpr int kTileThreads = 12 * 32;
+constexpr int kEpiWarps = 8;
+constexpr int kBarBytes = (2 * kStages + 4) * 8 + 16;
+constexpr int kTileSmem = kStages * kStageBytes + kBarBytes + 1024;
+
+struct TileArgs {
+    CUtensorMap a[2], b[2];
+    Finish f;
+    int k_blocks;          // stages per operand pair
+    int parts;             // operand pairs summed into one accumulator
+    int tiles_m, tiles_n, tiles, problems;
+    int skip;              // -1; the test-hooks build can name a stage whose copies are left out
+    int *status;
+    uint32_t idesc;
+};
+
+// Tiles in groups of eight rows of tiles (2048 rows), m fastest: the pairs at work share a few columns of
+// tiles of B and the group's rows of A, which L2 holds, and B is read from HBM once a group.
+struct Tile { int m, n, problem; };
+__device__ __forceinline__ Tile tile_at(const TileArgs &P, int i)
+{
+    const int per = P.tiles_m * P.tiles_n;
+    Tile t;
+    t.problem = P.problems > 1 ? i / per : 0;
+    i -= t.problem * per;
+    const int group = i / (8 * P.tiles_n), first = group * 8;
+    const int rows = P.tiles_m - first < 8 ? P.tiles_m - first : 8;
+    i -= group * 8 * P.tiles_n;
+    t.n = i / rows;
+    t.m = first + i - t.n * rows;
+    return t;
+}
+
+template <bool INT8, bool GATED, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(kTileThreads, 1)
+product_tile_kernel(const __grid_constant__ TileArgs P)
+{
+    extern __shared__ uint8_t smem_raw[];
+    constexpr int kTileN = GATED ? 128 : 256;        // columns of the output
+    constexpr int kBlockK = INT8 ? 128 : 64;
+    const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t bars = base + kStages * kStageBytes;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (kStages + s); };
+    auto sum_full = [&](int b) { return bars + 8u * (2 * kStages + b); };
+    auto sum_empty = [&](int b) { return bars + 8u * (2 * kStages + 2 + b); };
+    uint8_t *misc = smem_raw + (bars - smem_addr(smem_raw)) + (2 * kStages + 4) * 8;
+    volatile uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(misc);
+    volatile int *abort_flag = reinterpret_cast<int *>(misc + 4);
+    const Bounded bound{abort_flag, P.status};
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = cluster_rank();
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const int blocks = P.k_blocks * P.parts;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(full(s), 1);
+            bar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            bar_init(sum_full(b), 1);
+            bar_init(sum_empty(b), 2 * kEpiWarps);
+        }
+        *abort_flag = 0;
+        bar_init_fence();
+    }
+    if (warp == 1) tmem_alloc<2>(smem_addr(misc), 512);
+    if (warp == 2 && lane == 0) {
+        prefetch_map(&P.a[0]);
+        prefetch_map(&P.b[GATED ? rank : 0]);
+    }
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+    grid_wait();
+    grid_release();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            Ring r;
+            bool alive = true;
+            int count = 0;
+            for (int i = pair; i < P.tiles; i += pairs) {
+                const Tile t = tile_at(P, i);
+                const int m0 = t.m * kTileM + 128 * rank;
+                const int n0 = t.n * kTileN + (GATED ? 0 : 128 * (int)rank);
+                for (int kb = 0; kb < blocks; ++kb, ++count) {
+                    alive = alive && bound.wait(empty(r.stage), r.phase ^ 1u, kDevTmaWaitTimeout);
+                    if (!alive) break;
+                    if (rank == 0) bar_expect(full(r.stage), 2 * kStageBytes);
+                    if (count != P.skip) {
+                        const int part = kb >= P.k_blocks ? 1 : 0;
+                        const int k0 = (kb - part * P.k_blocks) * kBlockK;
+                        const CUtensorMap *ma = &P.a[P.problems > 1 ? t.problem : part];
+                        const CUtensorMap *mb = &P.b[GATED ? (int)rank : part];
+                        const uint32_t sa = base + r.stage * kStageBytes, sb = sa + kHalf;
+                        const uint32_t bar = peer_addr(full(r.stage), 0);
+                        if (A_MN) {
+                            load_tile_pair(sa, ma, m0, k0, bar);
+                            load_tile_pair(sa + kHalf / 2, ma, m0 + 64, k0, bar);
+                        } else {
+                            load_tile_pair(sa, ma, k0, m0, bar);
+                        }
+                        if (B_MN) {
+                            load_tile_pair(sb, mb, n0, k0, bar);
+                            load_tile_pair(sb + kHalf / 2, mb, n0 + 64, k0, bar);
+                        } else {
+                            load_tile_pair(sb, mb, k0, n0, bar);
+                        }
+                    }
+                    r.next(kStages);
+                }
+                if (!alive) break;
+            }
+            // the MMAs' last arrivals on this CTA's barriers come before it leaves
+            for (int s = 0; alive && s < kStages; ++s) {
+                alive = bound.wait(empty(r.stage), r.phase ^ 1u, kDevTmaWaitTimeout);
+                r.next(kStages);
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && lane == 0) {
+            Ring r;
+            bool alive = true;
+            int buf = 0;
+            uint32_t buf_phase = 0;
+            for (int i = pair; alive && i < P.tiles; i += pairs) {
+                alive = bound.wait(sum_empty(buf), buf_phase ^ 1u, kDevEpilogueWaitTimeout);
+                if (!alive) break;
+                fence_after();
+                const uint32_t d = tmem + 256u * buf;
+                for (int kb = 0; kb < blocks; ++kb) {
+                    alive = bound.wait(full(r.stage), r.phase, kDevMmaWaitTimeout);
+                    if (!alive) break;
+                    fence_after();
+                    const uint32_t sa = base + r.stage * kStageBytes;
+                    const uint32_t a = desc_low(sa, A_MN ? kHalf / 2 : 0), b = desc_low(sa + kHalf, B_MN ? kHalf / 2 : 0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)      // 32 bytes of the contraction each (16 rows where m or n is contiguous)
+                        mma<2, INT8>(d, a + j * (A_MN ? 128 : 2), b + j * (B_MN ? 128 : 2), P.idesc, kb + j > 0);
+                    mma_commit<2>(empty(r.stage));
+                    r.next(kStages);
+                }
+                if (alive) mma_commit<2>(sum_full(buf));
+                buf ^= 1;
+                buf_phase ^= buf == 0;
+            }
+        }
+    } else if (warp >= 4) {
+        const int quadrant = warp % 4, half = (warp - 4) / 4;
+        constexpr int kCols = kTileN / 2;                      // columns of one warp
+        int buf = 0;
+        uint32_t buf_phase = 0;
+        bool alive = true;
+        for (int i = pair; i < P.tiles; i += pairs) {
+            const Tile t = tile_at(P, i);
+            const int64_t m = (int64_t)t.m * kTileM + 128 * rank + 32 * quadrant + lane;
+            const int64_t n0 = (int64_t)t.n * kTileN + kCols * half;
+            alive = __all_sync(0xffffffffu, bound.wait(sum_full(buf), buf_phase, kDevEpilogueWaitTimeout));
+            if (!alive) break;
+            fence_after();
+            const uint32_t d = tmem + ((uint32_t)(32 * quadrant) << 16) + 256u * buf + kCols * half;
+#pragma unroll 1
+            for (int c = 0; c < kCols; c += 16) {
+                uint32_t g[16], u[16];
+                tmem_load16(d + c, g);
+                if (GATED) tmem_load16(d + 128 + c, u);
+                tmem_wait_load();
+                if (m < P.f.M && n0 + c < P.f.N) finish_row<INT8, GATED, 16>(P.f, t.problem, m, n0 + c, g, u);
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(peer_addr(sum_empty(buf), 0));
+            buf ^= 1;
+            buf_phase ^= buf == 0;
+        }
+    }
+
+    if (*abort_flag) {
+        // time for copies still in flight to land before the CTA goes away
+        const long long start = clock64();
+        while (clock64() - start < 2000000LL) __nanosleep(1000);
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (warp == 1) {
+        fence_after();
+        tmem_free<2>(tmem, 512);
+    }
+}
+
+template <bool INT8, bool GATED, bool A_MN, bool B_MN>
+int launch_tile(const TileArgs &args, cudaStream_t stream)
+{
+    const void *func = reinterpret_cast<const void *>(&product_tile_kernel<INT8, GATED, A_MN, B_MN>);
+    // co-resident pairs, asked for once a device: the query is slow
+    static std::mutex mu;
+    static int pairs_of[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return LORDBA_ECUDA;
+    int pairs;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (pairs_of[dev] == 0) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(2, 1, 1);
+            cfg.blockDim = dim3(kTileThreads, 1, 1);
+            cfg.dynamicSmemBytes = kTileSmem;
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            int n = 0;
+            if (cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmem) != cudaSuccess ||
+                cudaOccupancyMaxActiveClusters(&n, func, &cfg) != cudaSuccess || n < 1) {
+                cudaGetLastError();
+                return LORDBA_ECUDA;
+            }
+            pairs_of[dev] = n;
+        }
+        pairs = pairs_of[dev];
+    }
+    LaunchRec rec;
+    std::memset(&rec, 0, sizeof(rec));
+    rec.func = func;
+    rec.grid[0] = 2u * (unsigned)(args.tiles < pairs ? args.tiles : pairs);
+    rec.grid[1] = rec.grid[2] = 1;
+    rec.block = kTileThreads;
+    rec.smem = kTileSmem;
+    rec.cluster = 2;
+    rec.pdl = 1;
+    rec.n_args = 1;
+    rec.arg_bytes[0] = sizeof(TileArgs);
+    return launch_record(rec, &args, nullptr, stream);
+}
+
+}  // namespace
+
+int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
+{
+    const bool int8 = p.kind == kProductInt8, gated = p.form == Product::kGated, pair = p.form == Product::kPair;
+    const int e = int8 ? 1 : 2, block_k = int8 ? 128 : 64;
+    TileArgs a;
+    std::memset(&a, 0, sizeof(a));
+    for (int i = 0; i < 2; ++i) {
+        const Operand &oa = p.a[i], &ob = p.b[i];
+        if (oa.p && !(oa.mn_major ? encode_map(&a.a[i], oa.p, p.K, p.M, oa.ld, e, 64) : encode_map(&a.a[i], oa.p, p.M, p.K, oa.ld, e, 128)))
+            return LORDBA_ECUDA;
+        if (ob.p && !(ob.mn_major ? encode_map(&a.b[i], ob.p, p.K, p.N, ob.ld, e, 64) : encode_map(&a.b[i], ob.p, p.N, p.K, ob.ld, e, 128)))
+            return LORDBA_ECUDA;
+    }
+    const bool a_mn = p.a[0].mn_major, b_mn = p.b[0].mn_major;
+    a.f = f;
+    a.k_blocks = (int)((p.K + block_k - 1) / block_k);
+    a.parts = p.form == Product::kSum ? 2 : 1;
+    a.problems = pair ? 2 : 1;
+    const int64_t tm = (p.M + kTileM - 1) / kTileM, tn = (p.N + (gated ? 127 : 255)) / (gated ? 128 : 256);
+    if (tm * tn * a.problems > (int64_t)1 << 30) return LORDBA_EUNSUPPORTED;
+    a.tiles_m = (int)tm; a.tiles_n = (int)tn;
+    a.tiles = (int)(tm * tn) * a.problems;
+    a.skip = test_skip_item();
+    a.status = device_status_word();
+    if (!a.status) return LORDBA_ECUDA;
+    a.idesc = instr_desc(int8, p.kind == kProductBf16, a_mn, b_mn, 256, 256);
+    if (int8) return gated ? launch_tile<true, true, false, false>(a, stream) : launch_tile<true, false, false, false>(a, stream);
+    if (gated) return launch_tile<false, true, false, false>(a, stream);
+    if (pair) return launch_tile<false, false, true, true>(a, stream);
+    return launch_tile<false, false, false, true>(a, stream);
+}
+
+}  // namespace lordba
