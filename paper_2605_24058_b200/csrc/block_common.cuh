@@ -79,6 +79,38 @@ __device__ __forceinline__ void store_group(E *p, const float v[8])
     }
 }
 
+// Sixteen bytes at an address that is `by` (0 ... 15) past an aligned one, from the two aligned pieces there.
+__device__ __forceinline__ uint4 join_pieces(uint4 a, uint4 b, uint32_t by)
+{
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const bool eight = by & 8u, four = by & 4u;
+    const uint32_t shift = 8 * (by & 3u);
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = eight ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = four ? w[i + 1] : w[i];
+    return make_uint4(__funnelshift_r(w[0], w[1], shift), __funnelshift_r(w[1], w[2], shift),
+                      __funnelshift_r(w[2], w[3], shift), __funnelshift_r(w[3], w[4], shift));
+}
+
+// The sixteen bytes at any address at < end; bytes from `end` on read as zero, and an aligned piece is read
+// only when it holds a byte before `end`.
+__device__ __forceinline__ uint4 load_bytes16(uintptr_t at, uintptr_t end)
+{
+    const uintptr_t first = at & ~(uintptr_t)15;
+    const uintptr_t second = (at & 15) && first + 16 < end ? first + 16 : first;
+    const uint4 v = join_pieces(__ldg(reinterpret_cast<const uint4 *>(first)), __ldg(reinterpret_cast<const uint4 *>(second)),
+                                (uint32_t)at & 15u);
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const int left = end - at < 16 ? (int)(end - at) : 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int bytes = left - 4 * i;
+        w[i] &= bytes >= 4 ? 0xffffffffu : bytes <= 0 ? 0u : (1u << 8 * bytes) - 1u;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Programmatic dependent launch: a kernel's first global access comes after grid_wait(), so that the
 // kernels before it are complete; its successor may become resident as soon as every CTA has passed
 // grid_release().

@@ -119,9 +119,16 @@ int launch_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ldq, flo
 int launch_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr, void *out, int64_t ldo, int64_t T,
                    int64_t d, int cut, uint64_t seed, uint64_t offset, int dtype, cudaStream_t stream);
 int launch_gated_grad(const lordba_gated_grad &g, int64_t T, int dtype, cudaStream_t stream);
-// dst (pitch ld_dst bytes, a multiple of 16) = src, rows x cols bytes, any alignment of src
-int launch_repack(const void *src, int64_t ld_src, void *dst, int64_t ld_dst, int64_t rows, int64_t cols,
-                  cudaStream_t stream);
+// Copies that give operands a pitch of 16-byte multiples: rows x cols bytes each, any alignment of src.
+struct RepackList {
+    struct Item {
+        const void *src;
+        void *dst;
+        int64_t ld_src, ld_dst, rows, cols;      // bytes
+    } item[4];
+    int n;
+};
+int launch_repack(const RepackList &list, cudaStream_t stream);
 
 // --- product.cu --------------------------------------------------------------
 // D[m,n] = sum_k A[m,k] B[n,k], then an epilogue.  An operand is a row-major matrix; its rows run along m

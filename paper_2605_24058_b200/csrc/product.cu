@@ -56,13 +56,25 @@ int elt_of(const Product &p) { return p.kind == kProductInt8 ? 1 : 2; }
 int64_t rows_of(const Operand &o, int64_t mn, int64_t k) { return o.mn_major ? k : mn; }
 int64_t cols_of(const Operand &o, int64_t mn, int64_t k) { return o.mn_major ? mn : k; }
 
-bool taken_as_is(const Operand &o, int e) { return !o.p || (aligned(o.p, 16) && (o.ld * e) % 16 == 0); }
-
 size_t packed_pitch(const Operand &o, int64_t mn, int64_t k, int e) { return ((size_t)cols_of(o, mn, k) * e + 15) / 16 * 16; }
 
 size_t packed_bytes(const Operand &o, int64_t mn, int64_t k, int e)
 {
     return taken_as_is(o, e) ? 0 : (packed_pitch(o, mn, k, e) * (size_t)rows_of(o, mn, k) + 255) / 256 * 256;
+}
+
+// Few rows: the weights stream past them.  Many: tiles, if need be of copies of the operands, which cost a
+// launch and three passes over their bytes.  A sum over the tokens has no weights to stream.
+// Measured, 8-bit 4096 x 4096: 64 rows 8 us streaming, 16 us in tiles; 512 rows 16 and 17 us; 2048 rows 47 and
+// 31 us.  Gated, 16-bit 4096 x 11008: 64 rows 42 and 51 us, 256 rows 96 and 52 us.
+bool streams(const Product &p)
+{
+    if (p.form == Product::kPair) return false;
+    const double stream = stream_estimate(p);
+    if (stream < 0) return false;
+    double copied = 0;
+    for (int i = 0; i < 2; ++i) copied += (double)packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + (double)packed_bytes(p.b[i], p.N, p.K, elt_of(p));
+    return stream <= tile_estimate(p) + (copied > 0 ? 3.0 + copied * 3 / 6.0e6 : 0.0);
 }
 
 bool rows_vec(const void *p, int64_t ld, size_t e) { return aligned(p, 16) && ((size_t)ld * e) % 16 == 0; }
@@ -72,6 +84,7 @@ bool rows_vec(const void *p, int64_t ld, size_t e) { return aligned(p, 16) && ((
 size_t product_workspace_bytes(const Product &p)
 {
     size_t n = 0;
+    if (streams(p)) return 0;
     for (int i = 0; i < 2; ++i) n += packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + packed_bytes(p.b[i], p.N, p.K, elt_of(p));
     return n;
 }
@@ -81,18 +94,21 @@ int launch_product(const Product &given, void *workspace, cudaStream_t stream)
     Product p = given;
     const int e = elt_of(p);
     uint8_t *next = static_cast<uint8_t *>(workspace);
+    RepackList list = {};
+    const bool stream_it = streams(p);
     for (int i = 0; i < 4; ++i) {
         Operand &o = i < 2 ? p.a[i] : p.b[i - 2];
         const int64_t mn = i < 2 ? p.M : p.N;
-        if (taken_as_is(o, e)) continue;
+        if (stream_it || taken_as_is(o, e)) continue;
         const int64_t pitch = (int64_t)packed_pitch(o, mn, p.K, e);
-        const int rc = launch_repack(o.p, o.ld * e, next, pitch, rows_of(o, mn, p.K), cols_of(o, mn, p.K) * e, stream);
-        if (rc != LORDBA_OK) return rc;
+        list.item[list.n++] = RepackList::Item{o.p, next, o.ld * e, pitch, rows_of(o, mn, p.K), cols_of(o, mn, p.K) * e};
         const size_t bytes = packed_bytes(o, mn, p.K, e);
         o.p = next;
         o.ld = pitch / e;
         next += bytes;
     }
+    const int rc = launch_repack(list, stream);
+    if (rc != LORDBA_OK) return rc;
     Finish f = {};
     for (int i = 0; i < 2; ++i) {
         f.out[i] = p.out[i]; f.s_col[i] = p.s_col[i]; f.add[i] = p.add[i]; f.pre[i] = p.pre[i];
@@ -103,7 +119,7 @@ int launch_product(const Product &given, void *workspace, cudaStream_t stream)
     f.vec_out = rows_vec(p.out[0], p.ldo, eo) && aligned(p.out[1], 16);
     f.vec_add = rows_vec(p.add[0], p.ld_add, eo) && aligned(p.add[1], 16);
     f.vec_pre = rows_vec(p.pre[0], p.ld_pre, eo) && aligned(p.pre[1], 16);
-    if (p.form != Product::kPair && p.M <= 256) return launch_product_stream(p, f, stream);
+    if (stream_it) return launch_product_stream(p, f, stream);
     return launch_product_tile(p, f, stream);
 }
 

@@ -18,7 +18,13 @@ struct Finish {
     int vec_out, vec_add, vec_pre;
 };
 
-// Both kernels want operands that the copy engine can take: bases and pitches on 16-byte boundaries.
+// Whether the copy engine can take an operand of e-byte elements: base and pitch on 16-byte boundaries.  The
+// tile kernel wants them all so; the stream kernel reads others itself.
+inline bool taken_as_is(const Operand &o, int e) { return !o.p || (aligned(o.p, 16) && (o.ld * e) % 16 == 0); }
+
+// The kernels' times in microseconds, as far as choosing between them needs; < 0: cannot be had.
+double stream_estimate(const Product &p);
+double tile_estimate(const Product &p);
 int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream);     // product_tile.cu
 int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream);   // product_stream.cu
 

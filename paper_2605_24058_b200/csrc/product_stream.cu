@@ -9,8 +9,12 @@
 // partial sums through distributed shared memory and add them in rank order (the result does not depend
 // on timing), each the share of outputs that it then finishes and writes.
 //
-//   warp 0 copies, warp 1 MMAs (one thread), warps 2-5 move the sums from TMEM to shared memory; then all
-//   warps add, finish and write.
+//   warps 0-3 move the sums from TMEM to shared memory, warp 4 issues MMAs and warp 5 copies (one thread
+//   each); then all warps add, finish and write.
+//
+// Operands whose base or pitch is not a multiple of 16 bytes are out of the copy engine's reach.  Copying
+// them first would move each weight three times; instead (LOOSE) warps 0-3 and 6-9 fetch the aligned pieces
+// that hold a stage into a second ring, several stages ahead (cp.async), and shift them into place.
 #include <cstring>
 #include <mutex>
 
@@ -23,25 +27,106 @@ using namespace sm100;
 
 constexpr int kRows = 128;                    // weight rows a tile
 constexpr int kWeightBytes = kRows * 128;     // of one stage and weight matrix
-constexpr int kStreamThreads = 6 * 32;
+__host__ __device__ constexpr int threads_of(bool loose) { return loose ? 10 * 32 : 6 * 32; }
 constexpr int kMaxStages = 12;
 constexpr int kMaxSplit = 8;
 constexpr int kBarBytes = (2 * kMaxStages + 1) * 8 + 16;
+constexpr int kHalf = 113 * 1024, kWhole = 227 * 1024;      // shared memory of a CTA where two, or one, share an SM
+
+struct Rows {              // a row-major matrix in bytes
+    const uint8_t *p;
+    int64_t ld, rows, cols;
+};
 
 struct StreamArgs {
     CUtensorMap w[2], t[2];
+    Rows rw[2], rt[2];       // the same operands as they lie in memory
     Finish f;
     int k_blocks, parts;     // stages per operand pair; operand pairs summed into one accumulator
     int tokens;              // MMA columns: tokens of a tile, a multiple of 16
     int stages, split;
+    int raw_stages;          // LOOSE: stages fetched ahead (2 ... 6)
     int tmem_columns;
     int skip;                // -1; the test-hooks build can name a stage whose copies are left out
     int *status;
     uint32_t idesc;
 };
 
-template <bool INT8, bool GATED, bool W_MN>
-__global__ void __launch_bounds__(kStreamThreads, 2)
+// ---- LOOSE: rows of BOXES x 128 bytes from row y and byte x of a matrix on -----------------------------------
+// A warp fetches and shifts the same rows, so the two steps need no barrier between warps.  What lies past the
+// matrix's end in either direction is fetched as zeros, or masked where it shares a piece with valid bytes.
+constexpr int kLoaders = 8;                                                 // warps
+template <int BOXES> constexpr int kRawPitch = BOXES * 128 + 16;             // one more piece than the row's share
+
+// A lane's share of a matrix: up to four rows, kStep apart.  Their distance is a multiple of 16 rows, so they
+// all lie alike against the 16-byte grid.
+template <int BOXES>
+struct Share {
+    static constexpr int kAcross = 8 * BOXES, kPer = 32 / kAcross, kStep = kLoaders * kPer;
+    uintptr_t at;          // first row's byte x0, rounded down, plus the lane's piece
+    int64_t stride;        // to the next row
+    int64_t left;          // bytes from `at` to the end of the row
+    uint32_t raw, dst;     // offsets of the first row's piece in a raw and in an ordinary stage
+    uint32_t by;
+    int first, rows;       // first row in the tile; rows the tile has of the matrix, counted from it
+    bool edge;             // the lane also fetches the piece after its own
+
+    // the part of `tile_rows` rows from row y and byte x on
+    __device__ __forceinline__ Share(int loader, int lane, const Rows &m, int64_t x, int64_t y, int tile_rows)
+    {
+        const int piece = lane % kAcross;
+        first = loader * kPer + lane / kAcross;
+        const uintptr_t row = reinterpret_cast<uintptr_t>(m.p) + (y + first) * m.ld;
+        by = (uint32_t)(row + x) & 15u;
+        at = row + x - by + 16 * piece;
+        left = (int64_t)(row + m.cols - at);
+        stride = m.ld * kStep;
+        raw = first * kRawPitch<BOXES> + 16 * piece;
+        dst = (piece / 8) * tile_rows * 128 + first * 128 + (((piece % 8) ^ (first & 7)) * 16);     // kStep is a multiple of 8
+        edge = piece == kAcross - 1;
+        const int64_t have = m.rows - y < tile_rows ? m.rows - y : tile_rows;
+        rows = (int)have;
+    }
+    // `dx` bytes on along the row, `dy` rows down (both from the share's place; dy a multiple of 16)
+    __device__ __forceinline__ void fetch(uint32_t stage, int64_t dx, int64_t dy_bytes, int rows_now, int tile_rows) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (first + i * kStep >= tile_rows) break;
+            const bool in = first + i * kStep < rows_now;
+            const uintptr_t from = at + dx + dy_bytes + i * stride;
+            const uint32_t to = stage + raw + i * kStep * kRawPitch<BOXES>;
+            fetch16(to, from, in && dx < left);
+            if (edge) fetch16(to + 16, from + 16, in && dx + 16 < left);
+        }
+    }
+    __device__ __forceinline__ void shift(uint32_t stage, uint32_t to, int64_t dx, int tile_rows) const
+    {
+        const int64_t valid64 = left - by - dx;                    // valid bytes of the joined piece
+        const int valid = valid64 >= 16 ? 16 : valid64 > 0 ? (int)valid64 : 0;
+        uint32_t keep[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) keep[j] = valid >= 4 * j + 4 ? 0xffffffffu : valid <= 4 * j ? 0u : (1u << 8 * (valid - 4 * j)) - 1u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (first + i * kStep >= tile_rows) break;
+            const uint32_t from = stage + raw + i * kStep * kRawPitch<BOXES>;
+            const uint4 v = join_pieces(load_shared_v4(from), load_shared_v4(from + 16), by);
+            store_shared_v4(to + dst + i * kStep * 128, make_uint4(v.x & keep[0], v.y & keep[1], v.z & keep[2], v.w & keep[3]));
+        }
+    }
+};
+
+template <bool INT8>
+__device__ __forceinline__ uint4 add4(uint4 a, uint4 b)
+{
+    if (INT8) return make_uint4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+    return make_uint4(__float_as_uint(__uint_as_float(a.x) + __uint_as_float(b.x)), __float_as_uint(__uint_as_float(a.y) + __uint_as_float(b.y)),
+                      __float_as_uint(__uint_as_float(a.z) + __uint_as_float(b.z)), __float_as_uint(__uint_as_float(a.w) + __uint_as_float(b.w)));
+}
+
+template <bool INT8, bool GATED, bool W_MN, bool LOOSE>
+__global__ void __launch_bounds__(threads_of(LOOSE), LOOSE ? 1 : 2)
 product_stream_kernel(const __grid_constant__ StreamArgs P)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -67,15 +152,15 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < P.stages; ++s) {
-            bar_init(full(s), 1);
+            bar_init(full(s), LOOSE ? 32 * kLoaders : 1);
             bar_init(empty(s), 1);
         }
         bar_init(sum_full, 1);
         *abort_flag = 0;
         bar_init_fence();
     }
-    if (warp == 1) tmem_alloc<1>(smem_addr(misc), P.tmem_columns);
-    if (warp == 2 && lane == 0) {
+    if (warp == 4) tmem_alloc<1>(smem_addr(misc), P.tmem_columns);
+    if (!LOOSE && warp == 5 && lane == 0) {
         prefetch_map(&P.w[0]);
         prefetch_map(&P.t[0]);
         if (GATED) prefetch_map(&P.w[1]);
@@ -87,8 +172,8 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
     grid_wait();
     grid_release();
 
-    if (warp == 0) {
-        if (lane == 0) {
+    if (warp == 5) {
+        if (!LOOSE && lane == 0) {
             Ring r;
             for (int kb = first; kb < last; ++kb) {
                 if (!bound.wait(empty(r.stage), r.phase ^ 1u, kDevTmaWaitTimeout)) break;
@@ -112,7 +197,7 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                 r.next(P.stages);
             }
         }
-    } else if (warp == 1) {
+    } else if (warp == 4) {
         if (lane == 0) {
             Ring r;
             bool alive = true;
@@ -135,9 +220,70 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
             if (alive) mma_commit<1>(sum_full);
         }
     } else {
+        if (LOOSE) {
+            const int loader = warp < 4 ? warp : warp - 2;
+            const uint32_t raw0 = base + P.stages * stage_bytes;
+            const int raw_weight = W_MN ? 64 * kRawPitch<2> : kRows * kRawPitch<1>;
+            const int raw_bytes = kSums * raw_weight + P.tokens * kRawPitch<1>;
+            constexpr int kBoxes = W_MN ? 2 : 1, kBoxRows = W_MN ? 64 : kRows;
+            // of a sum of two products the second has operands of its own
+            const Share<kBoxes> w0(loader, lane, P.rw[0], W_MN ? 2 * (int64_t)n0 : 0, W_MN ? 0 : n0, kBoxRows);
+            const Share<kBoxes> w1(loader, lane, P.rw[GATED || P.parts > 1 ? 1 : 0], W_MN ? 2 * (int64_t)n0 : 0, W_MN ? 0 : n0, kBoxRows);
+            const Share<1> tok0(loader, lane, P.rt[0], 0, t0, P.tokens);
+            const Share<1> tok1(loader, lane, P.rt[W_MN && P.parts > 1 ? 1 : 0], 0, t0, P.tokens);
+            const int64_t contraction = W_MN ? P.rw[0].rows : 0, ld = P.rw[0].ld;
+            auto fetch = [&](int kb, int slot) {
+                const uint32_t raw = raw0 + slot * raw_bytes;
+                if (kb < last) {
+                    const bool second = W_MN && kb >= P.k_blocks;
+                    const int64_t at = kb - (second ? P.k_blocks : 0);
+                    if (W_MN) {
+                        const int64_t have = contraction - kBlockK * at;
+                        const int rows_now = (int)(have < kBoxRows ? have : kBoxRows);
+                        if (second) w1.fetch(raw, 0, kBlockK * at * ld, rows_now, kBoxRows);
+                        else w0.fetch(raw, 0, kBlockK * at * ld, rows_now, kBoxRows);
+                    } else {
+                        w0.fetch(raw, 128 * at, 0, w0.rows, kBoxRows);
+                        if (GATED) w1.fetch(raw + raw_weight, 128 * at, 0, w1.rows, kBoxRows);
+                    }
+                    if (second) tok1.fetch(raw + kSums * raw_weight, 128 * at, 0, tok1.rows, P.tokens);
+                    else tok0.fetch(raw + kSums * raw_weight, 128 * at, 0, tok0.rows, P.tokens);
+                }
+                fetch_commit();        // also where there is nothing left: the groups are counted
+            };
+            for (int i = 0; i < P.raw_stages; ++i) fetch(first + i, i);
+            Ring r;
+            int slot = 0;
+            for (int kb = first; kb < last; ++kb) {
+                fetch_wait(P.raw_stages - 1);
+                __syncwarp();
+                const bool go = __all_sync(0xffffffffu, bound.wait(empty(r.stage), r.phase ^ 1u, kDevTmaWaitTimeout));
+                if (!go) break;
+                const uint32_t sw = base + r.stage * stage_bytes, raw = raw0 + slot * raw_bytes;
+                const bool second = W_MN && kb >= P.k_blocks;
+                const int64_t at = kb - (second ? P.k_blocks : 0);
+                if (W_MN) {
+                    if (second) w1.shift(raw, sw, 0, kBoxRows);
+                    else w0.shift(raw, sw, 0, kBoxRows);
+                } else {
+                    w0.shift(raw, sw, 128 * at, kBoxRows);
+                    if (GATED) w1.shift(raw + raw_weight, sw + kWeightBytes, 128 * at, kBoxRows);
+                }
+                if (second) tok1.shift(raw + kSums * raw_weight, sw + kSums * kWeightBytes, 128 * at, P.tokens);
+                else tok0.shift(raw + kSums * raw_weight, sw + kSums * kWeightBytes, 128 * at, P.tokens);
+                fence_proxy_async();
+                if (kb - first != P.skip) bar_arrive(full(r.stage));
+                __syncwarp();
+                fetch(kb + P.raw_stages, slot);
+                slot = slot + 1 == P.raw_stages ? 0 : slot + 1;
+                r.next(P.stages);
+            }
+            fetch_wait(0);
+            __syncwarp();
+        }
         // the partial sums go where the ring was: [sum][token][128 weight rows]
-        const int quadrant = warp % 4;
-        const bool alive = __all_sync(0xffffffffu, bound.wait(sum_full, 0, kDevEpilogueWaitTimeout));
+        const int quadrant = warp;
+        const bool alive = warp < 4 && __all_sync(0xffffffffu, bound.wait(sum_full, 0, kDevEpilogueWaitTimeout));
         if (alive) {
             fence_after();
             const uint32_t d = tmem + ((uint32_t)(32 * quadrant) << 16);
@@ -161,39 +307,44 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
     }
     __syncwarp();
     cluster_sync();
-    if (warp == 1) {
+    if (warp == 4) {
         fence_after();
         tmem_free<1>(tmem, P.tmem_columns);
     }
 
-    // four weight rows of one token an item, the items dealt to the cluster's threads
+    // four weight rows of one token an item, the items dealt to the cluster's threads, kBatch of a thread's at
+    // a time: their sums are all on the way before the first is finished
     if (*abort_flag == 0) {
+        constexpr int kBatch = GATED ? 2 : 4;
         const int64_t have = P.f.M - t0;
-        const int items = (int)(have < P.tokens ? have : P.tokens) * (kRows / 4);
-        for (int it = rank * kStreamThreads + threadIdx.x; it < items; it += P.split * kStreamThreads) {
-            const int t = it / (kRows / 4), j = 4 * (it % (kRows / 4));
-            if (n0 + j >= P.f.N) continue;
-            uint32_t acc[2][4];
+        const int items = (int)(have < P.tokens ? have : P.tokens) * (kRows / 4), step = P.split * threads_of(LOOSE);
+        const int j = 4 * (threadIdx.x % (kRows / 4));             // a thread's items share their weight rows
+        if (n0 + j < P.f.N)
+            for (int it = rank * threads_of(LOOSE) + threadIdx.x; it < items; it += kBatch * step) {
+                uint4 acc[kBatch][2];
 #pragma unroll
-            for (int c = 0; c < kSums; ++c) {
-                const uint32_t at = base + 4u * ((c * P.tokens + t) * kRows + j);
-                uint4 v[kMaxSplit];
+                for (int r = 0; r < kMaxSplit; ++r) {
+                    if (r >= P.split) break;
+                    const uint32_t from = peer_addr(base, r) + 4u * j;
 #pragma unroll
-                for (int r = 0; r < kMaxSplit; ++r)
-                    if (r < P.split) v[r] = load_peer_v4(peer_addr(at, r));
-                uint32_t *a = acc[c];
-                a[0] = v[0].x; a[1] = v[0].y; a[2] = v[0].z; a[3] = v[0].w;
+                    for (int k = 0; k < kBatch; ++k) {
+                        const int i = it + k * step < items ? it + k * step : it;
 #pragma unroll
-                for (int r = 1; r < kMaxSplit; ++r)
-                    if (r < P.split) {
-                        const uint32_t w[4] = {v[r].x, v[r].y, v[r].z, v[r].w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            a[i] = INT8 ? a[i] + w[i] : __float_as_uint(__uint_as_float(a[i]) + __uint_as_float(w[i]));
+                        for (int c = 0; c < kSums; ++c) {
+                            const uint4 v = load_peer_v4(from + 4u * ((c * P.tokens + i / (kRows / 4)) * kRows));
+                            acc[k][c] = r == 0 ? v : add4<INT8>(acc[k][c], v);
+                        }
                     }
+                }
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    if (it + k * step >= items) break;
+                    const uint32_t g[4] = {acc[k][0].x, acc[k][0].y, acc[k][0].z, acc[k][0].w};
+                    const uint4 w = acc[k][GATED ? 1 : 0];
+                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                    finish_row<INT8, GATED, 4>(P.f, 0, t0 + (it + k * step) / (kRows / 4), n0 + j, g, u);
+                }
             }
-            finish_row<INT8, GATED, 4>(P.f, 0, t0 + t, n0 + j, acc[0], acc[GATED ? 1 : 0]);
-        }
     }
     if (P.split > 1) {
         __syncwarp();
@@ -201,84 +352,158 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
     }
 }
 
-template <bool INT8, bool GATED, bool W_MN>
-int launch_stream(const StreamArgs &args, dim3 grid, int smem, cudaStream_t stream)
+const void *kernel_of(bool int8, bool gated, bool loose)
 {
-    const void *func = reinterpret_cast<const void *>(&product_stream_kernel<INT8, GATED, W_MN>);
+    if (int8)
+        return gated ? (loose ? (const void *)&product_stream_kernel<true, true, false, true>
+                              : (const void *)&product_stream_kernel<true, true, false, false>)
+                     : (loose ? (const void *)&product_stream_kernel<true, false, false, true>
+                              : (const void *)&product_stream_kernel<true, false, false, false>);
+    return gated ? (loose ? (const void *)&product_stream_kernel<false, true, false, true>
+                          : (const void *)&product_stream_kernel<false, true, false, false>)
+                 : (loose ? (const void *)&product_stream_kernel<false, false, true, true>
+                          : (const void *)&product_stream_kernel<false, false, true, false>);
+}
+
+// Clusters of `split` CTAs, one CTA an SM, that fit the device at once (0: the query failed).  For a kernel
+// that allocates TMEM the query never counts more than one CTA an SM, whatever its size; two of this kernel's
+// were seen to run side by side where its shared memory allows it, so the caller multiplies.  The query is
+// slow: asked once for each device, kernel and cluster size.
+int resident_clusters(bool int8, bool gated, bool loose, int split)
+{
     static std::mutex mu;
-    static bool ready[64] = {false};
+    static int known[64][8][kMaxSplit + 1];
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return LORDBA_ECUDA;
-    {
-        std::lock_guard<std::mutex> lock(mu);
-        if (!ready[dev]) {
-            if (cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess) {
-                cudaGetLastError();
-                return LORDBA_ECUDA;
-            }
-            ready[dev] = true;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    std::lock_guard<std::mutex> lock(mu);
+    int &n = known[dev][4 * int8 + 2 * gated + loose][split];
+    if (n == 0) {
+        const void *func = kernel_of(int8, gated, loose);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)split, 1, 1);
+        cfg.blockDim = dim3(threads_of(loose), 1, 1);
+        cfg.dynamicSmemBytes = kWhole;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)split; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, kWhole) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, func, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            n = 0;
         }
     }
-    LaunchRec rec;
-    std::memset(&rec, 0, sizeof(rec));
-    rec.func = func;
-    rec.grid[0] = grid.x; rec.grid[1] = grid.y; rec.grid[2] = grid.z;
-    rec.block = kStreamThreads;
-    rec.smem = (uint32_t)smem;
-    rec.cluster = grid.x;
-    rec.pdl = 1;
-    rec.n_args = 1;
-    rec.arg_bytes[0] = sizeof(StreamArgs);
-    return launch_record(rec, &args, nullptr, stream);
+    return n;
+}
+
+struct StreamPlan {
+    bool loose;
+    int tokens, k_blocks, parts, stages, raw_stages, split, smem;
+    int64_t row_tiles, token_tiles;
+    double us;             // estimate
+};
+
+StreamPlan plan_stream(const Product &p)
+{
+    const bool int8 = p.kind == kProductInt8, gated = p.form == Product::kGated, w_mn = p.b[0].mn_major;
+    const int e = int8 ? 1 : 2, block_k = int8 ? 128 : 64, sums = gated ? 2 : 1;
+    StreamPlan s = {};
+    s.k_blocks = (int)((p.K + block_k - 1) / block_k);
+    s.parts = p.form == Product::kSum ? 2 : 1;
+    s.tokens = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    s.loose = !(taken_as_is(p.a[0], e) && taken_as_is(p.a[1], e) && taken_as_is(p.b[0], e) && taken_as_is(p.b[1], e));
+    s.row_tiles = (p.N + kRows - 1) / kRows;
+    s.token_tiles = (p.M + s.tokens - 1) / s.tokens;
+    const int stage = sums * kWeightBytes + s.tokens * 128, exchange = sums * s.tokens * kRows * 4;
+    const int fixed = kBarBytes + 1024, half = kHalf - fixed, whole = kWhole - fixed;
+    // two CTAs an SM where three stages and the exchange fit half of its shared memory, else one
+    const int per_sm = !s.loose && 3 * stage <= half && exchange <= half ? 2 : 1;
+    int used;
+    if (s.loose) {
+        const int raw = sums * (w_mn ? 64 * kRawPitch<2> : kRows * kRawPitch<1>) + s.tokens * kRawPitch<1>;
+        s.stages = 3 * stage + 3 * raw <= whole ? 3 : 2;
+        s.raw_stages = (whole - s.stages * stage) / raw < 6 ? (whole - s.stages * stage) / raw : 6;
+        used = s.stages * stage + s.raw_stages * raw;
+    } else {
+        const int room = per_sm == 2 ? half : whole;
+        s.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
+        used = s.stages * stage;
+    }
+    s.smem = fixed + (used > exchange ? used : exchange);
+    // The split with the least rounds of clusters x stages that a CTA walks; six stages' worth of time go to a
+    // CTA's start, the exchange and the epilogue.
+    const int64_t work = s.row_tiles * s.token_tiles;
+    const int blocks = s.k_blocks * s.parts;
+    int64_t best = 0;
+    for (int n = 1; n <= kMaxSplit && n <= blocks; ++n) {
+        const int fit = per_sm * resident_clusters(int8, gated, s.loose, n);
+        if (fit < 1) continue;
+        const int64_t cost = (work + fit - 1) / fit * ((blocks + n - 1) / n + 6);
+        if (s.split == 0 || cost < best) {
+            s.split = n;
+            best = cost;
+            // a stage takes a CTA the time of its bytes at what an SM draws from L2 (110 KB/us two CTAs, 80 one; shifted
+            // stages 25), and all of them together no less than the weights at HBM's rate
+            const double stage_us = per_sm * stage / (s.loose ? 25e3 : per_sm == 2 ? 110e3 : 80e3);
+            const double walk = (double)((work + fit - 1) / fit) * ((double)((blocks + n - 1) / n) * stage_us + 1.5);
+            const double hbm = (double)p.N * (double)p.K * e * sums * s.parts / 6.0e6;
+            s.us = 3.5 + (walk > hbm ? walk : hbm);
+        }
+    }
+    return s;
 }
 
 }  // namespace
 
+double stream_estimate(const Product &p)
+{
+    const StreamPlan s = plan_stream(p);
+    return s.split > 0 && s.row_tiles <= 65535 && s.token_tiles <= 65535 ? s.us : -1.0;
+}
+
 int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream)
 {
     const bool int8 = p.kind == kProductInt8, gated = p.form == Product::kGated, w_mn = p.b[0].mn_major;
-    const int e = int8 ? 1 : 2, block_k = int8 ? 128 : 64, sums = gated ? 2 : 1;
+    const int e = int8 ? 1 : 2;
+    const StreamPlan plan = plan_stream(p);
+    if (plan.split == 0) return LORDBA_ECUDA;
+    if (plan.row_tiles > 65535 || plan.token_tiles > 65535) return LORDBA_EUNSUPPORTED;
     StreamArgs a;
     std::memset(&a, 0, sizeof(a));
     a.f = f;
-    a.k_blocks = (int)((p.K + block_k - 1) / block_k);
-    a.parts = p.form == Product::kSum ? 2 : 1;
-    a.tokens = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    a.k_blocks = plan.k_blocks;
+    a.parts = plan.parts;
+    a.tokens = plan.tokens;
+    a.stages = plan.stages;
+    a.raw_stages = plan.raw_stages;
+    a.split = plan.split;
     for (int i = 0; i < 2; ++i) {
         const Operand &ot = p.a[i], &ow = p.b[i];
+        const int64_t w_rows = w_mn ? p.K : p.N, w_cols = w_mn ? p.N : p.K;
+        a.rt[i] = Rows{static_cast<const uint8_t *>(ot.p), ot.ld * e, p.M, p.K * e};
+        a.rw[i] = Rows{static_cast<const uint8_t *>(ow.p), ow.ld * e, w_rows, w_cols * e};
+        if (plan.loose) continue;
         if (ot.p && !encode_map(&a.t[i], ot.p, p.M, p.K, ot.ld, e, a.tokens)) return LORDBA_ECUDA;
-        if (ow.p && !(w_mn ? encode_map(&a.w[i], ow.p, p.K, p.N, ow.ld, e, 64) : encode_map(&a.w[i], ow.p, p.N, p.K, ow.ld, e, kRows)))
-            return LORDBA_ECUDA;
-    }
-    const int stage = sums * kWeightBytes + a.tokens * 128, exchange = sums * a.tokens * kRows * 4;
-    const int fixed = kBarBytes + 1024;
-    // two CTAs an SM where three stages and the exchange fit half of its shared memory, else one
-    const int half = 113 * 1024 - fixed, whole = 227 * 1024 - fixed;
-    const int per_sm = 3 * stage <= half && exchange <= half ? 2 : 1;
-    const int room = per_sm == 2 ? half : whole;
-    a.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
-    const int64_t row_tiles = (p.N + kRows - 1) / kRows, token_tiles = (p.M + a.tokens - 1) / a.tokens;
-    if (row_tiles > 65535 || token_tiles > 65535) return LORDBA_EUNSUPPORTED;
-    // The split with the least rounds of CTAs x stages a CTA walks; six stages' worth of time go to a CTA's
-    // start, the exchange and the epilogue.
-    const int64_t slots = (int64_t)sm_count() * per_sm, work = row_tiles * token_tiles;
-    const int blocks = a.k_blocks * a.parts;
-    int64_t best = 0;
-    for (int s = 1; s <= kMaxSplit && s <= blocks; ++s) {
-        const int64_t cost = (work * s + slots - 1) / slots * ((blocks + s - 1) / s + 6);
-        if (a.split == 0 || cost < best) { a.split = s; best = cost; }
+        if (ow.p && !encode_map(&a.w[i], ow.p, w_rows, w_cols, ow.ld, e, w_mn ? 64 : kRows)) return LORDBA_ECUDA;
     }
     a.tmem_columns = 32;
-    while (a.tmem_columns < sums * a.tokens) a.tmem_columns *= 2;
+    while (a.tmem_columns < (gated ? 2 : 1) * a.tokens) a.tmem_columns *= 2;
     a.skip = test_skip_item();
     a.status = device_status_word();
     if (!a.status) return LORDBA_ECUDA;
     a.idesc = instr_desc(int8, p.kind == kProductBf16, w_mn, false, kRows, a.tokens);
-    const int ring = a.stages * stage;
-    const int smem = fixed + (ring > exchange ? ring : exchange);
-    const dim3 grid((unsigned)a.split, (unsigned)row_tiles, (unsigned)token_tiles);
-    if (int8) return gated ? launch_stream<true, true, false>(a, grid, smem, stream) : launch_stream<true, false, false>(a, grid, smem, stream);
-    return gated ? launch_stream<false, true, false>(a, grid, smem, stream) : launch_stream<false, false, true>(a, grid, smem, stream);
+    LaunchRec rec;
+    std::memset(&rec, 0, sizeof(rec));
+    rec.func = kernel_of(int8, gated, plan.loose);
+    rec.grid[0] = (unsigned)plan.split; rec.grid[1] = (unsigned)plan.row_tiles; rec.grid[2] = (unsigned)plan.token_tiles;
+    rec.block = threads_of(plan.loose);
+    rec.smem = (uint32_t)plan.smem;
+    rec.cluster = (uint32_t)plan.split;
+    rec.pdl = 1;
+    rec.n_args = 1;
+    rec.arg_bytes[0] = sizeof(StreamArgs);
+    return launch_record(rec, &a, nullptr, stream);
 }
 
 }  // namespace lordba

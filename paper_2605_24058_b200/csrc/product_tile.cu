@@ -273,6 +273,18 @@ int launch_tile(const TileArgs &args, cudaStream_t stream)
 
 }  // namespace
 
+// 0.285 us a stage (its MMAs at the clock under load), at least 2.7 us a tile (the epilogue), 7 us around them.
+double tile_estimate(const Product &p)
+{
+    const bool gated = p.form == Product::kGated;
+    const int block_k = p.kind == kProductInt8 ? 128 : 64;
+    const double tiles = (double)((p.M + kTileM - 1) / kTileM) * (double)((p.N + (gated ? 127 : 255)) / (gated ? 128 : 256)) *
+                         (p.form == Product::kPair ? 2 : 1);
+    const double rounds = (double)(int64_t)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
+    const double walk = 0.285 * (double)((p.K + block_k - 1) / block_k) * (p.form == Product::kSum ? 2 : 1);
+    return 7.0 + rounds * (walk > 2.7 ? walk : 2.7);
+}
+
 int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
 {
     const bool int8 = p.kind == kProductInt8, gated = p.form == Product::kGated, pair = p.form == Product::kPair;

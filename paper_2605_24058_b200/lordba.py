@@ -160,8 +160,10 @@ def _check(status: int, where: str) -> None:
 
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return int(s.cuda_stream)
+    if stream is not None:
+        return int(stream.cuda_stream)
+    # the handle alone: making a torch.cuda.Stream object takes longer than a small call
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -440,57 +442,82 @@ def fit_scales(target, packed_A, packed_B, s_in, s_r, s_out, r: int, sweeps: int
     _check(rc, "lordba_fit_scales")
 
 
-def _matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
+_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _code(dtype: torch.dtype, what: str) -> int:
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (what, dtype))
+    return code
+
+
+def _pitch(t: torch.Tensor, shape, dtype: torch.dtype, device: int, what: str) -> int:
     """Check a 2-D operand with contiguous rows on the current device; its row pitch in elements."""
-    if t.dtype != dtype:
-        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise ValueError("%s must be on the current CUDA device" % what)
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError("%s must be (%d, %d), got %s" % (what, rows, cols, tuple(t.shape)))
-    ld, inner = t.stride()
-    if inner != 1 and cols > 1:
+    if t.dtype is dtype and t.get_device() == device and t.shape == shape:
+        ld, inner = t.stride()
+        rows, cols = shape
+        if inner == 1 or cols == 1:
+            if rows <= 1:
+                return ld if ld > cols else cols          # a single row has no pitch of its own
+            if ld >= cols:
+                return ld
+            raise ValueError("rows of %s overlap" % what)
         raise ValueError("rows of %s must be contiguous" % what)
-    if rows <= 1:
-        return max(cols, ld)          # a single row has no pitch of its own
-    if ld < cols:
-        raise ValueError("rows of %s overlap" % what)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if t.get_device() != device:
+        raise ValueError("%s must be on the current CUDA device" % what)
+    raise ValueError("%s must be %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+
+
+def _pitch_of_pair(a, b, shape, dtype, device: int, what: str) -> int:
+    """The pitch that both matrices of a pair have."""
+    if a is None or b is None:
+        raise ValueError("%s come together" % what)
+    ld = _pitch(a, shape, dtype, device, what)
+    if _pitch(b, shape, dtype, device, what) != ld and shape[0] > 1:
+        raise ValueError("%s must have one row pitch" % what)
     return ld
 
 
-def _vector(t: torch.Tensor, n: int, what: str) -> None:
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
-        raise TypeError("%s must be %d contiguous float32 values" % (what, n))
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _vector(t: torch.Tensor, n: int, device: int, what: str) -> int:
+    """Check a float32 vector; its address."""
+    if t.dtype is torch.float32 and t.numel() == n and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
+    if t.get_device() != device:
         raise ValueError("%s must be on the current CUDA device" % what)
+    raise TypeError("%s must be %d contiguous float32 values" % (what, n))
 
 
-def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
-    """A new tensor that belongs to the stream the call runs on: its memory is free for that stream's work."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _rows(rows: int, cols: int, dtype: torch.dtype, device, stream) -> torch.Tensor:
-    """A new rows x cols matrix whose rows start on 16-byte boundaries (what the copy engine takes)."""
+def _rows(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """A new matrix whose rows start on 16-byte boundaries (what the copy engine takes).  It belongs to the stream
+    the call runs on: its memory is free for that stream's work."""
     step = 16 // dtype.itemsize
-    pitch = (cols + step - 1) // step * step
-    out = _empty((rows, pitch), dtype, device, stream)
-    return out if pitch == cols else out[:, :cols]
+    pitch = -(-shape[1] // step) * step
+    if stream is None:
+        return torch.empty_strided(shape, (pitch, 1), dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty_strided(shape, (pitch, 1), dtype=dtype, device=device)
 
 
-def _workspace(nbytes: int, given: Optional[torch.Tensor], device, stream) -> Optional[torch.Tensor]:
-    """The workspace of a call: the caller's, or one made here."""
+def _values(n: int, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """A new vector, of the call's stream like _rows."""
+    if stream is None:
+        return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
+
+
+def _workspace(nbytes: int, given: Optional[torch.Tensor], device, stream):
+    """(tensor to keep alive, address, size) of a call's workspace: the caller's, or one made here."""
     if given is not None:
         _need_cuda(given)
-        return given
-    return _empty(nbytes, torch.uint8, device, stream) if nbytes else None
-
-
-def _ws_args(ws: Optional[torch.Tensor]):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+        return given, given.data_ptr(), given.numel() * given.element_size()
+    if nbytes == 0:
+        return None, None, 0
+    ws = _values(nbytes, torch.uint8, device, stream)
+    return ws, ws.data_ptr(), nbytes
 
 
 def int8_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, stream=None):
@@ -500,17 +527,18 @@ def int8_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale:
     below make, to the stream the call runs on."""
     if x.dim() != 2:
         raise ValueError("x must be (T, d)")
-    T, d = x.shape
-    dtype = _dtype_code(x)
-    ldx = _matrix(x, T, d, x.dtype, "x")
+    shape, dev = x.shape, torch.cuda.current_device()
+    T, d = shape
+    dtype = _code(x.dtype, "x")
+    ldx = _pitch(x, shape, x.dtype, dev, "x")
     if q is None:
-        q = _rows(T, d, torch.int8, x.device, stream)
+        q = _rows(shape, torch.int8, x.device, stream)
     if scale is None:
-        scale = _empty(T, torch.float32, x.device, stream)
-    ldq = _matrix(q, T, d, torch.int8, "q")
-    _vector(scale, T, "scale")
-    _check(load().lordba_int8_quantize_rows(x.data_ptr(), ldx, q.data_ptr(), ldq, scale.data_ptr(), T, d, dtype,
-                                            _stream(stream)), "lordba_int8_quantize_rows")
+        scale = _values(T, torch.float32, x.device, stream)
+    ldq = _pitch(q, shape, torch.int8, dev, "q")
+    rc = load().lordba_int8_quantize_rows(x.data_ptr(), ldx, q.data_ptr(), ldq, _vector(scale, T, dev, "scale"), T, d, dtype,
+                                          _stream(stream))
+    _check(rc, "lordba_int8_quantize_rows")
     return q, scale
 
 
@@ -522,35 +550,18 @@ def int8_linear(x, s_x, w, s_w, y: Optional[torch.Tensor] = None, dtype: torch.d
     if absent; only operands off 16-byte boundaries need one."""
     if x.dim() != 2 or w.dim() != 2:
         raise ValueError("x must be (T, d_in) and w (d_out, d_in)")
+    dev = torch.cuda.current_device()
     T, d_in = x.shape
     d_out = w.shape[0]
     if y is None:
-        y = _rows(T, d_out, dtype, x.device, stream)
-    code = _dtype_code(y)
-    _vector(s_x, T, "s_x")
-    _vector(s_w, d_out, "s_w")
-    p = Int8Proj(x.data_ptr(), s_x.data_ptr(), w.data_ptr(), s_w.data_ptr(), y.data_ptr(), d_in, d_out,
-                 _matrix(x, T, d_in, torch.int8, "x"), _matrix(w, d_out, d_in, torch.int8, "w"),
-                 _matrix(y, T, d_out, y.dtype, "y"))
-    lib = load()
-    ref = ctypes.byref(p)
-    ws = _workspace(lib.lordba_int8_linear_workspace_bytes(ref, T), workspace, x.device, stream)
-    _check(lib.lordba_int8_linear(ref, T, code, *_ws_args(ws), _stream(stream)), "lordba_int8_linear")
+        y = _rows((T, d_out), dtype, x.device, stream)
+    p = Int8Proj(x.data_ptr(), _vector(s_x, T, dev, "s_x"), w.data_ptr(), _vector(s_w, d_out, dev, "s_w"), y.data_ptr(), d_in, d_out,
+                 _pitch(x, x.shape, torch.int8, dev, "x"), _pitch(w, (d_out, d_in), torch.int8, dev, "w"),
+                 _pitch(y, (T, d_out), y.dtype, dev, "y"))
+    lib, ref = load(), ctypes.byref(p)
+    keep, ws, nbytes = _workspace(lib.lordba_int8_linear_workspace_bytes(ref, T), workspace, x.device, stream)
+    _check(lib.lordba_int8_linear(ref, T, _code(y.dtype, "y"), ws, nbytes, _stream(stream)), "lordba_int8_linear")
     return y
-
-
-def _pair(a, b, what: str):
-    if (a is None) != (b is None):
-        raise ValueError("%s come together" % what)
-    return a is not None
-
-
-def _pair_ld(a, b, rows: int, cols: int, dtype, what: str) -> int:
-    """The pitch that both matrices of a pair have."""
-    ld, ld_b = _matrix(a, rows, cols, dtype, what), _matrix(b, rows, cols, dtype, what)
-    if ld != ld_b:
-        raise ValueError("%s must have one row pitch" % what)
-    return ld
 
 
 def gated_forward(x, w_gate, w_up, h: Optional[torch.Tensor] = None, act: int = ACT_SILU, scales=None,
@@ -564,42 +575,42 @@ def gated_forward(x, w_gate, w_up, h: Optional[torch.Tensor] = None, act: int = 
     up come back as None."""
     if x.dim() != 2 or w_gate.dim() != 2:
         raise ValueError("x must be (T, d_in), w_gate and w_up (d_hidden, d_in)")
+    dev, kind = torch.cuda.current_device(), x.dtype
     T, d_in = x.shape
     d_hidden = w_gate.shape[0]
-    int8 = x.dtype == torch.int8
-    if int8 != (scales is not None):
+    shape = (T, d_hidden)
+    s_x = s_gate = s_up = None
+    flags = 0
+    if (kind is torch.int8) != (scales is not None):
         raise ValueError("int8 operands come with scales = (s_x, s_gate, s_up), others without")
-    if h is not None:
-        dtype = h.dtype
-    elif dtype is None or not int8:
-        dtype = torch.bfloat16 if int8 else x.dtype
-    p = Gated()
-    p.ldx = _matrix(x, T, d_in, x.dtype, "x")
-    p.ldw = _pair_ld(w_gate, w_up, d_hidden, d_in, x.dtype, "w_gate and w_up")
+    if scales is None:
+        dtype = kind
+    else:
+        dtype = h.dtype if h is not None else dtype or torch.bfloat16
+        s_x, s_gate, s_up = (_vector(scales[0], T, dev, "s_x"), _vector(scales[1], d_hidden, dev, "s_gate"),
+                             _vector(scales[2], d_hidden, dev, "s_up"))
+        flags = GATED_INT8
+    code = _code(dtype, "h")
+    ldx = _pitch(x, x.shape, kind, dev, "x")
+    ldw = _pitch_of_pair(w_gate, w_up, (d_hidden, d_in), kind, dev, "w_gate and w_up")
     if h is None:
-        h = _rows(T, d_hidden, dtype, x.device, stream)
-    code = _dtype_code(h)
-    p.ldh = _matrix(h, T, d_hidden, dtype if int8 else x.dtype, "h")
-    if int8:
-        s_x, s_gate, s_up = scales
-        _vector(s_x, T, "s_x")
-        _vector(s_gate, d_hidden, "s_gate")
-        _vector(s_up, d_hidden, "s_up")
-        p.s_x, p.s_gate, p.s_up, p.flags = s_x.data_ptr(), s_gate.data_ptr(), s_up.data_ptr(), GATED_INT8
-    if _pair(gate_add, up_add, "gate_add and up_add"):
-        p.ld_add = _pair_ld(gate_add, up_add, T, d_hidden, dtype, "gate_add and up_add")
-        p.gate_add, p.up_add = gate_add.data_ptr(), up_add.data_ptr()
-    if not _pair(gate, up, "gate and up") and save:
-        gate, up = (_rows(T, d_hidden, dtype, x.device, stream) for _ in range(2))
-    if gate is not None:
-        p.ld_pre = _pair_ld(gate, up, T, d_hidden, dtype, "gate and up")
-        p.gate, p.up = gate.data_ptr(), up.data_ptr()
-    p.x, p.w_gate, p.w_up, p.h = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr()
-    p.d_in, p.d_hidden, p.act = d_in, d_hidden, act
-    lib = load()
-    ref = ctypes.byref(p)
-    ws = _workspace(lib.lordba_gated_workspace_bytes(ref, T), workspace, x.device, stream)
-    _check(lib.lordba_gated_forward(ref, T, code, *_ws_args(ws), _stream(stream)), "lordba_gated_forward")
+        h = _rows(shape, dtype, x.device, stream)
+    ldh = _pitch(h, shape, dtype, dev, "h")
+    ga = ua = gp = up_ = None
+    ld_add = ld_pre = 0
+    if gate_add is not None or up_add is not None:
+        ld_add = _pitch_of_pair(gate_add, up_add, shape, dtype, dev, "gate_add and up_add")
+        ga, ua = gate_add.data_ptr(), up_add.data_ptr()
+    if save and gate is None and up is None:
+        gate, up = _rows(shape, dtype, x.device, stream), _rows(shape, dtype, x.device, stream)
+    if gate is not None or up is not None:
+        ld_pre = _pitch_of_pair(gate, up, shape, dtype, dev, "gate and up")
+        gp, up_ = gate.data_ptr(), up.data_ptr()
+    p = Gated(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), s_x, s_gate, s_up, ga, ua, gp, up_, h.data_ptr(), d_in, d_hidden,
+              ldx, ldw, ld_add, ld_pre, ldh, act, flags)
+    lib, ref = load(), ctypes.byref(p)
+    keep, ws, nbytes = _workspace(lib.lordba_gated_workspace_bytes(ref, T), workspace, x.device, stream)
+    _check(lib.lordba_gated_forward(ref, T, code, ws, nbytes, _stream(stream)), "lordba_gated_forward")
     return h, gate, up
 
 
@@ -611,42 +622,48 @@ def gated_backward(dh, gate, up, x=None, w_gate=None, w_up=None, dgate=None, dup
     given, dw_gate and dw_up when x is given (None: frozen weights); what is not made comes back as None."""
     if dh.dim() != 2:
         raise ValueError("dh must be (T, d_hidden)")
-    T, d_hidden = dh.shape
-    dtype, code = dh.dtype, _dtype_code(dh)
-    p = GatedGrad()
-    p.ld_dh = _matrix(dh, T, d_hidden, dtype, "dh")
-    p.ld_pre = _pair_ld(gate, up, T, d_hidden, dtype, "gate and up")
-    if not _pair(dgate, dup, "dgate and dup"):
-        dgate, dup = (_rows(T, d_hidden, dtype, dh.device, stream) for _ in range(2))
-    p.ld_dpre = _pair_ld(dgate, dup, T, d_hidden, dtype, "dgate and dup")
-    p.dh, p.gate, p.up, p.dgate, p.dup = dh.data_ptr(), gate.data_ptr(), up.data_ptr(), dgate.data_ptr(), dup.data_ptr()
+    dev, dtype, shape, device = torch.cuda.current_device(), dh.dtype, dh.shape, dh.device
+    T, d_hidden = shape
+    code = _code(dtype, "dh")
+    ld_dh = _pitch(dh, shape, dtype, dev, "dh")
+    ld_pre = _pitch_of_pair(gate, up, shape, dtype, dev, "gate and up")
+    if dgate is None and dup is None:
+        dgate, dup = _rows(shape, dtype, device, stream), _rows(shape, dtype, device, stream)
+    ld_dpre = _pitch_of_pair(dgate, dup, shape, dtype, dev, "dgate and dup")
     d_in = 1
-    if _pair(w_gate, w_up, "w_gate and w_up"):
+    ldx = ldw = ld_dx = ld_dw = 0
+    px = pwg = pwu = pdx = pdwg = pdwu = None
+    if w_gate is not None or w_up is not None:
+        if w_gate is None or w_up is None or w_gate.dim() != 2:
+            raise ValueError("w_gate and w_up come together, as (d_hidden, d_in)")
         d_in = w_gate.shape[1]
-        p.ldw = _pair_ld(w_gate, w_up, d_hidden, d_in, dtype, "w_gate and w_up")
+        ldw = _pitch_of_pair(w_gate, w_up, (d_hidden, d_in), dtype, dev, "w_gate and w_up")
         if dx is None:
-            dx = _rows(T, d_in, dtype, dh.device, stream)
-        p.ld_dx = _matrix(dx, T, d_in, dtype, "dx")
-        p.w_gate, p.w_up, p.dx = w_gate.data_ptr(), w_up.data_ptr(), dx.data_ptr()
+            dx = _rows((T, d_in), dtype, device, stream)
+        ld_dx = _pitch(dx, (T, d_in), dtype, dev, "dx")
+        pwg, pwu, pdx = w_gate.data_ptr(), w_up.data_ptr(), dx.data_ptr()
     elif dx is not None:
         raise ValueError("dx needs w_gate and w_up")
     if x is not None:
-        if w_gate is not None and x.shape[1] != d_in:
+        if x.dim() != 2 or (w_gate is not None and x.shape[1] != d_in):
             raise ValueError("x must be (T, d_in)")
         d_in = x.shape[1]
-        p.ldx = _matrix(x, T, d_in, dtype, "x")
-        if not _pair(dw_gate, dw_up, "dw_gate and dw_up"):
-            dw_gate, dw_up = (_rows(d_hidden, d_in, dtype, dh.device, stream) for _ in range(2))
-        p.ld_dw = _pair_ld(dw_gate, dw_up, d_hidden, d_in, dtype, "dw_gate and dw_up")
-        p.x, p.dw_gate, p.dw_up = x.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr()
+        ldx = _pitch(x, (T, d_in), dtype, dev, "x")
+        if dw_gate is None and dw_up is None:
+            dw_gate, dw_up = _rows((d_hidden, d_in), dtype, device, stream), _rows((d_hidden, d_in), dtype, device, stream)
+        ld_dw = _pitch_of_pair(dw_gate, dw_up, (d_hidden, d_in), dtype, dev, "dw_gate and dw_up")
+        px, pdwg, pdwu = x.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr()
     elif dw_gate is not None or dw_up is not None:
         raise ValueError("dw_gate and dw_up need x")
-    p.d_in, p.d_hidden, p.act = d_in, d_hidden, act
-    lib = load()
-    ref = ctypes.byref(p)
-    ws = _workspace(lib.lordba_gated_backward_workspace_bytes(ref, T), workspace, dh.device, stream)
-    _check(lib.lordba_gated_backward(ref, T, code, *_ws_args(ws), _stream(stream)), "lordba_gated_backward")
+    p = GatedGrad(dh.data_ptr(), gate.data_ptr(), up.data_ptr(), px, pwg, pwu, dgate.data_ptr(), dup.data_ptr(), pdx, pdwg, pdwu,
+                  d_in, d_hidden, ld_dh, ld_pre, ldx, ldw, ld_dpre, ld_dx, ld_dw, act, 0)
+    lib, ref = load(), ctypes.byref(p)
+    keep, ws, nbytes = _workspace(lib.lordba_gated_backward_workspace_bytes(ref, T), workspace, device, stream)
+    _check(lib.lordba_gated_backward(ref, T, code, ws, nbytes, _stream(stream)), "lordba_gated_backward")
     return dgate, dup, dx, dw_gate, dw_up
+
+
+_U64 = (1 << 64) - 1
 
 
 def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out: Optional[torch.Tensor] = None,
@@ -655,16 +672,16 @@ def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out: Optiona
     offset), so the same call on the gradient (without a residual) is the backward pass.  out may be x or residual."""
     if x.dim() != 2:
         raise ValueError("x must be (T, d)")
-    T, d = x.shape
-    ldx = _matrix(x, T, d, x.dtype, "x")
-    code = _dtype_code(x)
+    dev, shape, dtype = torch.cuda.current_device(), x.shape, x.dtype
+    code = _code(dtype, "x")
+    ldx = _pitch(x, shape, dtype, dev, "x")
     if out is None:
-        out = _rows(T, d, x.dtype, x.device, stream)
-    ldo = _matrix(out, T, d, x.dtype, "out")
-    rp, ldr = (None, 0) if residual is None else (residual.data_ptr(), _matrix(residual, T, d, x.dtype, "residual"))
-    mask = (1 << 64) - 1
-    _check(load().lordba_dropout(x.data_ptr(), ldx, rp, ldr, out.data_ptr(), ldo, T, d, p, seed & mask, offset & mask, code,
-                                 _stream(stream)), "lordba_dropout")
+        out = _rows(shape, dtype, x.device, stream)
+    ldo = _pitch(out, shape, dtype, dev, "out")
+    rp, ldr = (None, 0) if residual is None else (residual.data_ptr(), _pitch(residual, shape, dtype, dev, "residual"))
+    rc = load().lordba_dropout(x.data_ptr(), ldx, rp, ldr, out.data_ptr(), ldo, shape[0], shape[1], p, seed & _U64, offset & _U64, code,
+                               _stream(stream))
+    _check(rc, "lordba_dropout")
     return out
 
 
