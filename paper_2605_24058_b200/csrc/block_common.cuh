@@ -94,13 +94,14 @@ __device__ __forceinline__ uint4 join_pieces(uint4 a, uint4 b, uint32_t by)
 }
 
 // The sixteen bytes at any address at < end; bytes from `end` on read as zero, and an aligned piece is read
-// only when it holds a byte before `end`.
+// only when it holds a byte before `end`.  CONST: nothing writes there while the kernel runs.
+template <bool CONST = true>
 __device__ __forceinline__ uint4 load_bytes16(uintptr_t at, uintptr_t end)
 {
     const uintptr_t first = at & ~(uintptr_t)15;
     const uintptr_t second = (at & 15) && first + 16 < end ? first + 16 : first;
-    const uint4 v = join_pieces(__ldg(reinterpret_cast<const uint4 *>(first)), __ldg(reinterpret_cast<const uint4 *>(second)),
-                                (uint32_t)at & 15u);
+    const uint4 *pa = reinterpret_cast<const uint4 *>(first), *pb = reinterpret_cast<const uint4 *>(second);
+    const uint4 v = CONST ? join_pieces(__ldg(pa), __ldg(pb), (uint32_t)at & 15u) : join_pieces(*pa, *pb, (uint32_t)at & 15u);
     uint32_t w[4] = {v.x, v.y, v.z, v.w};
     const int left = end - at < 16 ? (int)(end - at) : 16;
 #pragma unroll

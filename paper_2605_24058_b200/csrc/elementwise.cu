@@ -19,8 +19,8 @@ __device__ __forceinline__ Group8<E> load8(const E *row, int64_t g, int64_t d, b
     if (vec && 8 * g + 8 <= d) return load_group(row + 8 * g);
     const uintptr_t at = reinterpret_cast<uintptr_t>(row + 8 * g), end = reinterpret_cast<uintptr_t>(row + d);
     Group8<E> v;
-    v.w = load_bytes16(at, end);
-    if constexpr (sizeof(E) == 4) v.w2 = at + 16 < end ? load_bytes16(at + 16, end) : make_uint4(0, 0, 0, 0);
+    v.w = load_bytes16<false>(at, end);          // dropout may run in place
+    if constexpr (sizeof(E) == 4) v.w2 = at + 16 < end ? load_bytes16<false>(at + 16, end) : make_uint4(0, 0, 0, 0);
     return v;
 }
 

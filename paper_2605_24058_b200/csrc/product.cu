@@ -119,6 +119,7 @@ int launch_product(const Product &given, void *workspace, cudaStream_t stream)
     f.vec_out = rows_vec(p.out[0], p.ldo, eo) && aligned(p.out[1], 16);
     f.vec_add = rows_vec(p.add[0], p.ld_add, eo) && aligned(p.add[1], 16);
     f.vec_pre = rows_vec(p.pre[0], p.ld_pre, eo) && aligned(p.pre[1], 16);
+    f.vec_scale = aligned(p.s_col[0], 16) && aligned(p.s_col[1], 16);
     if (stream_it) return launch_product_stream(p, f, stream);
     return launch_product_tile(p, f, stream);
 }

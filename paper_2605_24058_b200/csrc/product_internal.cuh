@@ -15,7 +15,7 @@ struct Finish {
     void *pre[2];
     int64_t ld_add, ld_pre, M, N;
     int dtype, act;
-    int vec_out, vec_add, vec_pre;
+    int vec_out, vec_add, vec_pre, vec_scale;
 };
 
 // Whether the copy engine can take an operand of e-byte elements: base and pitch on 16-byte boundaries.  The
@@ -35,114 +35,65 @@ bool encode_map(CUtensorMap *map, const void *p, int64_t rows, int64_t cols, int
 int sm_count();      // of the current device
 
 // ---- epilogue pieces ----------------------------------------------------------------------------------------
-// COUNT consecutive elements of a row, of which the first n exist.
+// COUNT scales, of which the first n exist.
 template <int COUNT>
-__device__ __forceinline__ void load_row(const void *p, int64_t at, int n, int vec, int dtype, float v[COUNT])
+__device__ __forceinline__ void load_scales(const float *p, int n, int vec, float v[COUNT])
 {
-    const uint16_t *q = static_cast<const uint16_t *>(p) + at;
     if (vec && n >= COUNT) {
-        uint32_t w[COUNT / 2];
-        if constexpr (COUNT % 8 == 0) {
 #pragma unroll
-            for (int i = 0; i < COUNT / 2; i += 4) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(q + 2 * i);
-                w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
-            }
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2 *>(q);
-            w[0] = x.x; w[1] = x.y;
-        }
-#pragma unroll
-        for (int i = 0; i < COUNT / 2; ++i) {
-            const float2 f = dtype == LORDBA_BF16 ? unpack2<__nv_bfloat16>(w[i]) : unpack2<__half>(w[i]);
-            v[2 * i] = f.x;
-            v[2 * i + 1] = f.y;
+        for (int i = 0; i < COUNT; i += 4) {
+            const float4 x = __ldg(reinterpret_cast<const float4 *>(p + i));
+            v[i] = x.x; v[i + 1] = x.y; v[i + 2] = x.z; v[i + 3] = x.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i)
-            v[i] = i >= n ? 0.0f
-                   : dtype == LORDBA_BF16 ? to_float(reinterpret_cast<const __nv_bfloat16 *>(q)[i])
-                                          : to_float(reinterpret_cast<const __half *>(q)[i]);
+        for (int i = 0; i < COUNT; ++i) v[i] = __ldg(p + (i < n ? i : 0));
     }
 }
 
-template <int COUNT>
-__device__ __forceinline__ void store_row(void *p, int64_t at, int n, int vec, int dtype, const float v[COUNT])
-{
-    if (dtype == LORDBA_F32) {
-        float *q = static_cast<float *>(p) + at;
-        if (vec && n >= COUNT) {
-#pragma unroll
-            for (int i = 0; i < COUNT; i += 4) *reinterpret_cast<float4 *>(q + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i)
-                if (i < n) q[i] = v[i];
-        }
-        return;
-    }
-    uint16_t *q = static_cast<uint16_t *>(p) + at;
-    uint32_t w[COUNT / 2];
-#pragma unroll
-    for (int i = 0; i < COUNT / 2; ++i)
-        w[i] = dtype == LORDBA_BF16 ? pack2<__nv_bfloat16>(v[2 * i], v[2 * i + 1]) : pack2<__half>(v[2 * i], v[2 * i + 1]);
-    if (vec && n >= COUNT) {
-        if constexpr (COUNT % 8 == 0) {
-#pragma unroll
-            for (int i = 0; i < COUNT / 2; i += 4) *reinterpret_cast<uint4 *>(q + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-        } else {
-            *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i)
-            if (i < n) q[i] = (uint16_t)((i & 1) ? w[i / 2] >> 16 : w[i / 2] & 0xffffu);
-    }
-}
-
-// The epilogue of COUNT columns of one row: acc0 the sums (of the gate), acc1 those of up.
+// The sums of COUNT columns from n on, `left` of which exist, as the products they stand for.
 template <bool INT8, bool GATED, int COUNT>
-__device__ __forceinline__ void finish_row(const Finish &F, int problem, int64_t m, int64_t n, const uint32_t acc0[COUNT],
-                                           const uint32_t acc1[COUNT])
+__device__ __forceinline__ void products_of(const Finish &F, int64_t m, int64_t n, int left, const uint32_t acc0[COUNT],
+                                            const uint32_t acc1[COUNT], float v[COUNT], float w[COUNT])
 {
-    const int left = (int)(F.N - n < COUNT ? F.N - n : COUNT);
-    float v[COUNT], w[COUNT];
-    const float s = INT8 ? __ldg(F.s_row + m) : 0.0f;
+    if (INT8) {
+        const float s = __ldg(F.s_row + m);
+        load_scales<COUNT>(F.s_col[0] + n, left, F.vec_scale, v);
+        if (GATED) load_scales<COUNT>(F.s_col[1] + n, left, F.vec_scale, w);
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        if (INT8) {
-            const int64_t c = n + (i < left ? i : 0);
-            v[i] = (float)(int)acc0[i] * s * __ldg(F.s_col[0] + c);
-            if (GATED) w[i] = (float)(int)acc1[i] * s * __ldg(F.s_col[1] + c);
-        } else {
+        for (int i = 0; i < COUNT; ++i) {
+            v[i] *= (float)(int)acc0[i] * s;
+            if (GATED) w[i] *= (float)(int)acc1[i] * s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
             v[i] = __uint_as_float(acc0[i]);
             if (GATED) w[i] = __uint_as_float(acc1[i]);
         }
     }
-    if (GATED) {
-        if (F.add[0]) {
-            float a[COUNT];
-            load_row<COUNT>(F.add[0], m * F.ld_add + n, left, F.vec_add, F.dtype, a);
+}
+
+// v = act(v) w
+template <int COUNT>
+__device__ __forceinline__ void gate(int act, float v[COUNT], const float w[COUNT])
+{
+    if (act == LORDBA_ACT_SILU) {
 #pragma unroll
-            for (int i = 0; i < COUNT; ++i) v[i] += a[i];
-            load_row<COUNT>(F.add[1], m * F.ld_add + n, left, F.vec_add, F.dtype, a);
+        for (int i = 0; i < COUNT; ++i) v[i] = act_gate<LORDBA_ACT_SILU>(v[i]) * w[i];
+    } else {
 #pragma unroll
-            for (int i = 0; i < COUNT; ++i) w[i] += a[i];
-        }
-        if (F.pre[0]) {
-            store_row<COUNT>(F.pre[0], m * F.ld_pre + n, left, F.vec_pre, F.dtype, v);
-            store_row<COUNT>(F.pre[1], m * F.ld_pre + n, left, F.vec_pre, F.dtype, w);
-        }
-        if (F.act == LORDBA_ACT_SILU) {
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i) v[i] = act_gate<LORDBA_ACT_SILU>(v[i]) * w[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i) v[i] = act_gate<LORDBA_ACT_GELU_TANH>(v[i]) * w[i];
-        }
+        for (int i = 0; i < COUNT; ++i) v[i] = act_gate<LORDBA_ACT_GELU_TANH>(v[i]) * w[i];
     }
-    store_row<COUNT>(F.out[problem], m * F.ldo + n, left, F.vec_out, F.dtype, v);
+}
+
+__device__ __forceinline__ float2 unpack2_any(uint32_t w, int dtype)
+{
+    return dtype == LORDBA_BF16 ? unpack2<__nv_bfloat16>(w) : unpack2<__half>(w);
+}
+__device__ __forceinline__ uint32_t pack2_any(float lo, float hi, int dtype)
+{
+    return dtype == LORDBA_BF16 ? pack2<__nv_bfloat16>(lo, hi) : pack2<__half>(lo, hi);
 }
 
 }  // namespace lordba

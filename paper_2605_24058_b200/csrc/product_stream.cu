@@ -117,6 +117,71 @@ struct Share {
     }
 };
 
+// ---- epilogue: four weight rows (columns of the output) of one token ------------------------------------------
+// Neighbouring lanes hold neighbouring columns, so whatever the alignment a warp's accesses are whole lines.
+__device__ __forceinline__ void load4(const void *p, int64_t at, int n, int vec, int dtype, float v[4])
+{
+    const uint16_t *q = static_cast<const uint16_t *>(p) + at;
+    uint2 w;
+    if (vec && n >= 4) {
+        w = *reinterpret_cast<const uint2 *>(q);
+    } else {
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < n ? q[i] : 0u;
+        w = make_uint2(x[0] | x[1] << 16, x[2] | x[3] << 16);
+    }
+    const float2 lo = unpack2_any(w.x, dtype), hi = unpack2_any(w.y, dtype);
+    v[0] = lo.x; v[1] = lo.y; v[2] = hi.x; v[3] = hi.y;
+}
+
+__device__ __forceinline__ void store4(void *p, int64_t at, int n, int vec, int dtype, const float v[4])
+{
+    if (dtype == LORDBA_F32) {
+        float *q = static_cast<float *>(p) + at;
+        if (vec && n >= 4) {
+            *reinterpret_cast<float4 *>(q) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < n) q[i] = v[i];
+        }
+        return;
+    }
+    uint16_t *q = static_cast<uint16_t *>(p) + at;
+    const uint32_t w[2] = {pack2_any(v[0], v[1], dtype), pack2_any(v[2], v[3], dtype)};
+    if (vec && n >= 4) {
+        *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) q[i] = (uint16_t)(w[i / 2] >> 16 * (i % 2));
+    }
+}
+
+template <bool INT8, bool GATED>
+__device__ __forceinline__ void finish4(const Finish &F, int64_t m, int64_t n, const uint32_t acc0[4], const uint32_t acc1[4])
+{
+    const int left = (int)(F.N - n < 4 ? F.N - n : 4);
+    float v[4], w[4];
+    products_of<INT8, GATED, 4>(F, m, n, left, acc0, acc1, v, w);
+    if (GATED) {
+        if (F.add[0]) {
+            float a[4], b[4];
+            load4(F.add[0], m * F.ld_add + n, left, F.vec_add, F.dtype, a);
+            load4(F.add[1], m * F.ld_add + n, left, F.vec_add, F.dtype, b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] += a[i]; w[i] += b[i]; }
+        }
+        if (F.pre[0]) {
+            store4(F.pre[0], m * F.ld_pre + n, left, F.vec_pre, F.dtype, v);
+            store4(F.pre[1], m * F.ld_pre + n, left, F.vec_pre, F.dtype, w);
+        }
+        gate<4>(F.act, v, w);
+    }
+    store4(F.out[0], m * F.ldo + n, left, F.vec_out, F.dtype, v);
+}
+
 template <bool INT8>
 __device__ __forceinline__ uint4 add4(uint4 a, uint4 b)
 {
@@ -342,7 +407,7 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                     const uint32_t g[4] = {acc[k][0].x, acc[k][0].y, acc[k][0].z, acc[k][0].w};
                     const uint4 w = acc[k][GATED ? 1 : 0];
                     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-                    finish_row<INT8, GATED, 4>(P.f, 0, t0 + (it + k * step) / (kRows / 4), n0 + j, g, u);
+                    finish4<INT8, GATED>(P.f, t0 + (it + k * step) / (kRows / 4), n0 + j, g, u);
                 }
             }
     }

@@ -31,7 +31,9 @@ constexpr int kTileM = 256;
 constexpr int kTileThreads = 12 * 32;
 constexpr int kEpiWarps = 8;
 constexpr int kBarBytes = (2 * kStages + 4) * 8 + 16;
-constexpr int kTileSmem = kStages * kStageBytes + kBarBytes + 1024;
+constexpr int kPatchPitch = 64 + 16;               // a warp's patch: 32 rows of 64 bytes, padded against bank conflicts
+constexpr int kPatchBytes = 32 * kPatchPitch;
+constexpr int kTileSmem = kStages * kStageBytes + kEpiWarps * kPatchBytes + kBarBytes + 1024;
 
 struct TileArgs {
     CUtensorMap a[2], b[2];
@@ -61,6 +63,100 @@ __device__ __forceinline__ Tile tile_at(const TileArgs &P, int i)
     return t;
 }
 
+// ---- epilogue: a warp's 32 rows x 64 bytes of a matrix -----------------------------------------------------------
+// TMEM gives a lane a row; memory wants neighbouring lanes on neighbouring columns (four of them on 64 bytes of a
+// row).  A patch of shared memory turns one into the other; the warp alone uses it.  With each lane reading
+// and writing rows of its own, 609 x 8596 outputs of a gated product with addends took 70 us, 8 us of them bytes.
+struct Patch {
+    uint32_t mine, shared;      // a lane's row; its place among the eight rows of an access
+    int row, piece;
+
+    __device__ __forceinline__ Patch(uint32_t base, int lane)
+        : mine(base + lane * kPatchPitch), shared(base + (lane / 4) * kPatchPitch + 16 * (lane % 4)), row(lane / 4), piece(lane % 4)
+    {
+    }
+    // fetch: the four pieces of 16 bytes that this lane reads of rows m0 ... m0 + 31, columns n ... n + 31 (16-bit)
+    __device__ __forceinline__ void fetch(uint4 x[4], const void *p, int64_t ld, int vec, int64_t m0, int64_t n, const Finish &F) const
+    {
+        const int64_t c = n + 8 * piece;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t m = m0 + row + 8 * i;
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (m < F.M && c < F.N) {
+                const uint16_t *q = static_cast<const uint16_t *>(p) + m * ld;
+                if (vec && c + 8 <= F.N) x[i] = *reinterpret_cast<const uint4 *>(q + c);
+                else x[i] = load_bytes16<false>(reinterpret_cast<uintptr_t>(q + c), reinterpret_cast<uintptr_t>(q + F.N));
+            }
+        }
+    }
+    // add: what the lanes fetched, to the 32 columns of the lane's own row
+    __device__ __forceinline__ void add(const uint4 x[4], float v[32], int dtype) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store_shared_v4(shared + 8 * i * kPatchPitch, x[i]);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 y = load_shared_v4(mine + 16 * i);
+            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = unpack2_any(w[j], dtype);
+                v[8 * i + 2 * j] += f.x;
+                v[8 * i + 2 * j + 1] += f.y;
+            }
+        }
+        __syncwarp();
+    }
+    // put: sixteen words of the lane's own row to memory: `e` bytes an element, from column n on
+    __device__ __forceinline__ void put(const uint32_t w[16], void *p, int64_t ld, int vec, int e, int64_t m0, int64_t n, const Finish &F) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store_shared_v4(mine + 16 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+        __syncwarp();
+        const int count = 16 / e;                            // elements of a piece
+        const int64_t c = n + count * piece;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 x = load_shared_v4(shared + 8 * i * kPatchPitch);
+            const int64_t m = m0 + row + 8 * i;
+            if (m >= F.M || c >= F.N) continue;
+            uint8_t *q = static_cast<uint8_t *>(p) + (m * ld + c) * e;
+            if (vec && c + count <= F.N) {
+                *reinterpret_cast<uint4 *>(q) = x;
+            } else {
+                const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+                const int left = F.N - c < count ? (int)(F.N - c) : count;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (j >= left) break;
+                    if (e == 4) { if (j < 4) reinterpret_cast<uint32_t *>(q)[j] = y[j % 4]; }
+                    else reinterpret_cast<uint16_t *>(q)[j] = (uint16_t)(y[j / 2] >> 16 * (j % 2));
+                }
+            }
+        }
+        __syncwarp();
+    }
+    // the same for 32 values, in their type
+    __device__ __forceinline__ void put32(const float v[32], void *p, int64_t ld, int vec, int dtype, int64_t m0, int64_t n, const Finish &F) const
+    {
+        uint32_t w[16];
+        if (dtype == LORDBA_F32) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * h + i]);
+                put(w, p, ld, vec, 4, m0, n + 16 * h, F);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack2_any(v[2 * i], v[2 * i + 1], dtype);
+            put(w, p, ld, vec, 2, m0, n, F);
+        }
+    }
+};
+
 template <bool INT8, bool GATED, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kTileThreads, 1)
 product_tile_kernel(const __grid_constant__ TileArgs P)
@@ -69,7 +165,7 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
     constexpr int kTileN = GATED ? 128 : 256;        // columns of the output
     constexpr int kBlockK = INT8 ? 128 : 64;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t bars = base + kStages * kStageBytes;
+    const uint32_t patches = base + kStages * kStageBytes, bars = patches + kEpiWarps * kPatchBytes;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (kStages + s); };
     auto sum_full = [&](int b) { return bars + 8u * (2 * kStages + b); };
@@ -183,24 +279,52 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
     } else if (warp >= 4) {
         const int quadrant = warp % 4, half = (warp - 4) / 4;
         constexpr int kCols = kTileN / 2;                      // columns of one warp
+        const Patch patch(patches + (warp - 4) * kPatchBytes, lane);
         int buf = 0;
         uint32_t buf_phase = 0;
         bool alive = true;
         for (int i = pair; i < P.tiles; i += pairs) {
             const Tile t = tile_at(P, i);
-            const int64_t m = (int64_t)t.m * kTileM + 128 * rank + 32 * quadrant + lane;
+            const int64_t m0 = (int64_t)t.m * kTileM + 128 * rank + 32 * quadrant;
             const int64_t n0 = (int64_t)t.n * kTileN + kCols * half;
             alive = __all_sync(0xffffffffu, bound.wait(sum_full(buf), buf_phase, kDevEpilogueWaitTimeout));
             if (!alive) break;
             fence_after();
             const uint32_t d = tmem + ((uint32_t)(32 * quadrant) << 16) + 256u * buf + kCols * half;
 #pragma unroll 1
-            for (int c = 0; c < kCols; c += 16) {
-                uint32_t g[16], u[16];
+            for (int c = 0; c < kCols; c += 32) {
+                const int64_t n = n0 + c;
+                if (m0 >= P.f.M || n >= P.f.N) break;          // the warp's rows or columns lie outside
+                const bool adds = GATED && P.f.add[0];
+                uint4 xg[4], xu[4];
+                if (adds) {
+                    patch.fetch(xg, P.f.add[0], P.f.ld_add, P.f.vec_add, m0, n, P.f);
+                    patch.fetch(xu, P.f.add[1], P.f.ld_add, P.f.vec_add, m0, n, P.f);
+                }
+                uint32_t g[32], u[32];
                 tmem_load16(d + c, g);
-                if (GATED) tmem_load16(d + 128 + c, u);
+                tmem_load16(d + c + 16, g + 16);
+                if (GATED) {
+                    tmem_load16(d + 128 + c, u);
+                    tmem_load16(d + 128 + c + 16, u + 16);
+                }
                 tmem_wait_load();
-                if (m < P.f.M && n0 + c < P.f.N) finish_row<INT8, GATED, 16>(P.f, t.problem, m, n0 + c, g, u);
+                float v[32], w[32];
+                const int64_t m = m0 + lane < P.f.M ? m0 + lane : m0;
+                const int left = (int)(P.f.N - n < 32 ? P.f.N - n : 32);
+                products_of<INT8, GATED, 32>(P.f, m, n, left, g, u, v, w);
+                if (GATED) {
+                    if (adds) {
+                        patch.add(xg, v, P.f.dtype);
+                        patch.add(xu, w, P.f.dtype);
+                    }
+                    if (P.f.pre[0]) {
+                        patch.put32(v, P.f.pre[0], P.f.ld_pre, P.f.vec_pre, P.f.dtype, m0, n, P.f);
+                        patch.put32(w, P.f.pre[1], P.f.ld_pre, P.f.vec_pre, P.f.dtype, m0, n, P.f);
+                    }
+                    gate<32>(P.f.act, v, w);
+                }
+                patch.put32(v, P.f.out[t.problem], P.f.ldo, P.f.vec_out, P.f.dtype, m0, n, P.f);
             }
             fence_before();
             __syncwarp();
