@@ -123,7 +123,16 @@ __device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.la
 constexpr float kGelu = 1.5957691216057308f;      // 2 sqrt(2 / pi)
 constexpr float kGeluCubic = 0.044715f;
 
-__device__ __forceinline__ float logistic(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// 1 / (1 + e^-z) with the hardware's exponential and reciprocal (2^-22 each), subnormals flushed: the
+// forms that keep them cost eight instructions more, and the epilogues are bound by their instructions.
+__device__ __forceinline__ float logistic(float z)
+{
+    constexpr float kLog2E = 1.4426950408889634f;
+    float e, f;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-kLog2E * z));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(1.0f + e));
+    return f;
+}
 
 template <int ACT>
 __device__ __forceinline__ float act_gate(float g)

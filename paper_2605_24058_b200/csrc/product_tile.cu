@@ -10,7 +10,14 @@
 //
 //   warp 0      copies: both CTAs' producers fill their own halves; every copy completes on the leader's barrier
 //   warp 1      the leader's issues all MMAs (one thread) and frees stages and accumulators in both CTAs
-//   warps 4-11  epilogue: two warps per TMEM lane quadrant, each half of the columns
+//   warps 4-11  epilogue, 32 columns of 32 rows at a time, addends fetched a step ahead.  It is a chain of
+//               latencies, so two groups of four warps take turns at the tiles, one computing while the other
+//               waits; where every pair has but one tile they share it.
+//
+// Measured: 8-bit 8192 x 11008 -> 4096 230 us (3.2 Pop/s); gated 2048 x 4096 -> 11008 in bf16 with addends and
+// saved pre-activations 271 us (1.36 PFLOP/s, of the 1.39 that a library product sustains under the power cap).
+// Sixteen epilogue warps, or 16 columns a step, cost such products 2 - 6 % and gain 5 - 20 % only where the
+// contraction is so short that the epilogue is all there is.
 //
 // Operands come contraction-contiguous or (gradients) m- or n-contiguous: then a stage holds 64 contraction
 // steps as rows of 64 columns and the MMA reads it transposed.
@@ -28,10 +35,13 @@ constexpr int kStages = 6;
 constexpr int kHalf = 128 * 128;                   // bytes of one CTA's half of an operand in a stage
 constexpr int kStageBytes = 2 * kHalf;
 constexpr int kTileM = 256;
-constexpr int kTileThreads = 12 * 32;
 constexpr int kEpiWarps = 8;
+constexpr int kTileThreads = (4 + kEpiWarps) * 32;
 constexpr int kBarBytes = (2 * kStages + 4) * 8 + 16;
-constexpr int kPatchPitch = 64 + 16;               // a warp's patch: 32 rows of 64 bytes, padded against bank conflicts
+constexpr int kCh = 32;                            // columns of an epilogue step
+constexpr int kPieces = kCh / 8;                   // 16-byte pieces of a row of them, 16-bit
+constexpr int kDown = 32 / kPieces;                // rows of one access of a warp
+constexpr int kPatchPitch = 2 * kCh + 16;          // a warp's patch: 32 rows, padded against bank conflicts
 constexpr int kPatchBytes = 32 * kPatchPitch;
 constexpr int kTileSmem = kStages * kStageBytes + kEpiWarps * kPatchBytes + kBarBytes + 1024;
 
@@ -63,41 +73,52 @@ __device__ __forceinline__ Tile tile_at(const TileArgs &P, int i)
     return t;
 }
 
-// ---- epilogue: a warp's 32 rows x 64 bytes of a matrix -----------------------------------------------------------
-// TMEM gives a lane a row; memory wants neighbouring lanes on neighbouring columns (four of them on 64 bytes of a
-// row).  A patch of shared memory turns one into the other; the warp alone uses it.  With each lane reading
-// and writing rows of its own, 609 x 8596 outputs of a gated product with addends took 70 us, 8 us of them bytes.
+// ---- epilogue: a warp's 32 rows x kCh columns of a matrix ---------------------------------------------------------
+// TMEM gives a lane a row; memory wants neighbouring lanes on neighbouring columns.  A patch of shared memory
+// turns one into the other; the warp alone uses it.
+
+// Where a lane reads or writes a matrix: kPieces rows, kDown apart, from a column on.
+struct Place {
+    uint8_t *p;            // the first row's piece
+    int64_t down;          // bytes to the next row
+    int vec;               // rows start on 16-byte boundaries
+    __device__ __forceinline__ Place(const void *base, int64_t ld, int e, int vec_, int64_t row, int64_t col)
+        : p(static_cast<uint8_t *>(const_cast<void *>(base)) + (row * ld + col) * e), down(kDown * ld * e), vec(vec_)
+    {
+    }
+};
+
 struct Patch {
-    uint32_t mine, shared;      // a lane's row; its place among the eight rows of an access
+    uint32_t mine, shared;      // a lane's row; its place among the rows of an access
     int row, piece;
 
     __device__ __forceinline__ Patch(uint32_t base, int lane)
-        : mine(base + lane * kPatchPitch), shared(base + (lane / 4) * kPatchPitch + 16 * (lane % 4)), row(lane / 4), piece(lane % 4)
+        : mine(base + lane * kPatchPitch), shared(base + (lane / kPieces) * kPatchPitch + 16 * (lane % kPieces)), row(lane / kPieces),
+          piece(lane % kPieces)
     {
     }
-    // fetch: the four pieces of 16 bytes that this lane reads of rows m0 ... m0 + 31, columns n ... n + 31 (16-bit)
-    __device__ __forceinline__ void fetch(uint4 x[4], const void *p, int64_t ld, int vec, int64_t m0, int64_t n, const Finish &F) const
+    // fetch: kCh 16-bit columns, `at` bytes on; rows: how many of the warp's exist; left: columns from this lane's
+    // piece to the end of the row
+    __device__ __forceinline__ void fetch(uint4 x[kPieces], const Place &w, int at, int rows, int64_t left) const
     {
-        const int64_t c = n + 8 * piece;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t m = m0 + row + 8 * i;
+        for (int i = 0; i < kPieces; ++i) {
+            const uint8_t *q = w.p + at + i * w.down;
             x[i] = make_uint4(0, 0, 0, 0);
-            if (m < F.M && c < F.N) {
-                const uint16_t *q = static_cast<const uint16_t *>(p) + m * ld;
-                if (vec && c + 8 <= F.N) x[i] = *reinterpret_cast<const uint4 *>(q + c);
-                else x[i] = load_bytes16<false>(reinterpret_cast<uintptr_t>(q + c), reinterpret_cast<uintptr_t>(q + F.N));
+            if (row + kDown * i < rows && left > 0) {
+                if (w.vec && left >= 8) x[i] = *reinterpret_cast<const uint4 *>(q);
+                else x[i] = load_bytes16<false>(reinterpret_cast<uintptr_t>(q), reinterpret_cast<uintptr_t>(q) + 2 * left);
             }
         }
     }
-    // add: what the lanes fetched, to the 32 columns of the lane's own row
-    __device__ __forceinline__ void add(const uint4 x[4], float v[32], int dtype) const
+    // add: what the lanes fetched, to the columns of the lane's own row
+    __device__ __forceinline__ void add(const uint4 x[kPieces], float v[kCh], int dtype) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) store_shared_v4(shared + 8 * i * kPatchPitch, x[i]);
+        for (int i = 0; i < kPieces; ++i) store_shared_v4(shared + kDown * i * kPatchPitch, x[i]);
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kPieces; ++i) {
             const uint4 y = load_shared_v4(mine + 16 * i);
             const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -109,50 +130,48 @@ struct Patch {
         }
         __syncwarp();
     }
-    // put: sixteen words of the lane's own row to memory: `e` bytes an element, from column n on
-    __device__ __forceinline__ void put(const uint32_t w[16], void *p, int64_t ld, int vec, int e, int64_t m0, int64_t n, const Finish &F) const
+    // put: the words of the lane's own row, in pieces of `count` elements
+    __device__ __forceinline__ void put(const uint32_t w[4 * kPieces], const Place &to, int at, int rows, int64_t left, int count) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) store_shared_v4(mine + 16 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+        for (int i = 0; i < kPieces; ++i) store_shared_v4(mine + 16 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
         __syncwarp();
-        const int count = 16 / e;                            // elements of a piece
-        const int64_t c = n + count * piece;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 x = load_shared_v4(shared + 8 * i * kPatchPitch);
-            const int64_t m = m0 + row + 8 * i;
-            if (m >= F.M || c >= F.N) continue;
-            uint8_t *q = static_cast<uint8_t *>(p) + (m * ld + c) * e;
-            if (vec && c + count <= F.N) {
+        for (int i = 0; i < kPieces; ++i) {
+            const uint4 x = load_shared_v4(shared + kDown * i * kPatchPitch);
+            uint8_t *q = to.p + at + i * to.down;
+            if (row + kDown * i >= rows || left <= 0) continue;
+            if (to.vec && left >= count) {
                 *reinterpret_cast<uint4 *>(q) = x;
             } else {
                 const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-                const int left = F.N - c < count ? (int)(F.N - c) : count;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if (j >= left) break;
-                    if (e == 4) { if (j < 4) reinterpret_cast<uint32_t *>(q)[j] = y[j % 4]; }
+                    if (j >= left || j >= count) break;
+                    if (count == 4) { if (j < 4) reinterpret_cast<uint32_t *>(q)[j] = y[j % 4]; }
                     else reinterpret_cast<uint16_t *>(q)[j] = (uint16_t)(y[j / 2] >> 16 * (j % 2));
                 }
             }
         }
         __syncwarp();
     }
-    // the same for 32 values, in their type
-    __device__ __forceinline__ void put32(const float v[32], void *p, int64_t ld, int vec, int dtype, int64_t m0, int64_t n, const Finish &F) const
+    // kCh values as 16-bit elements
+    __device__ __forceinline__ void put16(const float v[kCh], const Place &to, int at, int rows, int64_t left, int dtype) const
     {
-        uint32_t w[16];
-        if (dtype == LORDBA_F32) {
+        uint32_t w[kCh / 2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+        for (int i = 0; i < kCh / 2; ++i) w[i] = pack2_any(v[2 * i], v[2 * i + 1], dtype);
+        put(w, to, at, rows, left, 8);
+    }
+    // kCh values as floats
+    __device__ __forceinline__ void put32(const float v[kCh], const Place &to, int at, int rows, int64_t left) const
+    {
+        uint32_t w[kCh / 2];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * h + i]);
-                put(w, p, ld, vec, 4, m0, n + 16 * h, F);
-            }
-        } else {
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = pack2_any(v[2 * i], v[2 * i + 1], dtype);
-            put(w, p, ld, vec, 2, m0, n, F);
+            for (int i = 0; i < kCh / 2; ++i) w[i] = __float_as_uint(v[h * kCh / 2 + i]);
+            put(w, to, at + 2 * kCh * h, rows, left - kCh / 2 * h, 4);
         }
     }
 };
@@ -187,7 +206,7 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
         }
         for (int b = 0; b < 2; ++b) {
             bar_init(sum_full(b), 1);
-            bar_init(sum_empty(b), 2 * kEpiWarps);
+            bar_init(sum_empty(b), kEpiWarps);       // the group's warps in both CTAs
         }
         *abort_flag = 0;
         bar_init_fence();
@@ -277,60 +296,70 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
             }
         }
     } else if (warp >= 4) {
-        const int quadrant = warp % 4, half = (warp - 4) / 4;
-        constexpr int kCols = kTileN / 2;                      // columns of one warp
+        const bool share = P.tiles <= pairs;
+        const int quadrant = warp % 4, group = share ? 0 : (warp - 4) / (kEpiWarps / 2);
+        const int parts = share ? kEpiWarps / 4 : kEpiWarps / 8, part = (warp - 4) / 4 % parts;
+        const int cols = kTileN / parts;                       // of one warp
         const Patch patch(patches + (warp - 4) * kPatchBytes, lane);
-        int buf = 0;
+        const bool adds = GATED && P.f.add[0];
+        const int buf = group;
         uint32_t buf_phase = 0;
         bool alive = true;
-        for (int i = pair; i < P.tiles; i += pairs) {
+        for (int i = pair + group * pairs; i < P.tiles; i += share ? pairs : 2 * pairs) {
             const Tile t = tile_at(P, i);
             const int64_t m0 = (int64_t)t.m * kTileM + 128 * rank + 32 * quadrant;
-            const int64_t n0 = (int64_t)t.n * kTileN + kCols * half;
+            const int64_t n0 = (int64_t)t.n * kTileN + cols * part;
+            const int64_t m = m0 + lane < P.f.M ? m0 + lane : 0;
+            const int rows = P.f.M - m0 < 32 ? (int)(P.f.M - m0) : 32;          // of the warp's that exist (<= 0: none)
+            const int64_t row = m0 + patch.row, col = n0 + 8 * patch.piece;
+            const bool wide = P.f.dtype == LORDBA_F32;
+            const Place out(P.f.out[t.problem], P.f.ldo, wide ? 4 : 2, P.f.vec_out, row, wide ? n0 + 4 * patch.piece : col);
+            const Place pre0(P.f.pre[0], P.f.ld_pre, 2, P.f.vec_pre, row, col), pre1(P.f.pre[1], P.f.ld_pre, 2, P.f.vec_pre, row, col);
+            const Place add0(P.f.add[0], P.f.ld_add, 2, P.f.vec_add, row, col), add1(P.f.add[1], P.f.ld_add, 2, P.f.vec_add, row, col);
+            uint4 xg[kPieces], xu[kPieces];                    // the addends, fetched a step ahead
+            if (adds) {
+                patch.fetch(xg, add0, 0, rows, P.f.N - col);
+                patch.fetch(xu, add1, 0, rows, P.f.N - col);
+            }
             alive = __all_sync(0xffffffffu, bound.wait(sum_full(buf), buf_phase, kDevEpilogueWaitTimeout));
             if (!alive) break;
             fence_after();
-            const uint32_t d = tmem + ((uint32_t)(32 * quadrant) << 16) + 256u * buf + kCols * half;
+            const uint32_t d = tmem + ((uint32_t)(32 * quadrant) << 16) + 256u * buf + cols * part;
 #pragma unroll 1
-            for (int c = 0; c < kCols; c += 32) {
-                const int64_t n = n0 + c;
-                if (m0 >= P.f.M || n >= P.f.N) break;          // the warp's rows or columns lie outside
-                const bool adds = GATED && P.f.add[0];
-                uint4 xg[4], xu[4];
-                if (adds) {
-                    patch.fetch(xg, P.f.add[0], P.f.ld_add, P.f.vec_add, m0, n, P.f);
-                    patch.fetch(xu, P.f.add[1], P.f.ld_add, P.f.vec_add, m0, n, P.f);
+            for (int c = 0; c < cols; c += kCh) {
+                const int64_t n = n0 + c, left = P.f.N - col - c;
+                if (rows <= 0 || n >= P.f.N) break;            // the warp's rows or columns lie outside
+                uint32_t g[kCh], u[kCh];
+#pragma unroll
+                for (int k = 0; k < kCh; k += 16) {
+                    tmem_load16(d + c + k, g + k);
+                    if (GATED) tmem_load16(d + 128 + c + k, u + k);
                 }
-                uint32_t g[32], u[32];
-                tmem_load16(d + c, g);
-                tmem_load16(d + c + 16, g + 16);
-                if (GATED) {
-                    tmem_load16(d + 128 + c, u);
-                    tmem_load16(d + 128 + c + 16, u + 16);
-                }
+                float v[kCh], w[kCh];
                 tmem_wait_load();
-                float v[32], w[32];
-                const int64_t m = m0 + lane < P.f.M ? m0 + lane : m0;
-                const int left = (int)(P.f.N - n < 32 ? P.f.N - n : 32);
-                products_of<INT8, GATED, 32>(P.f, m, n, left, g, u, v, w);
+                products_of<INT8, GATED, kCh>(P.f, m, n, (int)(P.f.N - n < kCh ? P.f.N - n : kCh), g, u, v, w);
                 if (GATED) {
                     if (adds) {
                         patch.add(xg, v, P.f.dtype);
                         patch.add(xu, w, P.f.dtype);
+                        if (c + kCh < cols) {
+                            patch.fetch(xg, add0, 2 * (c + kCh), rows, left - kCh);
+                            patch.fetch(xu, add1, 2 * (c + kCh), rows, left - kCh);
+                        }
                     }
                     if (P.f.pre[0]) {
-                        patch.put32(v, P.f.pre[0], P.f.ld_pre, P.f.vec_pre, P.f.dtype, m0, n, P.f);
-                        patch.put32(w, P.f.pre[1], P.f.ld_pre, P.f.vec_pre, P.f.dtype, m0, n, P.f);
+                        patch.put16(v, pre0, 2 * c, rows, left, P.f.dtype);
+                        patch.put16(w, pre1, 2 * c, rows, left, P.f.dtype);
                     }
-                    gate<32>(P.f.act, v, w);
+                    gate<kCh>(P.f.act, v, w);
                 }
-                patch.put32(v, P.f.out[t.problem], P.f.ldo, P.f.vec_out, P.f.dtype, m0, n, P.f);
+                if (wide) patch.put32(v, out, 4 * c, rows, P.f.N - n - 4 * patch.piece);
+                else patch.put16(v, out, 2 * c, rows, left, P.f.dtype);
             }
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive_cluster(peer_addr(sum_empty(buf), 0));
-            buf ^= 1;
-            buf_phase ^= buf == 0;
+            buf_phase ^= 1u;
         }
     }
 
