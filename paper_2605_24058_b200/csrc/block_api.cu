@@ -206,12 +206,27 @@ int check_grad(const lordba_gated_grad &g, int64_t T, int dtype)
     return LORDBA_OK;
 }
 
-// The two products of a backward pass run one after the other and share the workspace.
-size_t grad_workspace(const lordba_gated_grad &g, int64_t T, int dtype)
+// The workspace of a backward pass: what rounding took from dgate and dup, where that is kept (few tokens), then
+// the operands that a product copies; the two products run one after the other and share that part.
+struct GradWorkspace {
+    size_t lo_bytes, bytes;      // of one of dgate and dup; in all
+    int64_t ld_lo;
+};
+
+GradWorkspace grad_workspace(const lordba_gated_grad &g, int64_t T, int dtype)
 {
-    const size_t a = g.dx ? product_workspace_bytes(dx_product(g, T, dtype)) : 0;
-    const size_t b = g.dw_gate ? product_workspace_bytes(dw_product(g, T, dtype)) : 0;
-    return a > b ? a : b;
+    GradWorkspace w = {};
+    if ((g.dx || g.dw_gate) && T <= kLoTokens) {
+        w.ld_lo = (g.d_hidden + 7) / 8 * 8;
+        w.lo_bytes = ((size_t)T * (size_t)w.ld_lo * 2 + 255) / 256 * 256;
+    }
+    Product dx = dx_product(g, T, dtype), dw = dw_product(g, T, dtype);
+    // the rest lies aligned and is never copied: its place says only that it is there
+    for (Product *q : {&dx, &dw})
+        if (w.lo_bytes) q->lo[0] = q->lo[1] = Operand{reinterpret_cast<const void *>(uintptr_t(256)), w.ld_lo, false};
+    const size_t a = g.dx ? product_workspace_bytes(dx) : 0, b = g.dw_gate ? product_workspace_bytes(dw) : 0;
+    w.bytes = 2 * w.lo_bytes + (a > b ? a : b);
+    return w;
 }
 
 }  // namespace
@@ -271,7 +286,7 @@ int lordba_gated_forward(const lordba_gated *g, int64_t T, int dtype, void *work
 size_t lordba_gated_backward_workspace_bytes(const lordba_gated_grad *g, int64_t T)
 {
     if (!g || bad_size(T, g->d_in) || bad_size(T, g->d_hidden) || T == 0) return 0;
-    return grad_workspace(*g, T, LORDBA_BF16);
+    return grad_workspace(*g, T, LORDBA_BF16).bytes;
 }
 
 int lordba_gated_backward(const lordba_gated_grad *g, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream)
@@ -289,11 +304,21 @@ int lordba_gated_backward(const lordba_gated_grad *g, int64_t T, int dtype, void
             }
         return LORDBA_OK;
     }
-    rc = check_workspace(grad_workspace(*g, T, dtype), workspace, workspace_bytes);
+    const GradWorkspace w = grad_workspace(*g, T, dtype);
+    rc = check_workspace(w.bytes, workspace, workspace_bytes);
     if (rc != LORDBA_OK) return rc;
-    rc = launch_gated_grad(*g, T, dtype, s);
-    if (rc == LORDBA_OK && g->dx) rc = launch_product(dx_product(*g, T, dtype), workspace, s);
-    if (rc == LORDBA_OK && g->dw_gate) rc = launch_product(dw_product(*g, T, dtype), workspace, s);
+    uint8_t *lo_gate = w.lo_bytes ? static_cast<uint8_t *>(workspace) : nullptr, *lo_up = lo_gate ? lo_gate + w.lo_bytes : nullptr;
+    uint8_t *copies = static_cast<uint8_t *>(workspace) + 2 * w.lo_bytes;
+    rc = launch_gated_grad(*g, T, dtype, lo_gate, lo_up, w.ld_lo, s);
+    for (int i = 0; i < 2 && rc == LORDBA_OK; ++i) {
+        if (!(i == 0 ? g->dx : g->dw_gate)) continue;
+        Product q = i == 0 ? dx_product(*g, T, dtype) : dw_product(*g, T, dtype);
+        if (lo_gate) {
+            q.lo[0] = Operand{lo_gate, w.ld_lo, q.a[0].mn_major};
+            q.lo[1] = Operand{lo_up, w.ld_lo, q.a[0].mn_major};
+        }
+        rc = launch_product(q, copies, s);
+    }
     return rc;
 }
 

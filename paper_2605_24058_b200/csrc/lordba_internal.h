@@ -118,7 +118,9 @@ int launch_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ldq, flo
                          int dtype, cudaStream_t stream);
 int launch_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr, void *out, int64_t ldo, int64_t T,
                    int64_t d, int cut, uint64_t seed, uint64_t offset, int dtype, cudaStream_t stream);
-int launch_gated_grad(const lordba_gated_grad &g, int64_t T, int dtype, cudaStream_t stream);
+// lo_gate, lo_up (pitch ld_lo, 16-byte rows; null: not wanted): what rounding took from dgate and dup
+int launch_gated_grad(const lordba_gated_grad &g, int64_t T, int dtype, void *lo_gate, void *lo_up, int64_t ld_lo,
+                      cudaStream_t stream);
 // Copies that give operands a pitch of 16-byte multiples: rows x cols bytes each, any alignment of src.
 struct RepackList {
     struct Item {
@@ -145,6 +147,7 @@ struct Product {
     ProductKind kind;
     int64_t M, N, K;
     Operand a[2], b[2];
+    Operand lo[2];       // added to a[0], a[1] (kSum with at most kLoTokens rows, kPair), or null: A in twice the bits
     // kSingle: D = A0 B0.  kSum: D = A0 B0 + A1 B1.  kGated: gate = A0 B0, up = A0 B1.
     // kPair: two products A0 B0 and A1 B0 with an output each.
     enum Form { kSingle, kSum, kGated, kPair } form;
@@ -158,6 +161,12 @@ struct Product {
     int64_t ld_add, ld_pre;
     int act;
 };
+
+// A product over a gradient's entries inherits their rounding.  Where it is bound by other bytes (the weights that
+// stream past a few tokens, the gradients of the weights) the entries go in with their rounding's rest, which
+// costs nothing; with more tokens they do not: the sums average over the errors (1.4 times that of rounding the
+// result, 1e-3 of it in bfloat16), and the products would take twice as long.
+constexpr int64_t kLoTokens = 64;
 
 size_t product_workspace_bytes(const Product &p);
 int launch_product(const Product &p, void *workspace, cudaStream_t stream);

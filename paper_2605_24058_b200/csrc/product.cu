@@ -71,7 +71,7 @@ bool streams(const Product &p)
 {
     if (p.form == Product::kPair) return false;
     const double stream = stream_estimate(p);
-    if (stream < 0) return false;
+    if (stream < 0 || p.lo[0].p) return p.lo[0].p != nullptr;
     double copied = 0;
     for (int i = 0; i < 2; ++i) copied += (double)packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + (double)packed_bytes(p.b[i], p.N, p.K, elt_of(p));
     return stream <= tile_estimate(p) + (copied > 0 ? 3.0 + copied * 3 / 6.0e6 : 0.0);

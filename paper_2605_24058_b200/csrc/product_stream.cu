@@ -39,11 +39,12 @@ struct Rows {              // a row-major matrix in bytes
 };
 
 struct StreamArgs {
-    CUtensorMap w[2], t[2];
-    Rows rw[2], rt[2];       // the same operands as they lie in memory
+    CUtensorMap w[2], t[4];   // t[2 + i]: the rest of t[i], where halves = 2
+    Rows rw[2], rt[4];       // the same operands as they lie in memory
     Finish f;
     int k_blocks, parts;     // stages per operand pair; operand pairs summed into one accumulator
-    int tokens;              // MMA columns: tokens of a tile, a multiple of 16
+    int tokens;              // of a tile: a multiple of 16
+    int halves;              // 2: the tokens' entries come as two terms, each term MMA columns of its own
     int stages, split;
     int raw_stages;          // LOOSE: stages fetched ahead (2 ... 6)
     int tmem_columns;
@@ -210,7 +211,9 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = (int)cluster_rank();
-    const int stage_bytes = kSums * kWeightBytes + P.tokens * 128;
+    constexpr int kHalves = W_MN ? 2 : 1;                         // at most
+    const int halves = W_MN ? P.halves : 1, columns = halves * P.tokens;
+    const int stage_bytes = kSums * kWeightBytes + columns * 128;
     const int n0 = blockIdx.y * kRows, t0 = blockIdx.z * P.tokens;
     const int blocks = P.k_blocks * P.parts;
     const int first = (int)((int64_t)blocks * rank / P.split), last = (int)((int64_t)blocks * (rank + 1) / P.split);
@@ -258,6 +261,7 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                         }
                     }
                     load_tile(sw + kSums * kWeightBytes, &P.t[part], k0, t0, full(r.stage));
+                    if (halves > 1) load_tile(sw + kSums * kWeightBytes + P.tokens * 128, &P.t[2 + part], k0, t0, full(r.stage));
                 }
                 r.next(P.stages);
             }
@@ -277,7 +281,7 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                     const uint32_t w = desc_low(sw + c * kWeightBytes, W_MN ? kWeightBytes / 2 : 0);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        mma<1, INT8>(tmem + c * P.tokens, w + j * (W_MN ? 128 : 2), t + j * 2, P.idesc, kb - first + j > 0);
+                        mma<1, INT8>(tmem + c * columns, w + j * (W_MN ? 128 : 2), t + j * 2, P.idesc, kb - first + j > 0);
                 }
                 mma_commit<1>(empty(r.stage));
                 r.next(P.stages);
@@ -289,13 +293,16 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
             const int loader = warp < 4 ? warp : warp - 2;
             const uint32_t raw0 = base + P.stages * stage_bytes;
             const int raw_weight = W_MN ? 64 * kRawPitch<2> : kRows * kRawPitch<1>;
-            const int raw_bytes = kSums * raw_weight + P.tokens * kRawPitch<1>;
+            const int raw_bytes = kSums * raw_weight + columns * kRawPitch<1>;
             constexpr int kBoxes = W_MN ? 2 : 1, kBoxRows = W_MN ? 64 : kRows;
             // of a sum of two products the second has operands of its own
             const Share<kBoxes> w0(loader, lane, P.rw[0], W_MN ? 2 * (int64_t)n0 : 0, W_MN ? 0 : n0, kBoxRows);
             const Share<kBoxes> w1(loader, lane, P.rw[GATED || P.parts > 1 ? 1 : 0], W_MN ? 2 * (int64_t)n0 : 0, W_MN ? 0 : n0, kBoxRows);
             const Share<1> tok0(loader, lane, P.rt[0], 0, t0, P.tokens);
             const Share<1> tok1(loader, lane, P.rt[W_MN && P.parts > 1 ? 1 : 0], 0, t0, P.tokens);
+            const Share<1> rest0(loader, lane, P.rt[halves > 1 ? 2 : 0], 0, t0, P.tokens);
+            const Share<1> rest1(loader, lane, P.rt[halves > 1 ? 3 : 0], 0, t0, P.tokens);
+            const int raw_rest = kSums * raw_weight + P.tokens * kRawPitch<1>, rest_at = kSums * kWeightBytes + P.tokens * 128;
             const int64_t contraction = W_MN ? P.rw[0].rows : 0, ld = P.rw[0].ld;
             auto fetch = [&](int kb, int slot) {
                 const uint32_t raw = raw0 + slot * raw_bytes;
@@ -313,6 +320,10 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                     }
                     if (second) tok1.fetch(raw + kSums * raw_weight, 128 * at, 0, tok1.rows, P.tokens);
                     else tok0.fetch(raw + kSums * raw_weight, 128 * at, 0, tok0.rows, P.tokens);
+                    if (halves > 1) {
+                        if (second) rest1.fetch(raw + raw_rest, 128 * at, 0, rest1.rows, P.tokens);
+                        else rest0.fetch(raw + raw_rest, 128 * at, 0, rest0.rows, P.tokens);
+                    }
                 }
                 fetch_commit();        // also where there is nothing left: the groups are counted
             };
@@ -336,6 +347,10 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                 }
                 if (second) tok1.shift(raw + kSums * raw_weight, sw + kSums * kWeightBytes, 128 * at, P.tokens);
                 else tok0.shift(raw + kSums * raw_weight, sw + kSums * kWeightBytes, 128 * at, P.tokens);
+                if (halves > 1) {
+                    if (second) rest1.shift(raw + raw_rest, sw + rest_at, 128 * at, P.tokens);
+                    else rest0.shift(raw + raw_rest, sw + rest_at, 128 * at, P.tokens);
+                }
                 fence_proxy_async();
                 if (kb - first != P.skip) bar_arrive(full(r.stage));
                 __syncwarp();
@@ -346,14 +361,14 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
             fetch_wait(0);
             __syncwarp();
         }
-        // the partial sums go where the ring was: [sum][token][128 weight rows]
+        // the partial sums go where the ring was: [sum][half][token][128 weight rows]
         const int quadrant = warp;
         const bool alive = warp < 4 && __all_sync(0xffffffffu, bound.wait(sum_full, 0, kDevEpilogueWaitTimeout));
         if (alive) {
             fence_after();
             const uint32_t d = tmem + ((uint32_t)(32 * quadrant) << 16);
             uint32_t *sums = reinterpret_cast<uint32_t *>(smem_raw + (base - raw)) + 32 * quadrant + lane;
-            for (int c = 0; c < kSums * P.tokens; c += 16) {
+            for (int c = 0; c < kSums * columns; c += 16) {
                 uint32_t v[16];
                 tmem_load16(d + c, v);
                 tmem_wait_load();
@@ -396,7 +411,9 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                         const int i = it + k * step < items ? it + k * step : it;
 #pragma unroll
                         for (int c = 0; c < kSums; ++c) {
-                            const uint4 v = load_peer_v4(from + 4u * ((c * P.tokens + i / (kRows / 4)) * kRows));
+                            const uint32_t at = from + 4u * ((c * columns + i / (kRows / 4)) * kRows);
+                            uint4 v = load_peer_v4(at);
+                            if (kHalves > 1 && halves > 1) v = add4<INT8>(v, load_peer_v4(at + 4u * P.tokens * kRows));
                             acc[k][c] = r == 0 ? v : add4<INT8>(acc[k][c], v);
                         }
                     }
@@ -464,7 +481,7 @@ int resident_clusters(bool int8, bool gated, bool loose, int split)
 
 struct StreamPlan {
     bool loose;
-    int tokens, k_blocks, parts, stages, raw_stages, split, smem;
+    int tokens, halves, k_blocks, parts, stages, raw_stages, split, smem;
     int64_t row_tiles, token_tiles;
     double us;             // estimate
 };
@@ -477,16 +494,17 @@ StreamPlan plan_stream(const Product &p)
     s.k_blocks = (int)((p.K + block_k - 1) / block_k);
     s.parts = p.form == Product::kSum ? 2 : 1;
     s.tokens = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    s.halves = p.lo[0].p ? 2 : 1;
     s.loose = !(taken_as_is(p.a[0], e) && taken_as_is(p.a[1], e) && taken_as_is(p.b[0], e) && taken_as_is(p.b[1], e));
     s.row_tiles = (p.N + kRows - 1) / kRows;
     s.token_tiles = (p.M + s.tokens - 1) / s.tokens;
-    const int stage = sums * kWeightBytes + s.tokens * 128, exchange = sums * s.tokens * kRows * 4;
+    const int columns = s.halves * s.tokens, stage = sums * kWeightBytes + columns * 128, exchange = sums * columns * kRows * 4;
     const int fixed = kBarBytes + 1024, half = kHalf - fixed, whole = kWhole - fixed;
     // two CTAs an SM where three stages and the exchange fit half of its shared memory, else one
     const int per_sm = !s.loose && 3 * stage <= half && exchange <= half ? 2 : 1;
     int used;
     if (s.loose) {
-        const int raw = sums * (w_mn ? 64 * kRawPitch<2> : kRows * kRawPitch<1>) + s.tokens * kRawPitch<1>;
+        const int raw = sums * (w_mn ? 64 * kRawPitch<2> : kRows * kRawPitch<1>) + columns * kRawPitch<1>;
         s.stages = 3 * stage + 3 * raw <= whole ? 3 : 2;
         s.raw_stages = (whole - s.stages * stage) / raw < 6 ? (whole - s.stages * stage) / raw : 6;
         used = s.stages * stage + s.raw_stages * raw;
@@ -540,6 +558,7 @@ int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream
     a.k_blocks = plan.k_blocks;
     a.parts = plan.parts;
     a.tokens = plan.tokens;
+    a.halves = plan.halves;
     a.stages = plan.stages;
     a.raw_stages = plan.raw_stages;
     a.split = plan.split;
@@ -548,16 +567,19 @@ int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream
         const int64_t w_rows = w_mn ? p.K : p.N, w_cols = w_mn ? p.N : p.K;
         a.rt[i] = Rows{static_cast<const uint8_t *>(ot.p), ot.ld * e, p.M, p.K * e};
         a.rw[i] = Rows{static_cast<const uint8_t *>(ow.p), ow.ld * e, w_rows, w_cols * e};
+        const Operand &ol = p.lo[i];
+        a.rt[2 + i] = Rows{static_cast<const uint8_t *>(ol.p), ol.ld * e, p.M, p.K * e};
         if (plan.loose) continue;
+        if (ol.p && !encode_map(&a.t[2 + i], ol.p, p.M, p.K, ol.ld, e, a.tokens)) return LORDBA_ECUDA;
         if (ot.p && !encode_map(&a.t[i], ot.p, p.M, p.K, ot.ld, e, a.tokens)) return LORDBA_ECUDA;
         if (ow.p && !encode_map(&a.w[i], ow.p, w_rows, w_cols, ow.ld, e, w_mn ? 64 : kRows)) return LORDBA_ECUDA;
     }
     a.tmem_columns = 32;
-    while (a.tmem_columns < (gated ? 2 : 1) * a.tokens) a.tmem_columns *= 2;
+    while (a.tmem_columns < (gated ? 2 : 1) * a.halves * a.tokens) a.tmem_columns *= 2;
     a.skip = test_skip_item();
     a.status = device_status_word();
     if (!a.status) return LORDBA_ECUDA;
-    a.idesc = instr_desc(int8, p.kind == kProductBf16, w_mn, false, kRows, a.tokens);
+    a.idesc = instr_desc(int8, p.kind == kProductBf16, w_mn, false, kRows, a.halves * a.tokens);
     LaunchRec rec;
     std::memset(&rec, 0, sizeof(rec));
     rec.func = kernel_of(int8, gated, plan.loose);

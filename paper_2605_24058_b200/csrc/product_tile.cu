@@ -46,7 +46,7 @@ constexpr int kPatchBytes = 32 * kPatchPitch;
 constexpr int kTileSmem = kStages * kStageBytes + kEpiWarps * kPatchBytes + kBarBytes + 1024;
 
 struct TileArgs {
-    CUtensorMap a[2], b[2];
+    CUtensorMap a[4], b[2];      // of two problems, the second one's A (and rest of A) are a[1] (and a[3])
     Finish f;
     int k_blocks;          // stages per operand pair
     int parts;             // operand pairs summed into one accumulator
@@ -240,8 +240,8 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
                     if (count != P.skip) {
                         const int part = kb >= P.k_blocks ? 1 : 0;
                         const int k0 = (kb - part * P.k_blocks) * kBlockK;
-                        const CUtensorMap *ma = &P.a[P.problems > 1 ? t.problem : part];
-                        const CUtensorMap *mb = &P.b[GATED ? (int)rank : part];
+                        const CUtensorMap *ma = &P.a[P.problems > 1 ? t.problem + 2 * part : part];
+                        const CUtensorMap *mb = &P.b[GATED ? (int)rank : P.problems > 1 ? 0 : part];
                         const uint32_t sa = base + r.stage * kStageBytes, sb = sa + kHalf;
                         const uint32_t bar = peer_addr(full(r.stage), 0);
                         if (A_MN) {
@@ -451,10 +451,14 @@ int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
         if (ob.p && !(ob.mn_major ? encode_map(&a.b[i], ob.p, p.K, p.N, ob.ld, e, 64) : encode_map(&a.b[i], ob.p, p.N, p.K, ob.ld, e, 128)))
             return LORDBA_ECUDA;
     }
+    for (int i = 0; i < 2; ++i) {
+        const Operand &ol = p.lo[i];
+        if (ol.p && !encode_map(&a.a[2 + i], ol.p, p.K, p.M, ol.ld, e, 64)) return LORDBA_ECUDA;
+    }
     const bool a_mn = p.a[0].mn_major, b_mn = p.b[0].mn_major;
     a.f = f;
     a.k_blocks = (int)((p.K + block_k - 1) / block_k);
-    a.parts = p.form == Product::kSum ? 2 : 1;
+    a.parts = p.form == Product::kSum || p.lo[0].p ? 2 : 1;
     a.problems = pair ? 2 : 1;
     const int64_t tm = (p.M + kTileM - 1) / kTileM, tn = (p.N + (gated ? 127 : 255)) / (gated ? 128 : 256);
     if (tm * tn * a.problems > (int64_t)1 << 30) return LORDBA_EUNSUPPORTED;

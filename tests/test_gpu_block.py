@@ -8,7 +8,9 @@ f16 results below 2^-14 are multiples of 2^-24).
     (truncating adders), so |err| <= K 2^-23 sum |a b|, then u.
   activation: the hardware exponential and division are good to 2^-20 for |g| < 16; 2^-18 covers both.
   gradients to x and to the weights are held to the float64 products of the dgate / dup that the call itself
-    returned (they are operands of the products in that type), dgate and dup to the formula.
+    returned (they are operands of the products in that type), dgate and dup to the formula.  Up to 64 tokens
+    the products take dgate and dup as two terms, and are held to products of the formula's values: the second
+    term leaves u^2 of an entry (of float16 at least 2^-25), the formula 2^-18 of its magnitudes.
 """
 import math
 
@@ -304,9 +306,17 @@ def test_gated_backward(T, d_in, d_hidden, pad, lead, dtype, act):
     close(dgate, v * u * slope, 2.0 ** -18 * np.abs(v * u) * 2.4, dtype, "dgate")
     close(dup, v * a, 2.0 ** -18 * np.abs(v * a), dtype, "dup")
     dg, du = f64(dgate), f64(dup)
-    close(dx, dg @ vg + du @ vu, 2 * d_hidden * 2.0 ** -23 * (np.abs(dg) @ np.abs(vg) + np.abs(du) @ np.abs(vu)), dtype, "dx")
-    close(dwg, dg.T @ vx, T * 2.0 ** -23 * (np.abs(dg).T @ np.abs(vx)), dtype, "dw_gate")
-    close(dwu, du.T @ vx, T * 2.0 ** -23 * (np.abs(du).T @ np.abs(vx)), dtype, "dw_up")
+    eg = eu = 0.0
+    terms = 1
+    if T <= 64:
+        dg, du, terms = v * u * slope, v * a, 2
+        eg = 2.0 ** -18 * np.abs(v * u) * 2.4 + UNIT[dtype] ** 2 * np.abs(dg) + TINY[dtype]
+        eu = 2.0 ** -18 * np.abs(du) + UNIT[dtype] ** 2 * np.abs(du) + TINY[dtype]
+    mg, mu = np.abs(dg) + eg, np.abs(du) + eu
+    err = terms * 2 * d_hidden * 2.0 ** -23 * (mg @ np.abs(vg) + mu @ np.abs(vu))
+    close(dx, dg @ vg + du @ vu, err + (eg + 0 * dg) @ np.abs(vg) + (eu + 0 * du) @ np.abs(vu), dtype, "dx")
+    close(dwg, dg.T @ vx, terms * T * 2.0 ** -23 * (mg.T @ np.abs(vx)) + (eg + 0 * dg).T @ np.abs(vx), dtype, "dw_gate")
+    close(dwu, du.T @ vx, terms * T * 2.0 ** -23 * (mu.T @ np.abs(vx)) + (eu + 0 * du).T @ np.abs(vx), dtype, "dw_up")
     for (buf, _), rows, cols in zip(bufs, (T, T, T, d_hidden, d_hidden), (d_hidden, d_hidden, d_in, d_in, d_in)):
         untouched(buf, rows, cols, pad, lead)
     # the parts alone give the same bits
