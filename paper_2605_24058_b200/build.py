@@ -1,4 +1,4 @@
-"""Build liblordba.so (sm_100a only) in-tree with nvcc.
+"""Build liblordba.so (sm_100a only) in-tree with nvcc, and the Python module _block next to it.
 
 ``python -m paper_2605_24058_b200.build`` or ``build_library()``.  Objects go
 to ``paper_2605_24058_b200/_build``; the shared object sits next to this file so
@@ -19,6 +19,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblordba.so")
 TESTHOOKS_LIB = os.path.join(PKG, "liblordba_testhooks.so")
 SOURCES = ("api.cu", "block_api.cu", "elementwise.cu", "product.cu", "product_tile.cu", "product_stream.cu", "pack.cu", "fit.cu", "forward_fma.cu", "forward_tc.cu", "forward_mma.cu")
+BINDING = os.path.join(PKG, "_block.so")       # Python module of csrc/binding.cpp
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Wno-deprecated-gpu-targets",
               "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -35,6 +36,32 @@ def _newest_header() -> float:
     paths = [os.path.join(ROOT, "include", "lordba.h")]
     paths += [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
     return max(os.path.getmtime(p) for p in paths)
+
+
+def build_binding(force: bool = False) -> str:
+    """Build the Python module ``_block`` (csrc/binding.cpp; g++ against the headers of the installed torch)."""
+    src = os.path.join(CSRC, "binding.cpp")
+    newest = max(os.path.getmtime(src), os.path.getmtime(os.path.join(ROOT, "include", "lordba.h")))
+    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= newest:
+        return BINDING
+    import sysconfig
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    includes = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"], os.path.join(cuda, "include"), os.path.join(ROOT, "include")]
+    tmp = BINDING + ".tmp.%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    for d in includes:
+        cmd += ["-isystem" if d.startswith(home) else "-I", d]
+    cmd += [src, "-o", tmp, "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ldl"]
+    p = subprocess.run(cmd, capture_output=True, text=True)
+    if p.returncode != 0:
+        sys.stderr.write(p.stdout + p.stderr)
+        raise RuntimeError("g++ failed: " + " ".join(cmd))
+    os.replace(tmp, BINDING)
+    return BINDING
 
 
 def build_library(force: bool = False, verbose: bool = False, test_hooks: bool = False) -> str:
@@ -70,6 +97,8 @@ def build_library(force: bool = False, verbose: bool = False, test_hooks: bool =
         tmp = lib_path + ".tmp.%d" % os.getpid()
         run([nvcc, "-shared", "-o", tmp] + objs + ["-Xlinker", "--exclude-libs=ALL"])
         os.replace(tmp, lib_path)
+    if not test_hooks:
+        build_binding(force)
     return lib_path
 
 

@@ -1,7 +1,8 @@
-"""Thin ctypes binding of liblordba.so: argument marshalling only.
+"""Thin binding of liblordba.so: argument marshalling only.
 
 Every function has the name of the C entry point it calls (see
-``include/lordba.h``).  torch supplies device memory and the current stream;
+``include/lordba.h``).  The adapter's and the fit's calls go through ctypes, the
+operators next to the adapters through the module ``_block`` (``csrc/binding.cpp``).  torch supplies device memory and the current stream;
 all arithmetic happens in the CUDA kernels.  There is no CPU fallback: if the
 shared library is missing or a call fails, an exception is raised.
 """
@@ -140,6 +141,20 @@ def load() -> ctypes.CDLL:
                                "`python -m paper_2605_24058_b200.build`" % LIB_PATH)
         _lib = bind(LIB_PATH)
     return _lib
+
+
+_block = None
+
+
+def _native():
+    """The module that marshals the operators next to the adapters, bound to the library."""
+    global _block
+    if _block is None:
+        load()
+        from . import _block as module
+        module.bind(LIB_PATH, LordbaError)
+        _block = module
+    return _block
 
 
 def exported_symbols() -> Sequence[str]:
@@ -442,104 +457,12 @@ def fit_scales(target, packed_A, packed_B, s_in, s_r, s_out, r: int, sweeps: int
     _check(rc, "lordba_fit_scales")
 
 
-_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-
-
-def _code(dtype: torch.dtype, what: str) -> int:
-    code = _CODES.get(dtype)
-    if code is None:
-        raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (what, dtype))
-    return code
-
-
-def _pitch(t: torch.Tensor, shape, dtype: torch.dtype, device: int, what: str) -> int:
-    """Check a 2-D operand with contiguous rows on the current device; its row pitch in elements."""
-    if t.dtype is dtype and t.get_device() == device and t.shape == shape:
-        ld, inner = t.stride()
-        rows, cols = shape
-        if inner == 1 or cols == 1:
-            if rows <= 1:
-                return ld if ld > cols else cols          # a single row has no pitch of its own
-            if ld >= cols:
-                return ld
-            raise ValueError("rows of %s overlap" % what)
-        raise ValueError("rows of %s must be contiguous" % what)
-    if t.dtype is not dtype:
-        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
-    if t.get_device() != device:
-        raise ValueError("%s must be on the current CUDA device" % what)
-    raise ValueError("%s must be %s, got %s" % (what, tuple(shape), tuple(t.shape)))
-
-
-def _pitch_of_pair(a, b, shape, dtype, device: int, what: str) -> int:
-    """The pitch that both matrices of a pair have."""
-    if a is None or b is None:
-        raise ValueError("%s come together" % what)
-    ld = _pitch(a, shape, dtype, device, what)
-    if _pitch(b, shape, dtype, device, what) != ld and shape[0] > 1:
-        raise ValueError("%s must have one row pitch" % what)
-    return ld
-
-
-def _vector(t: torch.Tensor, n: int, device: int, what: str) -> int:
-    """Check a float32 vector; its address."""
-    if t.dtype is torch.float32 and t.numel() == n and t.is_contiguous() and t.get_device() == device:
-        return t.data_ptr()
-    if t.get_device() != device:
-        raise ValueError("%s must be on the current CUDA device" % what)
-    raise TypeError("%s must be %d contiguous float32 values" % (what, n))
-
-
-def _rows(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
-    """A new matrix whose rows start on 16-byte boundaries (what the copy engine takes).  It belongs to the stream
-    the call runs on: its memory is free for that stream's work."""
-    step = 16 // dtype.itemsize
-    pitch = -(-shape[1] // step) * step
-    if stream is None:
-        return torch.empty_strided(shape, (pitch, 1), dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty_strided(shape, (pitch, 1), dtype=dtype, device=device)
-
-
-def _values(n: int, dtype: torch.dtype, device, stream) -> torch.Tensor:
-    """A new vector, of the call's stream like _rows."""
-    if stream is None:
-        return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
-
-
-def _workspace(nbytes: int, given: Optional[torch.Tensor], device, stream):
-    """(tensor to keep alive, address, size) of a call's workspace: the caller's, or one made here."""
-    if given is not None:
-        _need_cuda(given)
-        return given, given.data_ptr(), given.numel() * given.element_size()
-    if nbytes == 0:
-        return None, None, 0
-    ws = _values(nbytes, torch.uint8, device, stream)
-    return ws, ws.data_ptr(), nbytes
-
-
 def int8_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, stream=None):
     """Activations (T, d) in bfloat16, float16 or float32 -> (q, scale): int8 rows and one float32 scale a row,
     scale = max|row| / 127, q = round(row * 127 / max|row|) (ties to even).  q and scale are made here if absent
     (q with rows on 16-byte boundaries, as int8_linear likes them best) and belong, like all tensors that the calls
     below make, to the stream the call runs on."""
-    if x.dim() != 2:
-        raise ValueError("x must be (T, d)")
-    shape, dev = x.shape, torch.cuda.current_device()
-    T, d = shape
-    dtype = _code(x.dtype, "x")
-    ldx = _pitch(x, shape, x.dtype, dev, "x")
-    if q is None:
-        q = _rows(shape, torch.int8, x.device, stream)
-    if scale is None:
-        scale = _values(T, torch.float32, x.device, stream)
-    ldq = _pitch(q, shape, torch.int8, dev, "q")
-    rc = load().lordba_int8_quantize_rows(x.data_ptr(), ldx, q.data_ptr(), ldq, _vector(scale, T, dev, "scale"), T, d, dtype,
-                                          _stream(stream))
-    _check(rc, "lordba_int8_quantize_rows")
-    return q, scale
+    return _native().int8_quantize_rows(x, q, scale, stream)
 
 
 def int8_linear(x, s_x, w, s_w, y: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
@@ -547,21 +470,8 @@ def int8_linear(x, s_x, w, s_w, y: Optional[torch.Tensor] = None, dtype: torch.d
     """y[t, n] = s_x[t] s_w[n] sum_k x[t, k] w[n, k] for int8 x (T, d_in) and w (d_out, d_in): the frozen base
     projection that an adapter's term is added to.  y (of its own type, or of ``dtype`` when made here) is
     overwritten and returned.  workspace: a uint8 CUDA tensor of lordba_int8_linear_workspace_bytes(), made here
-    if absent; only operands off 16-byte boundaries need one."""
-    if x.dim() != 2 or w.dim() != 2:
-        raise ValueError("x must be (T, d_in) and w (d_out, d_in)")
-    dev = torch.cuda.current_device()
-    T, d_in = x.shape
-    d_out = w.shape[0]
-    if y is None:
-        y = _rows((T, d_out), dtype, x.device, stream)
-    p = Int8Proj(x.data_ptr(), _vector(s_x, T, dev, "s_x"), w.data_ptr(), _vector(s_w, d_out, dev, "s_w"), y.data_ptr(), d_in, d_out,
-                 _pitch(x, x.shape, torch.int8, dev, "x"), _pitch(w, (d_out, d_in), torch.int8, dev, "w"),
-                 _pitch(y, (T, d_out), y.dtype, dev, "y"))
-    lib, ref = load(), ctypes.byref(p)
-    keep, ws, nbytes = _workspace(lib.lordba_int8_linear_workspace_bytes(ref, T), workspace, x.device, stream)
-    _check(lib.lordba_int8_linear(ref, T, _code(y.dtype, "y"), ws, nbytes, _stream(stream)), "lordba_int8_linear")
-    return y
+    if absent; only some calls with operands off 16-byte boundaries need one."""
+    return _native().int8_linear(x, s_x, w, s_w, y, dtype, workspace, stream)
 
 
 def gated_forward(x, w_gate, w_up, h: Optional[torch.Tensor] = None, act: int = ACT_SILU, scales=None,
@@ -573,45 +483,7 @@ def gated_forward(x, w_gate, w_up, h: Optional[torch.Tensor] = None, act: int = 
     s_up) and ``dtype`` the type of the rest (bfloat16 if not given).  gate_add / up_add: what the adapters of the
     two projections add.  save=True (or gate and up given) stores g and u for gated_backward; otherwise gate and
     up come back as None."""
-    if x.dim() != 2 or w_gate.dim() != 2:
-        raise ValueError("x must be (T, d_in), w_gate and w_up (d_hidden, d_in)")
-    dev, kind = torch.cuda.current_device(), x.dtype
-    T, d_in = x.shape
-    d_hidden = w_gate.shape[0]
-    shape = (T, d_hidden)
-    s_x = s_gate = s_up = None
-    flags = 0
-    if (kind is torch.int8) != (scales is not None):
-        raise ValueError("int8 operands come with scales = (s_x, s_gate, s_up), others without")
-    if scales is None:
-        dtype = kind
-    else:
-        dtype = h.dtype if h is not None else dtype or torch.bfloat16
-        s_x, s_gate, s_up = (_vector(scales[0], T, dev, "s_x"), _vector(scales[1], d_hidden, dev, "s_gate"),
-                             _vector(scales[2], d_hidden, dev, "s_up"))
-        flags = GATED_INT8
-    code = _code(dtype, "h")
-    ldx = _pitch(x, x.shape, kind, dev, "x")
-    ldw = _pitch_of_pair(w_gate, w_up, (d_hidden, d_in), kind, dev, "w_gate and w_up")
-    if h is None:
-        h = _rows(shape, dtype, x.device, stream)
-    ldh = _pitch(h, shape, dtype, dev, "h")
-    ga = ua = gp = up_ = None
-    ld_add = ld_pre = 0
-    if gate_add is not None or up_add is not None:
-        ld_add = _pitch_of_pair(gate_add, up_add, shape, dtype, dev, "gate_add and up_add")
-        ga, ua = gate_add.data_ptr(), up_add.data_ptr()
-    if save and gate is None and up is None:
-        gate, up = _rows(shape, dtype, x.device, stream), _rows(shape, dtype, x.device, stream)
-    if gate is not None or up is not None:
-        ld_pre = _pitch_of_pair(gate, up, shape, dtype, dev, "gate and up")
-        gp, up_ = gate.data_ptr(), up.data_ptr()
-    p = Gated(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), s_x, s_gate, s_up, ga, ua, gp, up_, h.data_ptr(), d_in, d_hidden,
-              ldx, ldw, ld_add, ld_pre, ldh, act, flags)
-    lib, ref = load(), ctypes.byref(p)
-    keep, ws, nbytes = _workspace(lib.lordba_gated_workspace_bytes(ref, T), workspace, x.device, stream)
-    _check(lib.lordba_gated_forward(ref, T, code, ws, nbytes, _stream(stream)), "lordba_gated_forward")
-    return h, gate, up
+    return _native().gated_forward(x, w_gate, w_up, h, act, scales, dtype, gate_add, up_add, gate, up, save, workspace, stream)
 
 
 def gated_backward(dh, gate, up, x=None, w_gate=None, w_up=None, dgate=None, dup=None, dx=None, dw_gate=None, dw_up=None,
@@ -620,69 +492,14 @@ def gated_backward(dh, gate, up, x=None, w_gate=None, w_up=None, dgate=None, dup
 
     dgate and dup (the gradients of gate_add and up_add) are always made.  dx is made when w_gate and w_up are
     given, dw_gate and dw_up when x is given (None: frozen weights); what is not made comes back as None."""
-    if dh.dim() != 2:
-        raise ValueError("dh must be (T, d_hidden)")
-    dev, dtype, shape, device = torch.cuda.current_device(), dh.dtype, dh.shape, dh.device
-    T, d_hidden = shape
-    code = _code(dtype, "dh")
-    ld_dh = _pitch(dh, shape, dtype, dev, "dh")
-    ld_pre = _pitch_of_pair(gate, up, shape, dtype, dev, "gate and up")
-    if dgate is None and dup is None:
-        dgate, dup = _rows(shape, dtype, device, stream), _rows(shape, dtype, device, stream)
-    ld_dpre = _pitch_of_pair(dgate, dup, shape, dtype, dev, "dgate and dup")
-    d_in = 1
-    ldx = ldw = ld_dx = ld_dw = 0
-    px = pwg = pwu = pdx = pdwg = pdwu = None
-    if w_gate is not None or w_up is not None:
-        if w_gate is None or w_up is None or w_gate.dim() != 2:
-            raise ValueError("w_gate and w_up come together, as (d_hidden, d_in)")
-        d_in = w_gate.shape[1]
-        ldw = _pitch_of_pair(w_gate, w_up, (d_hidden, d_in), dtype, dev, "w_gate and w_up")
-        if dx is None:
-            dx = _rows((T, d_in), dtype, device, stream)
-        ld_dx = _pitch(dx, (T, d_in), dtype, dev, "dx")
-        pwg, pwu, pdx = w_gate.data_ptr(), w_up.data_ptr(), dx.data_ptr()
-    elif dx is not None:
-        raise ValueError("dx needs w_gate and w_up")
-    if x is not None:
-        if x.dim() != 2 or (w_gate is not None and x.shape[1] != d_in):
-            raise ValueError("x must be (T, d_in)")
-        d_in = x.shape[1]
-        ldx = _pitch(x, (T, d_in), dtype, dev, "x")
-        if dw_gate is None and dw_up is None:
-            dw_gate, dw_up = _rows((d_hidden, d_in), dtype, device, stream), _rows((d_hidden, d_in), dtype, device, stream)
-        ld_dw = _pitch_of_pair(dw_gate, dw_up, (d_hidden, d_in), dtype, dev, "dw_gate and dw_up")
-        px, pdwg, pdwu = x.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr()
-    elif dw_gate is not None or dw_up is not None:
-        raise ValueError("dw_gate and dw_up need x")
-    p = GatedGrad(dh.data_ptr(), gate.data_ptr(), up.data_ptr(), px, pwg, pwu, dgate.data_ptr(), dup.data_ptr(), pdx, pdwg, pdwu,
-                  d_in, d_hidden, ld_dh, ld_pre, ldx, ldw, ld_dpre, ld_dx, ld_dw, act, 0)
-    lib, ref = load(), ctypes.byref(p)
-    keep, ws, nbytes = _workspace(lib.lordba_gated_backward_workspace_bytes(ref, T), workspace, device, stream)
-    _check(lib.lordba_gated_backward(ref, T, code, ws, nbytes, _stream(stream)), "lordba_gated_backward")
-    return dgate, dup, dx, dw_gate, dw_up
-
-
-_U64 = (1 << 64) - 1
+    return _native().gated_backward(dh, gate, up, x, w_gate, w_up, dgate, dup, dx, dw_gate, dw_up, act, workspace, stream)
 
 
 def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out: Optional[torch.Tensor] = None,
             stream=None) -> torch.Tensor:
     """out = residual + (keep ? x / (1 - p) : 0), p to the nearest 1/65536; keep follows from (row, column, seed,
     offset), so the same call on the gradient (without a residual) is the backward pass.  out may be x or residual."""
-    if x.dim() != 2:
-        raise ValueError("x must be (T, d)")
-    dev, shape, dtype = torch.cuda.current_device(), x.shape, x.dtype
-    code = _code(dtype, "x")
-    ldx = _pitch(x, shape, dtype, dev, "x")
-    if out is None:
-        out = _rows(shape, dtype, x.device, stream)
-    ldo = _pitch(out, shape, dtype, dev, "out")
-    rp, ldr = (None, 0) if residual is None else (residual.data_ptr(), _pitch(residual, shape, dtype, dev, "residual"))
-    rc = load().lordba_dropout(x.data_ptr(), ldx, rp, ldr, out.data_ptr(), ldo, shape[0], shape[1], p, seed & _U64, offset & _U64, code,
-                               _stream(stream))
-    _check(rc, "lordba_dropout")
-    return out
+    return _native().dropout(x, p, seed, offset, residual, out, stream)
 
 
 def adapter_bits(d_in: int, d_out: int, r: int, ell: int = 1) -> int:
