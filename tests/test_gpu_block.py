@@ -518,3 +518,19 @@ def test_the_binding_refuses_what_it_cannot_take():
     with pytest.raises(lordba.LordbaError):
         lordba.dropout(x[:, :32], 0.5, 0, out=x[:, 16:48])                       # overlapping, not the same
     clean()
+
+
+@pytest.mark.parametrize("tokens,d_model,d_hidden", [(3, 128, 320), (150, 256, 700)])
+def test_the_adapted_block_of_the_example(tokens, d_model, d_hidden):
+    """Served and trained against the same block in float32.  A dozen bfloat16 roundings (2^-9 each in the mean)
+    lie between the two; in the served path a value near a step of the 8-bit grid may land on the other side
+    (1/127 of a row's largest entry, for the few entries that do)."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "adapted_feed_forward.py")
+    spec = importlib.util.spec_from_file_location("adapted_feed_forward", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    errors = example.run(tokens, d_model, d_hidden, 8)
+    assert set(errors) == {"served", "output", "dx", "dw_gate", "dw_up"}
+    assert all(e < 12 * 2.0 ** -9 for e in errors.values()), errors
