@@ -12,28 +12,53 @@ namespace {
 
 constexpr int kEltThreads = 256;
 
-// Columns 8 g ... 8 g + 7 of a row of d elements; what lies past d reads as zero.
+// Columns 8 g ... 8 g + 7 of a row of d elements; what lies past d reads as zero.  (Dropout may run in place:
+// these are ordinary loads.)
 template <typename E>
-__device__ __forceinline__ Group8<E> load8(const E *row, int64_t g, int64_t d, bool vec)
+__device__ __noinline__ Group8<E> load8_last(const E *row, int64_t g, int64_t d)
 {
-    if (vec && 8 * g + 8 <= d) return load_group(row + 8 * g);
-    const uintptr_t at = reinterpret_cast<uintptr_t>(row + 8 * g), end = reinterpret_cast<uintptr_t>(row + d);
     Group8<E> v;
-    v.w = load_bytes16<false>(at, end);          // dropout may run in place
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + 8 * g), end = reinterpret_cast<uintptr_t>(row + d);
+    v.w = load_bytes16<false>(at, end);
     if constexpr (sizeof(E) == 4) v.w2 = at + 16 < end ? load_bytes16<false>(at + 16, end) : make_uint4(0, 0, 0, 0);
     return v;
 }
 
 template <typename E>
+__device__ __forceinline__ Group8<E> load8(const E *row, int64_t g, int64_t d, bool vec)
+{
+    if (8 * g + 8 > d) return load8_last(row, g, d);
+    if (vec) return load_group(row + 8 * g);
+    // a whole group, off the 16-byte grid: the aligned pieces that hold it all hold bytes of it
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + 8 * g);
+    const uint4 *p = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
+    const uint32_t by = (uint32_t)at & 15u;
+    constexpr int kWhole = sizeof(Group8<E>) / 16;
+    uint4 x[kWhole + 1];
+#pragma unroll
+    for (int i = 0; i < kWhole; ++i) x[i] = p[i];
+    x[kWhole] = p[by ? kWhole : 0];
+    Group8<E> v;
+    v.w = join_pieces(x[0], x[1], by);
+    if constexpr (sizeof(E) == 4) v.w2 = join_pieces(x[1], x[2], by);
+    return v;
+}
+
+template <typename E>
+__device__ __noinline__ void store8_parts(E *row, int64_t g, int64_t d, float v0, float v1, float v2, float v3, float v4, float v5,
+                                          float v6, float v7)
+{
+    const float v[8] = {v0, v1, v2, v3, v4, v5, v6, v7};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (8 * g + i < d) row[8 * g + i] = from_float<E>(v[i]);
+}
+
+template <typename E>
 __device__ __forceinline__ void store8(E *row, int64_t g, int64_t d, bool vec, const float v[8])
 {
-    if (vec && 8 * g + 8 <= d) {
-        store_group<E>(row + 8 * g, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (8 * g + i < d) row[8 * g + i] = from_float<E>(v[i]);
-    }
+    if (vec && 8 * g + 8 <= d) store_group<E>(row + 8 * g, v);
+    else store8_parts(row, g, d, v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]);
 }
 
 // ---- lordba_int8_quantize_rows ----------------------------------------------------------------------
@@ -186,7 +211,7 @@ __device__ __forceinline__ void store_either(E *row, int64_t g, int64_t d, bool 
 // instructions per eight elements fit beside the loads only with its keys out of the registers: kept there (20
 // words a thread) the same call took 127 us, and two or four rows a thread at a time 91 and 97 us.
 template <typename E, bool RESIDUAL, bool FULL>
-__global__ void __launch_bounds__(kEltThreads, FULL ? 5 : 3)
+__global__ void __launch_bounds__(kEltThreads, FULL ? 5 : 4)
 dropout_kernel(const E *x, int64_t ldx, const E *residual, int64_t ldr, E *out, int64_t ldo, int64_t T, int64_t d,
                uint32_t cut, float scale, const __grid_constant__ PhiloxKeys keys, uint64_t offset, int width_log2, Vec3 vec)
 {
@@ -226,7 +251,7 @@ __device__ __forceinline__ float *rest_of(float v[8])
 // ---- dgate = dh up act'(gate), dup = dh act(gate) ---------------------------------------------------------
 // Measured (2048 x 11008 bf16, 225 MB): 35 us, 6.4 TB/s.
 template <typename E, int ACT, bool FULL>
-__global__ void __launch_bounds__(kEltThreads, FULL ? 4 : 2)
+__global__ void __launch_bounds__(kEltThreads, FULL ? 4 : 3)
 gated_grad_kernel(const E *__restrict__ dh, int64_t ld_dh, const E *__restrict__ gate, const E *__restrict__ up,
                   int64_t ld_pre, E *__restrict__ dgate, E *__restrict__ dup, int64_t ld_dpre, E *__restrict__ lo_gate,
                   E *__restrict__ lo_up, int64_t ld_lo, int64_t T, int64_t d, int width_log2, Vec3 vec)

@@ -63,18 +63,42 @@ size_t packed_bytes(const Operand &o, int64_t mn, int64_t k, int e)
     return taken_as_is(o, e) ? 0 : (packed_pitch(o, mn, k, e) * (size_t)rows_of(o, mn, k) + 255) / 256 * 256;
 }
 
-// Few rows: the weights stream past them.  Many: tiles, if need be of copies of the operands, which cost a
-// launch and three passes over their bytes.  A sum over the tokens has no weights to stream.
+// The product with its unaligned operands as copies would leave them (for planning: the addresses are not
+// looked at).
+Product copied_form(const Product &p)
+{
+    Product q = p;
+    for (int i = 0; i < 2; ++i) {
+        if (!taken_as_is(q.a[i], elt_of(p))) q.a[i] = Operand{reinterpret_cast<const void *>(uintptr_t(256)), (int64_t)packed_pitch(p.a[i], p.M, p.K, elt_of(p)) / elt_of(p), p.a[i].mn_major};
+        if (!taken_as_is(q.b[i], elt_of(p))) q.b[i] = Operand{reinterpret_cast<const void *>(uintptr_t(256)), (int64_t)packed_pitch(p.b[i], p.N, p.K, elt_of(p)) / elt_of(p), p.b[i].mn_major};
+    }
+    return q;
+}
+
+// Few rows, or few results of long sums: the streaming kernel.  Else tiles.  Unaligned operands are copied for the
+// tiles, and for the streaming kernel where that is quicker than its own shifting (many rows, which shift the
+// weights once for each 128 of them); copies cost a launch and three passes over their bytes.
 // Measured, 8-bit 4096 x 4096: 64 rows 8 us streaming, 16 us in tiles; 512 rows 16 and 17 us; 2048 rows 47 and
 // 31 us.  Gated, 16-bit 4096 x 11008: 64 rows 42 and 51 us, 256 rows 96 and 52 us.
-bool streams(const Product &p)
+struct Way {
+    bool stream, copy;
+};
+
+Way way_of(const Product &p)
 {
-    if (p.form == Product::kPair) return false;
-    const double stream = stream_estimate(p);
-    if (stream < 0 || p.lo[0].p) return p.lo[0].p != nullptr;
     double copied = 0;
     for (int i = 0; i < 2; ++i) copied += (double)packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + (double)packed_bytes(p.b[i], p.N, p.K, elt_of(p));
-    return stream <= tile_estimate(p) + (copied > 0 ? 3.0 + copied * 3 / 6.0e6 : 0.0);
+    const double copies = copied > 0 ? 3.0 + copied * 3 / 6.0e6 : 0.0;
+    const bool tiles_too = !(p.lo[0].p && p.form == Product::kSum);       // the second terms of a sum: streaming only
+    Way best = {!tiles_too, copied > 0};
+    double us = tiles_too ? tile_estimate(p) + copies : 1e30;
+    if (copied > 0) {
+        const double t = stream_estimate(copied_form(p));
+        if (t >= 0 && t + copies <= us) { best = Way{true, true}; us = t + copies; }
+    }
+    const double t = stream_estimate(p);
+    if (t >= 0 && t <= us) best = Way{true, false};
+    return best;
 }
 
 bool rows_vec(const void *p, int64_t ld, size_t e) { return aligned(p, 16) && ((size_t)ld * e) % 16 == 0; }
@@ -84,7 +108,7 @@ bool rows_vec(const void *p, int64_t ld, size_t e) { return aligned(p, 16) && ((
 size_t product_workspace_bytes(const Product &p)
 {
     size_t n = 0;
-    if (streams(p)) return 0;
+    if (!way_of(p).copy) return 0;
     for (int i = 0; i < 2; ++i) n += packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + packed_bytes(p.b[i], p.N, p.K, elt_of(p));
     return n;
 }
@@ -95,11 +119,11 @@ int launch_product(const Product &given, void *workspace, cudaStream_t stream)
     const int e = elt_of(p);
     uint8_t *next = static_cast<uint8_t *>(workspace);
     RepackList list = {};
-    const bool stream_it = streams(p);
+    const Way way = way_of(p);
     for (int i = 0; i < 4; ++i) {
         Operand &o = i < 2 ? p.a[i] : p.b[i - 2];
         const int64_t mn = i < 2 ? p.M : p.N;
-        if (stream_it || taken_as_is(o, e)) continue;
+        if (!way.copy || taken_as_is(o, e)) continue;
         const int64_t pitch = (int64_t)packed_pitch(o, mn, p.K, e);
         list.item[list.n++] = RepackList::Item{o.p, next, o.ld * e, pitch, rows_of(o, mn, p.K), cols_of(o, mn, p.K) * e};
         const size_t bytes = packed_bytes(o, mn, p.K, e);
@@ -120,7 +144,7 @@ int launch_product(const Product &given, void *workspace, cudaStream_t stream)
     f.vec_add = rows_vec(p.add[0], p.ld_add, eo) && aligned(p.add[1], 16);
     f.vec_pre = rows_vec(p.pre[0], p.ld_pre, eo) && aligned(p.pre[1], 16);
     f.vec_scale = aligned(p.s_col[0], 16) && aligned(p.s_col[1], 16);
-    if (stream_it) return launch_product_stream(p, f, stream);
+    if (way.stream) return launch_product_stream(p, f, stream);
     return launch_product_tile(p, f, stream);
 }
 

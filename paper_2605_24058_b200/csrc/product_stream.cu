@@ -1,5 +1,7 @@
 // The product kernel for few rows (tokens): the weights stream through, on tcgen05 with the roles swapped.
 //
+// (and for sums so long that their few results leave SMs idle: the split along the contraction fills them)
+//
 //   D[t,n] = sum_k tokens[t,k] weights[n,k]: 128 weight rows are the MMA's 128 rows, 16 ... 128 tokens its
 //   columns, so that nothing is padded to 128 tokens.
 //
@@ -45,6 +47,7 @@ struct StreamArgs {
     int k_blocks, parts;     // stages per operand pair; operand pairs summed into one accumulator
     int tokens;              // of a tile: a multiple of 16
     int halves;              // 2: the tokens' entries come as two terms, each term MMA columns of its own
+    int token_tiles;         // of one problem (T_MN: two problems, with the tokens t[0] and t[1])
     int stages, split;
     int raw_stages;          // LOOSE: stages fetched ahead (2 ... 6)
     int tmem_columns;
@@ -161,7 +164,7 @@ __device__ __forceinline__ void store4(void *p, int64_t at, int n, int vec, int 
 }
 
 template <bool INT8, bool GATED>
-__device__ __forceinline__ void finish4(const Finish &F, int64_t m, int64_t n, const uint32_t acc0[4], const uint32_t acc1[4])
+__device__ __forceinline__ void finish4(const Finish &F, int problem, int64_t m, int64_t n, const uint32_t acc0[4], const uint32_t acc1[4])
 {
     const int left = (int)(F.N - n < 4 ? F.N - n : 4);
     float v[4], w[4];
@@ -180,7 +183,7 @@ __device__ __forceinline__ void finish4(const Finish &F, int64_t m, int64_t n, c
         }
         gate<4>(F.act, v, w);
     }
-    store4(F.out[0], m * F.ldo + n, left, F.vec_out, F.dtype, v);
+    store4(F.out[problem], m * F.ldo + n, left, F.vec_out, F.dtype, v);
 }
 
 template <bool INT8>
@@ -191,7 +194,9 @@ __device__ __forceinline__ uint4 add4(uint4 a, uint4 b)
                       __float_as_uint(__uint_as_float(a.z) + __uint_as_float(b.z)), __float_as_uint(__uint_as_float(a.w) + __uint_as_float(b.w)));
 }
 
-template <bool INT8, bool GATED, bool W_MN, bool LOOSE>
+// W_MN, T_MN: the contraction runs along the rows of the weights (the tokens).  T_MN is the gradients of weights:
+// the "tokens" are rows of the result, the entries of dgate or dup, and the contraction is over the real tokens.
+template <bool INT8, bool GATED, bool W_MN, bool T_MN, bool LOOSE>
 __global__ void __launch_bounds__(threads_of(LOOSE), LOOSE ? 1 : 2)
 product_stream_kernel(const __grid_constant__ StreamArgs P)
 {
@@ -211,10 +216,11 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = (int)cluster_rank();
-    constexpr int kHalves = W_MN ? 2 : 1;                         // at most
-    const int halves = W_MN ? P.halves : 1, columns = halves * P.tokens;
+    constexpr int kHalves = W_MN && !T_MN ? 2 : 1;                // at most
+    const int halves = kHalves > 1 ? P.halves : 1, columns = halves * P.tokens;
     const int stage_bytes = kSums * kWeightBytes + columns * 128;
-    const int n0 = blockIdx.y * kRows, t0 = blockIdx.z * P.tokens;
+    const int problem = T_MN && (int)blockIdx.z >= P.token_tiles ? 1 : 0;
+    const int n0 = blockIdx.y * kRows, t0 = ((int)blockIdx.z - problem * P.token_tiles) * P.tokens;
     const int blocks = P.k_blocks * P.parts;
     const int first = (int)((int64_t)blocks * rank / P.split), last = (int)((int64_t)blocks * (rank + 1) / P.split);
 
@@ -260,7 +266,12 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                             load_tile(sw + c * kWeightBytes, mw, k0, n0, full(r.stage));
                         }
                     }
-                    load_tile(sw + kSums * kWeightBytes, &P.t[part], k0, t0, full(r.stage));
+                    if (T_MN) {
+                        for (int b = 0; b < P.tokens; b += 64)
+                            load_tile(sw + kWeightBytes + b * 128, &P.t[problem], t0 + b, k0, full(r.stage));
+                    } else {
+                        load_tile(sw + kSums * kWeightBytes, &P.t[part], k0, t0, full(r.stage));
+                    }
                     if (halves > 1) load_tile(sw + kSums * kWeightBytes + P.tokens * 128, &P.t[2 + part], k0, t0, full(r.stage));
                 }
                 r.next(P.stages);
@@ -275,13 +286,13 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                 if (!alive) break;
                 fence_after();
                 const uint32_t sw = base + r.stage * stage_bytes;
-                const uint32_t t = desc_low(sw + kSums * kWeightBytes);
+                const uint32_t t = desc_low(sw + kSums * kWeightBytes, T_MN ? 64 * 128 : 0);
 #pragma unroll
                 for (int c = 0; c < kSums; ++c) {
                     const uint32_t w = desc_low(sw + c * kWeightBytes, W_MN ? kWeightBytes / 2 : 0);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        mma<1, INT8>(tmem + c * columns, w + j * (W_MN ? 128 : 2), t + j * 2, P.idesc, kb - first + j > 0);
+                        mma<1, INT8>(tmem + c * columns, w + j * (W_MN ? 128 : 2), t + j * (T_MN ? 128 : 2), P.idesc, kb - first + j > 0);
                 }
                 mma_commit<1>(empty(r.stage));
                 r.next(P.stages);
@@ -424,7 +435,7 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                     const uint32_t g[4] = {acc[k][0].x, acc[k][0].y, acc[k][0].z, acc[k][0].w};
                     const uint4 w = acc[k][GATED ? 1 : 0];
                     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-                    finish4<INT8, GATED>(P.f, t0 + (it + k * step) / (kRows / 4), n0 + j, g, u);
+                    finish4<INT8, GATED>(P.f, problem, t0 + (it + k * step) / (kRows / 4), n0 + j, g, u);
                 }
             }
     }
@@ -434,33 +445,44 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
     }
 }
 
-const void *kernel_of(bool int8, bool gated, bool loose)
+// The instantiations, by number.
+enum Form { kLinear8, kGated8, kGated16, kSum16, kPair16 };
+
+Form form_of(const Product &p)
 {
-    if (int8)
-        return gated ? (loose ? (const void *)&product_stream_kernel<true, true, false, true>
-                              : (const void *)&product_stream_kernel<true, true, false, false>)
-                     : (loose ? (const void *)&product_stream_kernel<true, false, false, true>
-                              : (const void *)&product_stream_kernel<true, false, false, false>);
-    return gated ? (loose ? (const void *)&product_stream_kernel<false, true, false, true>
-                          : (const void *)&product_stream_kernel<false, true, false, false>)
-                 : (loose ? (const void *)&product_stream_kernel<false, false, true, true>
-                          : (const void *)&product_stream_kernel<false, false, true, false>);
+    if (p.kind == kProductInt8) return p.form == Product::kGated ? kGated8 : kLinear8;
+    return p.form == Product::kGated ? kGated16 : p.form == Product::kPair ? kPair16 : kSum16;
+}
+
+const void *kernel_of(Form form, bool loose)
+{
+    switch (form) {
+        case kLinear8: return loose ? (const void *)&product_stream_kernel<true, false, false, false, true>
+                                    : (const void *)&product_stream_kernel<true, false, false, false, false>;
+        case kGated8: return loose ? (const void *)&product_stream_kernel<true, true, false, false, true>
+                                   : (const void *)&product_stream_kernel<true, true, false, false, false>;
+        case kGated16: return loose ? (const void *)&product_stream_kernel<false, true, false, false, true>
+                                    : (const void *)&product_stream_kernel<false, true, false, false, false>;
+        case kSum16: return loose ? (const void *)&product_stream_kernel<false, false, true, false, true>
+                                  : (const void *)&product_stream_kernel<false, false, true, false, false>;
+        default: return (const void *)&product_stream_kernel<false, false, true, true, false>;
+    }
 }
 
 // Clusters of `split` CTAs, one CTA an SM, that fit the device at once (0: the query failed).  For a kernel
 // that allocates TMEM the query never counts more than one CTA an SM, whatever its size; two of this kernel's
 // were seen to run side by side where its shared memory allows it, so the caller multiplies.  The query is
 // slow: asked once for each device, kernel and cluster size.
-int resident_clusters(bool int8, bool gated, bool loose, int split)
+int resident_clusters(Form form, bool loose, int split)
 {
     static std::mutex mu;
-    static int known[64][8][kMaxSplit + 1];
+    static int known[64][2 * (kPair16 + 1)][kMaxSplit + 1];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     std::lock_guard<std::mutex> lock(mu);
-    int &n = known[dev][4 * int8 + 2 * gated + loose][split];
+    int &n = known[dev][2 * form + loose][split];
     if (n == 0) {
-        const void *func = kernel_of(int8, gated, loose);
+        const void *func = kernel_of(form, loose);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)split, 1, 1);
         cfg.blockDim = dim3(threads_of(loose), 1, 1);
@@ -488,14 +510,18 @@ struct StreamPlan {
 
 StreamPlan plan_stream(const Product &p)
 {
+    const Form form = form_of(p);
     const bool int8 = p.kind == kProductInt8, gated = p.form == Product::kGated, w_mn = p.b[0].mn_major;
     const int e = int8 ? 1 : 2, block_k = int8 ? 128 : 64, sums = gated ? 2 : 1;
     StreamPlan s = {};
     s.k_blocks = (int)((p.K + block_k - 1) / block_k);
     s.parts = p.form == Product::kSum ? 2 : 1;
+    const int problems = p.form == Product::kPair ? 2 : 1;
     s.tokens = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    if (problems > 1 && s.tokens < 64) s.tokens = 64;        // whole boxes of 64 columns
     s.halves = p.lo[0].p ? 2 : 1;
     s.loose = !(taken_as_is(p.a[0], e) && taken_as_is(p.a[1], e) && taken_as_is(p.b[0], e) && taken_as_is(p.b[1], e));
+    if ((s.loose || s.halves > 1) && problems > 1) return s;         // not built: the tile kernel's
     s.row_tiles = (p.N + kRows - 1) / kRows;
     s.token_tiles = (p.M + s.tokens - 1) / s.tokens;
     const int columns = s.halves * s.tokens, stage = sums * kWeightBytes + columns * 128, exchange = sums * columns * kRows * 4;
@@ -516,20 +542,22 @@ StreamPlan plan_stream(const Product &p)
     s.smem = fixed + (used > exchange ? used : exchange);
     // The split with the least rounds of clusters x stages that a CTA walks; six stages' worth of time go to a
     // CTA's start, the exchange and the epilogue.
-    const int64_t work = s.row_tiles * s.token_tiles;
+    const int64_t work = s.row_tiles * s.token_tiles * problems;
     const int blocks = s.k_blocks * s.parts;
     int64_t best = 0;
     for (int n = 1; n <= kMaxSplit && n <= blocks; ++n) {
-        const int fit = per_sm * resident_clusters(int8, gated, s.loose, n);
+        const int fit = per_sm * resident_clusters(form, s.loose, n);
         if (fit < 1) continue;
         const int64_t cost = (work + fit - 1) / fit * ((blocks + n - 1) / n + 6);
         if (s.split == 0 || cost < best) {
             s.split = n;
             best = cost;
             // a stage takes a CTA the time of its bytes at what an SM draws from L2 (110 KB/us two CTAs, 80 one; shifted
-            // stages 25), and all of them together no less than the weights at HBM's rate
-            const double stage_us = per_sm * stage / (s.loose ? 25e3 : per_sm == 2 ? 110e3 : 80e3);
-            const double walk = (double)((work + fit - 1) / fit) * ((double)((blocks + n - 1) / n) * stage_us + 1.5);
+            // stages 18), an epilogue of 128 tokens 5.5 us (gated 12) shared by the cluster, and all of them together
+            // no less than the weights at HBM's rate
+            const double stage_us = per_sm * stage / (s.loose ? 18e3 : per_sm == 2 ? 110e3 : 80e3);
+            const double finish = 1.0 + s.tokens / 128.0 * (gated ? 12.0 : 5.5) / n;
+            const double walk = (double)((work + fit - 1) / fit) * ((double)((blocks + n - 1) / n) * stage_us + finish);
             const double hbm = (double)p.N * (double)p.K * e * sums * s.parts / 6.0e6;
             s.us = 3.5 + (walk > hbm ? walk : hbm);
         }
@@ -542,7 +570,7 @@ StreamPlan plan_stream(const Product &p)
 double stream_estimate(const Product &p)
 {
     const StreamPlan s = plan_stream(p);
-    return s.split > 0 && s.row_tiles <= 65535 && s.token_tiles <= 65535 ? s.us : -1.0;
+    return s.split > 0 && s.row_tiles <= 65535 && s.token_tiles <= 32767 ? s.us : -1.0;
 }
 
 int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream)
@@ -551,7 +579,8 @@ int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream
     const int e = int8 ? 1 : 2;
     const StreamPlan plan = plan_stream(p);
     if (plan.split == 0) return LORDBA_ECUDA;
-    if (plan.row_tiles > 65535 || plan.token_tiles > 65535) return LORDBA_EUNSUPPORTED;
+    if (plan.row_tiles > 65535 || plan.token_tiles > 32767) return LORDBA_EUNSUPPORTED;
+    const bool t_mn = p.a[0].mn_major;
     StreamArgs a;
     std::memset(&a, 0, sizeof(a));
     a.f = f;
@@ -559,6 +588,7 @@ int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream
     a.parts = plan.parts;
     a.tokens = plan.tokens;
     a.halves = plan.halves;
+    a.token_tiles = (int)plan.token_tiles;
     a.stages = plan.stages;
     a.raw_stages = plan.raw_stages;
     a.split = plan.split;
@@ -571,7 +601,8 @@ int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream
         a.rt[2 + i] = Rows{static_cast<const uint8_t *>(ol.p), ol.ld * e, p.M, p.K * e};
         if (plan.loose) continue;
         if (ol.p && !encode_map(&a.t[2 + i], ol.p, p.M, p.K, ol.ld, e, a.tokens)) return LORDBA_ECUDA;
-        if (ot.p && !encode_map(&a.t[i], ot.p, p.M, p.K, ot.ld, e, a.tokens)) return LORDBA_ECUDA;
+        if (ot.p && !(t_mn ? encode_map(&a.t[i], ot.p, p.K, p.M, ot.ld, e, 64) : encode_map(&a.t[i], ot.p, p.M, p.K, ot.ld, e, a.tokens)))
+            return LORDBA_ECUDA;
         if (ow.p && !encode_map(&a.w[i], ow.p, w_rows, w_cols, ow.ld, e, w_mn ? 64 : kRows)) return LORDBA_ECUDA;
     }
     a.tmem_columns = 32;
@@ -579,11 +610,11 @@ int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream
     a.skip = test_skip_item();
     a.status = device_status_word();
     if (!a.status) return LORDBA_ECUDA;
-    a.idesc = instr_desc(int8, p.kind == kProductBf16, w_mn, false, kRows, a.halves * a.tokens);
+    a.idesc = instr_desc(int8, p.kind == kProductBf16, w_mn, t_mn, kRows, a.halves * a.tokens);
     LaunchRec rec;
     std::memset(&rec, 0, sizeof(rec));
-    rec.func = kernel_of(int8, gated, plan.loose);
-    rec.grid[0] = (unsigned)plan.split; rec.grid[1] = (unsigned)plan.row_tiles; rec.grid[2] = (unsigned)plan.token_tiles;
+    rec.func = kernel_of(form_of(p), plan.loose);
+    rec.grid[0] = (unsigned)plan.split; rec.grid[1] = (unsigned)plan.row_tiles; rec.grid[2] = (unsigned)plan.token_tiles * (p.form == Product::kPair ? 2u : 1u);
     rec.block = threads_of(plan.loose);
     rec.smem = (uint32_t)plan.smem;
     rec.cluster = (uint32_t)plan.split;

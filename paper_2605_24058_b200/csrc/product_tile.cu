@@ -426,16 +426,17 @@ int launch_tile(const TileArgs &args, cudaStream_t stream)
 
 }  // namespace
 
-// 0.285 us a stage (its MMAs at the clock under load), at least 2.7 us a tile (the epilogue), 7 us around them.
+// 0.285 us a stage (its MMAs at the clock under load), at least the epilogue's time a tile, 7 us around them.
 double tile_estimate(const Product &p)
 {
-    const bool gated = p.form == Product::kGated;
-    const int block_k = p.kind == kProductInt8 ? 128 : 64;
+    const bool gated = p.form == Product::kGated, int8 = p.kind == kProductInt8;
+    const int block_k = int8 ? 128 : 64;
     const double tiles = (double)((p.M + kTileM - 1) / kTileM) * (double)((p.N + (gated ? 127 : 255)) / (gated ? 128 : 256)) *
                          (p.form == Product::kPair ? 2 : 1);
     const double rounds = (double)(int64_t)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
     const double walk = 0.285 * (double)((p.K + block_k - 1) / block_k) * (p.form == Product::kSum ? 2 : 1);
-    return 7.0 + rounds * (walk > 2.7 ? walk : 2.7);
+    const double finish = 2.7 + (int8 ? 0.8 : 0.0) + (int8 && gated ? 0.7 : 0.0) + (p.add[0] ? 2.0 : 0.0) + (p.pre[0] ? 1.5 : 0.0);
+    return 7.0 + rounds * (walk > finish ? walk : finish);
 }
 
 int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)

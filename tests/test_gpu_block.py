@@ -285,7 +285,7 @@ def test_gated_forward_far_out(act, T):
 
 GRAD_SIZES = [  # T, d_in, d_hidden, pad, lead
     (1, 1, 1, 0, 0), (1, 512, 640, 0, 0), (2, 64, 128, 0, 0), (7, 100, 130, 0, 0), (16, 256, 1024, 8, 0), (33, 129, 257, 0, 1), (64, 512, 384, 0, 0),
-    (65, 72, 264, 0, 0), (128, 256, 256, 0, 0), (200, 333, 700, 3, 0), (333, 520, 1365, 0, 0), (700, 1024, 256, 0, 0)]
+    (65, 72, 264, 0, 0), (128, 256, 256, 0, 0), (200, 333, 700, 3, 0), (333, 520, 1365, 0, 0), (700, 1024, 256, 0, 0), (2500, 96, 200, 0, 0), (3000, 130, 72, 5, 0), (4097, 256, 130, 0, 0)]
 
 
 @pytest.mark.parametrize("T,d_in,d_hidden,pad,lead", GRAD_SIZES)
@@ -319,10 +319,12 @@ def test_gated_backward(T, d_in, d_hidden, pad, lead, dtype, act):
     close(dwu, du.T @ vx, terms * T * 2.0 ** -23 * (mu.T @ np.abs(vx)) + (eu + 0 * du).T @ np.abs(vx), dtype, "dw_up")
     for (buf, _), rows, cols in zip(bufs, (T, T, T, d_hidden, d_hidden), (d_hidden, d_hidden, d_in, d_in, d_in)):
         untouched(buf, rows, cols, pad, lead)
-    # the parts alone give the same bits
-    only = lordba.gated_backward(dh, gate, up, None, wg, wu, act=act)
+    # the parts alone give the same bits (into buffers of the same layout: another one may take another kernel)
+    again = lambda rows, cols: target(rows, cols, dtype, pad, lead)[1]
+    only = lordba.gated_backward(dh, gate, up, None, wg, wu, again(T, d_hidden), again(T, d_hidden), again(T, d_in), act=act)
     assert only[3] is None and torch.equal(only[0], dgate) and torch.equal(only[1], dup) and torch.equal(only[2], dx)
-    only = lordba.gated_backward(dh, gate, up, x, act=act)
+    only = lordba.gated_backward(dh, gate, up, x, None, None, again(T, d_hidden), again(T, d_hidden), None, again(d_hidden, d_in),
+                                 again(d_hidden, d_in), act=act)
     assert only[2] is None and torch.equal(only[3], dwg) and torch.equal(only[4], dwu)
 
 
