@@ -36,6 +36,18 @@ bool encode_map(CUtensorMap *map, const void *p, int64_t rows, int64_t cols, int
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_store_map(CUtensorMap *map, void *p, int64_t rows, int64_t cols, int64_t ld, int e)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * e};
+    const cuuint32_t box[2] = {(cuuint32_t)(64 / e), 32}, step[2] = {1, 1};
+    return fn(map, e == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, p, dims, strides, box, step,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int sm_count()
 {
     static std::mutex mu;
@@ -107,10 +119,10 @@ bool rows_vec(const void *p, int64_t ld, size_t e) { return aligned(p, 16) && ((
 
 size_t product_workspace_bytes(const Product &p)
 {
+    const Way way = way_of(p);
     size_t n = 0;
-    if (!way_of(p).copy) return 0;
-    for (int i = 0; i < 2; ++i) n += packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + packed_bytes(p.b[i], p.N, p.K, elt_of(p));
-    return n;
+    for (int i = 0; way.copy && i < 2; ++i) n += packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + packed_bytes(p.b[i], p.N, p.K, elt_of(p));
+    return n + (way.stream ? stream_workspace_bytes(way.copy ? copied_form(p) : p) : 0);
 }
 
 int launch_product(const Product &given, void *workspace, cudaStream_t stream)
@@ -144,7 +156,7 @@ int launch_product(const Product &given, void *workspace, cudaStream_t stream)
     f.vec_add = rows_vec(p.add[0], p.ld_add, eo) && aligned(p.add[1], 16);
     f.vec_pre = rows_vec(p.pre[0], p.ld_pre, eo) && aligned(p.pre[1], 16);
     f.vec_scale = aligned(p.s_col[0], 16) && aligned(p.s_col[1], 16);
-    if (way.stream) return launch_product_stream(p, f, stream);
+    if (way.stream) return launch_product_stream(p, f, next, stream);
     return launch_product_tile(p, f, stream);
 }
 

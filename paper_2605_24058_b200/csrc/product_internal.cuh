@@ -26,11 +26,14 @@ inline bool taken_as_is(const Operand &o, int e) { return !o.p || (aligned(o.p, 
 double stream_estimate(const Product &p);
 double tile_estimate(const Product &p);
 int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream);     // product_tile.cu
-int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream);   // product_stream.cu
+size_t stream_workspace_bytes(const Product &p);                                     // product_stream.cu
+int launch_product_stream(const Product &p, const Finish &f, void *workspace, cudaStream_t stream);
 
 // Encode a map of the row-major rows x cols matrix (pitch ld elements of e bytes) read in boxes of box_rows
 // rows of 128 bytes, 128-byte swizzled; what lies outside the matrix reads as zero.
 bool encode_map(CUtensorMap *map, const void *p, int64_t rows, int64_t cols, int64_t ld, int e, int box_rows);
+// The same for writing boxes of 32 rows of 64 bytes, 64-byte swizzled (e = 2 or 4).
+bool encode_store_map(CUtensorMap *map, void *p, int64_t rows, int64_t cols, int64_t ld, int e);
 
 int sm_count();      // of the current device
 

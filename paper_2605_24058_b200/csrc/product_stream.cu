@@ -17,6 +17,7 @@
 // Operands whose base or pitch is not a multiple of 16 bytes are out of the copy engine's reach.  Copying
 // them first would move each weight three times; instead (LOOSE) warps 0-3 and 6-9 fetch the aligned pieces
 // that hold a stage into a second ring, several stages ahead (cp.async), and shift them into place.
+#include <atomic>
 #include <cstring>
 #include <mutex>
 
@@ -48,6 +49,10 @@ struct StreamArgs {
     int tokens;              // of a tile: a multiple of 16
     int halves;              // 2: the tokens' entries come as two terms, each term MMA columns of its own
     int token_tiles;         // of one problem (T_MN: two problems, with the tokens t[0] and t[1])
+    int problems;
+    int groups;              // more than 1: so many clusters share a tile's contraction and write their sums to
+    uint32_t *raw;           // raw, [group][problem or gate, up][M][raw_ld], for finish_kernel to add
+    int64_t raw_ld;          // N rounded up to 4
     int stages, split;
     int raw_stages;          // LOOSE: stages fetched ahead (2 ... 6)
     int tmem_columns;
@@ -219,10 +224,12 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
     constexpr int kHalves = W_MN && !T_MN ? 2 : 1;                // at most
     const int halves = kHalves > 1 ? P.halves : 1, columns = halves * P.tokens;
     const int stage_bytes = kSums * kWeightBytes + columns * 128;
-    const int problem = T_MN && (int)blockIdx.z >= P.token_tiles ? 1 : 0;
-    const int n0 = blockIdx.y * kRows, t0 = ((int)blockIdx.z - problem * P.token_tiles) * P.tokens;
+    const int z = (int)blockIdx.z / P.token_tiles;
+    const int t0 = ((int)blockIdx.z - z * P.token_tiles) * P.tokens, n0 = blockIdx.y * kRows;
+    const int group = z / P.problems, problem = z - group * P.problems;
     const int blocks = P.k_blocks * P.parts;
-    const int first = (int)((int64_t)blocks * rank / P.split), last = (int)((int64_t)blocks * (rank + 1) / P.split);
+    const int slice = group * P.split + rank, slices = P.groups * P.split;
+    const int first = (int)((int64_t)blocks * slice / slices), last = (int)((int64_t)blocks * (slice + 1) / slices);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < P.stages; ++s) {
@@ -432,6 +439,14 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
                     if (it + k * step >= items) break;
+                    if (P.groups > 1) {
+                        const int64_t row = t0 + (it + k * step) / (kRows / 4);
+#pragma unroll
+                        for (int c = 0; c < kSums; ++c)
+                            *reinterpret_cast<uint4 *>(P.raw + (((int64_t)group * (GATED ? 2 : P.problems) + (GATED ? c : problem)) * P.f.M + row) *
+                                                                   P.raw_ld + n0 + j) = acc[k][c];
+                        continue;
+                    }
                     const uint32_t g[4] = {acc[k][0].x, acc[k][0].y, acc[k][0].z, acc[k][0].w};
                     const uint4 w = acc[k][GATED ? 1 : 0];
                     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -442,6 +457,32 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
     if (P.split > 1) {
         __syncwarp();
         cluster_sync();         // the sums stay until every CTA has read them
+    }
+}
+
+// Adds what the groups of a product left in raw, in group order, and finishes.  A thread: four columns of a row.
+template <bool INT8, bool GATED>
+__global__ void __launch_bounds__(256)
+finish_kernel(const __grid_constant__ Finish F, const uint32_t *__restrict__ raw, int64_t ld, int groups, int problems)
+{
+    const int64_t n = 4 * ((int64_t)blockIdx.x * 64 + threadIdx.x % 64);
+    const int planes = GATED ? 2 : problems, problem = GATED ? 0 : blockIdx.z;
+    grid_wait();
+    grid_release();
+    if (n >= F.N) return;
+    for (int64_t m = (int64_t)blockIdx.y * 4 + threadIdx.x / 64; m < F.M; m += (int64_t)gridDim.y * 4) {
+        uint4 acc[2];
+#pragma unroll
+        for (int c = 0; c < (GATED ? 2 : 1); ++c) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(raw + ((GATED ? c : problem) * F.M + m) * ld + n);
+            const int64_t next = planes * F.M * ld / 4;
+            acc[c] = __ldcs(p);
+#pragma unroll 4
+            for (int g = 1; g < groups; ++g) acc[c] = add4<INT8>(acc[c], __ldcs(p + g * next));
+        }
+        const uint4 w = acc[GATED ? 1 : 0];
+        const uint32_t g[4] = {acc[0].x, acc[0].y, acc[0].z, acc[0].w}, u[4] = {w.x, w.y, w.z, w.w};
+        finish4<INT8, GATED>(F, problem, m, n, g, u);
     }
 }
 
@@ -469,20 +510,28 @@ const void *kernel_of(Form form, bool loose)
     }
 }
 
-// Clusters of `split` CTAs, one CTA an SM, that fit the device at once (0: the query failed).  For a kernel
-// that allocates TMEM the query never counts more than one CTA an SM, whatever its size; two of this kernel's
-// were seen to run side by side where its shared memory allows it, so the caller multiplies.  The query is
-// slow: asked once for each device, kernel and cluster size.
-int resident_clusters(Form form, bool loose, int split)
+// Clusters of 1 ... 8 CTAs, one CTA an SM, that fit the device at once ([split]; 0: the query failed).  For a
+// kernel that allocates TMEM the query never counts more than one CTA an SM, whatever its size; two of this
+// kernel's were seen to run side by side where its shared memory allows it, so the caller multiplies.  The query
+// is slow: asked once for each device and kernel.
+struct Resident {
+    int clusters[kMaxSplit + 1];
+};
+
+const Resident *resident(Form form, bool loose)
 {
     static std::mutex mu;
-    static int known[64][2 * (kPair16 + 1)][kMaxSplit + 1];
+    static Resident known[64][2 * (kPair16 + 1)];
+    static std::atomic<bool> asked[64][2 * (kPair16 + 1)];
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    Resident &r = known[dev][2 * form + loose];
+    std::atomic<bool> &done = asked[dev][2 * form + loose];
+    if (done.load(std::memory_order_acquire)) return &r;
     std::lock_guard<std::mutex> lock(mu);
-    int &n = known[dev][2 * form + loose][split];
-    if (n == 0) {
-        const void *func = kernel_of(form, loose);
+    if (done.load(std::memory_order_relaxed)) return &r;
+    const void *func = kernel_of(form, loose);
+    for (int split = 1; split <= kMaxSplit; ++split) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)split, 1, 1);
         cfg.blockDim = dim3(threads_of(loose), 1, 1);
@@ -493,18 +542,20 @@ int resident_clusters(Form form, bool loose, int split)
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
         if (cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, kWhole) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, func, &cfg) != cudaSuccess) {
+            cudaOccupancyMaxActiveClusters(&r.clusters[split], func, &cfg) != cudaSuccess) {
             cudaGetLastError();
-            n = 0;
+            r.clusters[split] = 0;
         }
     }
-    return n;
+    done.store(true, std::memory_order_release);
+    return &r;
 }
 
 struct StreamPlan {
     bool loose;
-    int tokens, halves, k_blocks, parts, stages, raw_stages, split, smem;
+    int tokens, halves, k_blocks, parts, stages, raw_stages, split, groups, smem;
     int64_t row_tiles, token_tiles;
+    size_t raw_bytes;      // of the sums that groups leave
     double us;             // estimate
 };
 
@@ -540,28 +591,32 @@ StreamPlan plan_stream(const Product &p)
         used = s.stages * stage;
     }
     s.smem = fixed + (used > exchange ? used : exchange);
-    // The split with the least rounds of clusters x stages that a CTA walks; six stages' worth of time go to a
-    // CTA's start, the exchange and the epilogue.
+    // The split over a cluster, and over clusters, that takes the least time.  A stage takes a CTA the time of its
+    // bytes at what an SM draws from L2 (110 KB/us two CTAs, 80 one; shifted stages 18); an epilogue of 128 tokens
+    // 5.5 us (gated 12), shared by the cluster; all together no less than the weights at HBM's rate.  Groups write
+    // their sums and another kernel reads them.
     const int64_t work = s.row_tiles * s.token_tiles * problems;
     const int blocks = s.k_blocks * s.parts;
-    int64_t best = 0;
-    for (int n = 1; n <= kMaxSplit && n <= blocks; ++n) {
-        const int fit = per_sm * resident_clusters(form, s.loose, n);
+    const double stage_us = per_sm * stage / (s.loose ? 18e3 : per_sm == 2 ? 110e3 : 80e3);
+    const double hbm = (double)p.N * (double)p.K * e * sums * s.parts / 6.0e6;
+    const double plane = (double)p.M * (double)((p.N + 3) / 4 * 16) * sums * problems;       // bytes of a group's sums
+    const Resident *res = resident(form, s.loose);
+    for (int n = 1; res && n <= kMaxSplit && n <= blocks; ++n) {
+        const int fit = per_sm * res->clusters[n];
         if (fit < 1) continue;
-        const int64_t cost = (work + fit - 1) / fit * ((blocks + n - 1) / n + 6);
-        if (s.split == 0 || cost < best) {
-            s.split = n;
-            best = cost;
-            // a stage takes a CTA the time of its bytes at what an SM draws from L2 (110 KB/us two CTAs, 80 one; shifted
-            // stages 18), an epilogue of 128 tokens 5.5 us (gated 12) shared by the cluster, and all of them together
-            // no less than the weights at HBM's rate
-            const double stage_us = per_sm * stage / (s.loose ? 18e3 : per_sm == 2 ? 110e3 : 80e3);
-            const double finish = 1.0 + s.tokens / 128.0 * (gated ? 12.0 : 5.5) / n;
-            const double walk = (double)((work + fit - 1) / fit) * ((double)((blocks + n - 1) / n) * stage_us + finish);
-            const double hbm = (double)p.N * (double)p.K * e * sums * s.parts / 6.0e6;
-            s.us = 3.5 + (walk > hbm ? walk : hbm);
+        for (int g = 1; g <= 16 && n * g * (g > 1 ? 4 : 1) <= blocks && (g == 1 || g * plane < 64e6); g *= 2) {
+            const double rounds = (double)((work * g + fit - 1) / fit), steps = (double)((blocks + n * g - 1) / (n * g));
+            const double finish = 1.0 + s.tokens / 128.0 * (g > 1 ? 3.0 * sums : gated ? 12.0 : 5.5) / n;
+            const double walk = rounds * (steps * stage_us + finish);
+            const double us = 3.5 + (walk > hbm ? walk : hbm) + (g > 1 ? 4.0 + 2 * g * plane / 4.0e6 : 0.0);
+            if (s.split == 0 || us < s.us * (g > 1 ? 0.9 : 1.0)) {
+                s.split = n;
+                s.groups = g;
+                s.us = us;
+            }
         }
     }
+    s.raw_bytes = s.groups > 1 ? (size_t)s.groups * (size_t)plane : 0;
     return s;
 }
 
@@ -570,16 +625,18 @@ StreamPlan plan_stream(const Product &p)
 double stream_estimate(const Product &p)
 {
     const StreamPlan s = plan_stream(p);
-    return s.split > 0 && s.row_tiles <= 65535 && s.token_tiles <= 32767 ? s.us : -1.0;
+    return s.split > 0 && s.row_tiles <= 65535 && s.token_tiles <= 65535 / 32 ? s.us : -1.0;
 }
 
-int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream)
+size_t stream_workspace_bytes(const Product &p) { return plan_stream(p).raw_bytes; }
+
+int launch_product_stream(const Product &p, const Finish &f, void *workspace, cudaStream_t stream)
 {
     const bool int8 = p.kind == kProductInt8, gated = p.form == Product::kGated, w_mn = p.b[0].mn_major;
     const int e = int8 ? 1 : 2;
     const StreamPlan plan = plan_stream(p);
     if (plan.split == 0) return LORDBA_ECUDA;
-    if (plan.row_tiles > 65535 || plan.token_tiles > 32767) return LORDBA_EUNSUPPORTED;
+    if (plan.row_tiles > 65535 || plan.token_tiles > 65535 / 32) return LORDBA_EUNSUPPORTED;
     const bool t_mn = p.a[0].mn_major;
     StreamArgs a;
     std::memset(&a, 0, sizeof(a));
@@ -589,6 +646,10 @@ int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream
     a.tokens = plan.tokens;
     a.halves = plan.halves;
     a.token_tiles = (int)plan.token_tiles;
+    a.problems = p.form == Product::kPair ? 2 : 1;
+    a.groups = plan.groups;
+    a.raw = static_cast<uint32_t *>(workspace);
+    a.raw_ld = (p.N + 3) / 4 * 4;
     a.stages = plan.stages;
     a.raw_stages = plan.raw_stages;
     a.split = plan.split;
@@ -614,14 +675,20 @@ int launch_product_stream(const Product &p, const Finish &f, cudaStream_t stream
     LaunchRec rec;
     std::memset(&rec, 0, sizeof(rec));
     rec.func = kernel_of(form_of(p), plan.loose);
-    rec.grid[0] = (unsigned)plan.split; rec.grid[1] = (unsigned)plan.row_tiles; rec.grid[2] = (unsigned)plan.token_tiles * (p.form == Product::kPair ? 2u : 1u);
+    rec.grid[0] = (unsigned)plan.split; rec.grid[1] = (unsigned)plan.row_tiles; rec.grid[2] = (unsigned)(plan.token_tiles * a.problems * plan.groups);
     rec.block = threads_of(plan.loose);
     rec.smem = (uint32_t)plan.smem;
     rec.cluster = (uint32_t)plan.split;
     rec.pdl = 1;
     rec.n_args = 1;
     rec.arg_bytes[0] = sizeof(StreamArgs);
-    return launch_record(rec, &a, nullptr, stream);
+    const int rc = launch_record(rec, &a, nullptr, stream);
+    if (rc != LORDBA_OK || plan.groups == 1) return rc;
+    const int64_t gx = (p.N + 255) / 256, gy = (p.M + 3) / 4, most = gx >= 148 * 32 ? 1 : 148 * 32 / gx;
+    const dim3 grid((unsigned)gx, (unsigned)(gy < most ? gy : most), (unsigned)a.problems);
+    const auto kernel = int8 ? (gated ? finish_kernel<true, true> : finish_kernel<true, false>)
+                             : (gated ? finish_kernel<false, true> : finish_kernel<false, false>);
+    return launch_kernel(kernel, grid, 256, 0, stream, f, static_cast<const uint32_t *>(a.raw), a.raw_ld, plan.groups, a.problems);
 }
 
 }  // namespace lordba

@@ -39,14 +39,12 @@ constexpr int kEpiWarps = 8;
 constexpr int kTileThreads = (4 + kEpiWarps) * 32;
 constexpr int kBarBytes = (2 * kStages + 4) * 8 + 16;
 constexpr int kCh = 32;                            // columns of an epilogue step
-constexpr int kPieces = kCh / 8;                   // 16-byte pieces of a row of them, 16-bit
-constexpr int kDown = 32 / kPieces;                // rows of one access of a warp
-constexpr int kPatchPitch = 2 * kCh + 16;          // a warp's patch: 32 rows, padded against bank conflicts
-constexpr int kPatchBytes = 32 * kPatchPitch;
-constexpr int kTileSmem = kStages * kStageBytes + kEpiWarps * kPatchBytes + kBarBytes + 1024;
+constexpr int kPatchBytes = 32 * 64;               // 32 rows of 64 bytes on their way to memory; two for each warp
+constexpr int kTileSmem = kStages * kStageBytes + 2 * kEpiWarps * kPatchBytes + kBarBytes + 1024;
 
 struct TileArgs {
     CUtensorMap a[4], b[2];      // of two problems, the second one's A (and rest of A) are a[1] (and a[3])
+    CUtensorMap out[2], pre[2];  // where rows start on 16-byte boundaries
     Finish f;
     int k_blocks;          // stages per operand pair
     int parts;             // operand pairs summed into one accumulator
@@ -73,110 +71,119 @@ __device__ __forceinline__ Tile tile_at(const TileArgs &P, int i)
     return t;
 }
 
-// ---- epilogue: a warp's 32 rows x kCh columns of a matrix ---------------------------------------------------------
-// TMEM gives a lane a row; memory wants neighbouring lanes on neighbouring columns.  A patch of shared memory
-// turns one into the other; the warp alone uses it.
+// ---- epilogue: a warp's 32 rows x 64 bytes of a matrix -----------------------------------------------------------
+// TMEM gives a lane a row.  A lane reads the addends of its row itself; results go through a patch of shared memory,
+// from which the copy engine writes them (64-byte swizzled: the lanes' rows do not meet in a bank).  Rows that
+// it cannot take are written element by element.  What is rare stays out of line: where a CTA has one tile,
+// fetching instructions is a good part of its time.
+__device__ __noinline__ uint4 fetch_part(const uint8_t *q, int64_t left)
+{
+    return left > 0 ? load_bytes16<false>(reinterpret_cast<uintptr_t>(q), reinterpret_cast<uintptr_t>(q) + 2 * left) : make_uint4(0, 0, 0, 0);
+}
 
-// Where a lane reads or writes a matrix: kPieces rows, kDown apart, from a column on.
-struct Place {
-    uint8_t *p;            // the first row's piece
-    int64_t down;          // bytes to the next row
-    int vec;               // rows start on 16-byte boundaries
-    __device__ __forceinline__ Place(const void *base, int64_t ld, int e, int vec_, int64_t row, int64_t col)
-        : p(static_cast<uint8_t *>(const_cast<void *>(base)) + (row * ld + col) * e), down(kDown * ld * e), vec(vec_)
+// 32 columns of 16 bits, `left` of which exist
+__device__ __forceinline__ void fetch(uint4 x[4], const uint8_t *q, int vec, int64_t left)
+{
+    if (vec && left >= 32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4 *>(q + 16 * i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = fetch_part(q + 16 * i, left - 8 * i);
+    }
+}
+
+__device__ __forceinline__ void add(const uint4 x[4], float v[32], int dtype)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = unpack2_any(w[j], dtype);
+            v[8 * i + 2 * j] += f.x;
+            v[8 * i + 2 * j + 1] += f.y;
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t patch_piece(uint32_t patch, int row, int i) { return patch + 64 * row + 16 * (i ^ (row >> 1 & 3)); }
+
+// rows x left elements of e bytes from a patch to q (row pitch ld bytes), whatever the alignment
+__device__ __noinline__ void put_elements(uint32_t patch, uint8_t *q, int64_t ld, int rows, int64_t left, int e)
+{
+    const int lane = threadIdx.x % 32, per = 64 / e;
+    const int n = left < per ? (int)left : per;
+#pragma unroll 1
+    for (int i = lane; i < rows * per; i += 32) {
+        const int r = i / per, c = i % per;
+        if (c >= n) continue;
+        const uint32_t at = patch_piece(patch, r, c * e / 16) + c * e % 16;
+        if (e == 4) {
+            uint32_t v;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+            reinterpret_cast<uint32_t *>(q + r * ld)[c] = v;
+        } else {
+            uint16_t v;
+            asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+            reinterpret_cast<uint16_t *>(q + r * ld)[c] = v;
+        }
+    }
+}
+
+// A matrix that results go to.
+struct Target {
+    const CUtensorMap *map;
+    void *p;
+    int64_t ld;
+    int vec, e;
+};
+
+struct Patches {
+    uint32_t base;
+    int which = 0;
+
+    // sixteen words of the lane's row m0 + lane, from column n on
+    __device__ __forceinline__ void put(const uint32_t w[16], const Target &t, int64_t m0, int64_t n, int rows, int64_t left, int lane)
     {
+        const uint32_t patch = base + which * kPatchBytes;
+        which ^= 1;
+        if (lane == 0) stores_read_but_one();          // what went out of this patch has left it
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store_shared_v4(patch_piece(patch, lane, i), make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+        fence_proxy_async();
+        __syncwarp();
+        if (t.vec) {
+            if (lane == 0) store_tile(t.map, patch, (int)n, (int)m0);
+        } else {
+            put_elements(patch, static_cast<uint8_t *>(t.p) + (m0 * t.ld + n) * t.e, t.ld * t.e, rows, left, t.e);
+            __syncwarp();
+        }
+    }
+    // 32 values, in the target's type
+    __device__ __forceinline__ void put32(const float v[32], const Target &t, int64_t m0, int64_t n, int rows, int64_t left, int lane, int dtype)
+    {
+        uint32_t w[16];
+        if (t.e == 4) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (left <= 16 * h) break;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * h + i]);
+                put(w, t, m0, n + 16 * h, rows, left - 16 * h, lane);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack2_any(v[2 * i], v[2 * i + 1], dtype);
+            put(w, t, m0, n, rows, left, lane);
+        }
     }
 };
 
-struct Patch {
-    uint32_t mine, shared;      // a lane's row; its place among the rows of an access
-    int row, piece;
-
-    __device__ __forceinline__ Patch(uint32_t base, int lane)
-        : mine(base + lane * kPatchPitch), shared(base + (lane / kPieces) * kPatchPitch + 16 * (lane % kPieces)), row(lane / kPieces),
-          piece(lane % kPieces)
-    {
-    }
-    // fetch: kCh 16-bit columns, `at` bytes on; rows: how many of the warp's exist; left: columns from this lane's
-    // piece to the end of the row
-    __device__ __forceinline__ void fetch(uint4 x[kPieces], const Place &w, int at, int rows, int64_t left) const
-    {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const uint8_t *q = w.p + at + i * w.down;
-            x[i] = make_uint4(0, 0, 0, 0);
-            if (row + kDown * i < rows && left > 0) {
-                if (w.vec && left >= 8) x[i] = *reinterpret_cast<const uint4 *>(q);
-                else x[i] = load_bytes16<false>(reinterpret_cast<uintptr_t>(q), reinterpret_cast<uintptr_t>(q) + 2 * left);
-            }
-        }
-    }
-    // add: what the lanes fetched, to the columns of the lane's own row
-    __device__ __forceinline__ void add(const uint4 x[kPieces], float v[kCh], int dtype) const
-    {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) store_shared_v4(shared + kDown * i * kPatchPitch, x[i]);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const uint4 y = load_shared_v4(mine + 16 * i);
-            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 f = unpack2_any(w[j], dtype);
-                v[8 * i + 2 * j] += f.x;
-                v[8 * i + 2 * j + 1] += f.y;
-            }
-        }
-        __syncwarp();
-    }
-    // put: the words of the lane's own row, in pieces of `count` elements
-    __device__ __forceinline__ void put(const uint32_t w[4 * kPieces], const Place &to, int at, int rows, int64_t left, int count) const
-    {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) store_shared_v4(mine + 16 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const uint4 x = load_shared_v4(shared + kDown * i * kPatchPitch);
-            uint8_t *q = to.p + at + i * to.down;
-            if (row + kDown * i >= rows || left <= 0) continue;
-            if (to.vec && left >= count) {
-                *reinterpret_cast<uint4 *>(q) = x;
-            } else {
-                const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (j >= left || j >= count) break;
-                    if (count == 4) { if (j < 4) reinterpret_cast<uint32_t *>(q)[j] = y[j % 4]; }
-                    else reinterpret_cast<uint16_t *>(q)[j] = (uint16_t)(y[j / 2] >> 16 * (j % 2));
-                }
-            }
-        }
-        __syncwarp();
-    }
-    // kCh values as 16-bit elements
-    __device__ __forceinline__ void put16(const float v[kCh], const Place &to, int at, int rows, int64_t left, int dtype) const
-    {
-        uint32_t w[kCh / 2];
-#pragma unroll
-        for (int i = 0; i < kCh / 2; ++i) w[i] = pack2_any(v[2 * i], v[2 * i + 1], dtype);
-        put(w, to, at, rows, left, 8);
-    }
-    // kCh values as floats
-    __device__ __forceinline__ void put32(const float v[kCh], const Place &to, int at, int rows, int64_t left) const
-    {
-        uint32_t w[kCh / 2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int i = 0; i < kCh / 2; ++i) w[i] = __float_as_uint(v[h * kCh / 2 + i]);
-            put(w, to, at + 2 * kCh * h, rows, left - kCh / 2 * h, 4);
-        }
-    }
-};
-
-template <bool INT8, bool GATED, bool A_MN, bool B_MN>
+// DT: type of the outputs and addends (known here: with a choice at each element the epilogue takes a third more
+// instructions).
+template <bool INT8, bool GATED, bool A_MN, bool B_MN, int DT>
 __global__ void __launch_bounds__(kTileThreads, 1)
 product_tile_kernel(const __grid_constant__ TileArgs P)
 {
@@ -184,7 +191,7 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
     constexpr int kTileN = GATED ? 128 : 256;        // columns of the output
     constexpr int kBlockK = INT8 ? 128 : 64;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t patches = base + kStages * kStageBytes, bars = patches + kEpiWarps * kPatchBytes;
+    const uint32_t patches = base + kStages * kStageBytes, bars = patches + 2 * kEpiWarps * kPatchBytes;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (kStages + s); };
     auto sum_full = [&](int b) { return bars + 8u * (2 * kStages + b); };
@@ -300,7 +307,7 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
         const int quadrant = warp % 4, group = share ? 0 : (warp - 4) / (kEpiWarps / 2);
         const int parts = share ? kEpiWarps / 4 : kEpiWarps / 8, part = (warp - 4) / 4 % parts;
         const int cols = kTileN / parts;                       // of one warp
-        const Patch patch(patches + (warp - 4) * kPatchBytes, lane);
+        Patches patch{patches + (warp - 4) * 2 * kPatchBytes};
         const bool adds = GATED && P.f.add[0];
         const int buf = group;
         uint32_t buf_phase = 0;
@@ -311,15 +318,13 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
             const int64_t n0 = (int64_t)t.n * kTileN + cols * part;
             const int64_t m = m0 + lane < P.f.M ? m0 + lane : 0;
             const int rows = P.f.M - m0 < 32 ? (int)(P.f.M - m0) : 32;          // of the warp's that exist (<= 0: none)
-            const int64_t row = m0 + patch.row, col = n0 + 8 * patch.piece;
-            const bool wide = P.f.dtype == LORDBA_F32;
-            const Place out(P.f.out[t.problem], P.f.ldo, wide ? 4 : 2, P.f.vec_out, row, wide ? n0 + 4 * patch.piece : col);
-            const Place pre0(P.f.pre[0], P.f.ld_pre, 2, P.f.vec_pre, row, col), pre1(P.f.pre[1], P.f.ld_pre, 2, P.f.vec_pre, row, col);
-            const Place add0(P.f.add[0], P.f.ld_add, 2, P.f.vec_add, row, col), add1(P.f.add[1], P.f.ld_add, 2, P.f.vec_add, row, col);
-            uint4 xg[kPieces], xu[kPieces];                    // the addends, fetched a step ahead
+            const Target out{&P.out[t.problem], P.f.out[t.problem], P.f.ldo, P.f.vec_out, DT == LORDBA_F32 ? 4 : 2};
+            const uint8_t *add0 = static_cast<const uint8_t *>(P.f.add[0]) + 2 * (m * P.f.ld_add + n0);
+            const uint8_t *add1 = static_cast<const uint8_t *>(P.f.add[1]) + 2 * (m * P.f.ld_add + n0);
+            uint4 xg[4], xu[4];                                // the addends, fetched a step ahead
             if (adds) {
-                patch.fetch(xg, add0, 0, rows, P.f.N - col);
-                patch.fetch(xu, add1, 0, rows, P.f.N - col);
+                fetch(xg, add0, P.f.vec_add, P.f.N - n0);
+                fetch(xu, add1, P.f.vec_add, P.f.N - n0);
             }
             alive = __all_sync(0xffffffffu, bound.wait(sum_full(buf), buf_phase, kDevEpilogueWaitTimeout));
             if (!alive) break;
@@ -327,8 +332,8 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
             const uint32_t d = tmem + ((uint32_t)(32 * quadrant) << 16) + 256u * buf + cols * part;
 #pragma unroll 1
             for (int c = 0; c < cols; c += kCh) {
-                const int64_t n = n0 + c, left = P.f.N - col - c;
-                if (rows <= 0 || n >= P.f.N) break;            // the warp's rows or columns lie outside
+                const int64_t n = n0 + c, left = P.f.N - n;
+                if (rows <= 0 || left <= 0) break;             // the warp's rows or columns lie outside
                 uint32_t g[kCh], u[kCh];
 #pragma unroll
                 for (int k = 0; k < kCh; k += 16) {
@@ -337,30 +342,30 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
                 }
                 float v[kCh], w[kCh];
                 tmem_wait_load();
-                products_of<INT8, GATED, kCh>(P.f, m, n, (int)(P.f.N - n < kCh ? P.f.N - n : kCh), g, u, v, w);
+                products_of<INT8, GATED, kCh>(P.f, m, n, (int)(left < kCh ? left : kCh), g, u, v, w);
                 if (GATED) {
                     if (adds) {
-                        patch.add(xg, v, P.f.dtype);
-                        patch.add(xu, w, P.f.dtype);
+                        add(xg, v, DT);
+                        add(xu, w, DT);
                         if (c + kCh < cols) {
-                            patch.fetch(xg, add0, 2 * (c + kCh), rows, left - kCh);
-                            patch.fetch(xu, add1, 2 * (c + kCh), rows, left - kCh);
+                            fetch(xg, add0 + 2 * (c + kCh), P.f.vec_add, left - kCh);
+                            fetch(xu, add1 + 2 * (c + kCh), P.f.vec_add, left - kCh);
                         }
                     }
                     if (P.f.pre[0]) {
-                        patch.put16(v, pre0, 2 * c, rows, left, P.f.dtype);
-                        patch.put16(w, pre1, 2 * c, rows, left, P.f.dtype);
+                        patch.put32(v, Target{&P.pre[0], P.f.pre[0], P.f.ld_pre, P.f.vec_pre, 2}, m0, n, rows, left, lane, DT);
+                        patch.put32(w, Target{&P.pre[1], P.f.pre[1], P.f.ld_pre, P.f.vec_pre, 2}, m0, n, rows, left, lane, DT);
                     }
                     gate<kCh>(P.f.act, v, w);
                 }
-                if (wide) patch.put32(v, out, 4 * c, rows, P.f.N - n - 4 * patch.piece);
-                else patch.put16(v, out, 2 * c, rows, left, P.f.dtype);
+                patch.put32(v, out, m0, n, rows, left, lane, DT);
             }
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive_cluster(peer_addr(sum_empty(buf), 0));
             buf_phase ^= 1u;
         }
+        if (lane == 0) stores_complete();
     }
 
     if (*abort_flag) {
@@ -378,10 +383,10 @@ product_tile_kernel(const __grid_constant__ TileArgs P)
     }
 }
 
-template <bool INT8, bool GATED, bool A_MN, bool B_MN>
+template <bool INT8, bool GATED, bool A_MN, bool B_MN, int DT>
 int launch_tile(const TileArgs &args, cudaStream_t stream)
 {
-    const void *func = reinterpret_cast<const void *>(&product_tile_kernel<INT8, GATED, A_MN, B_MN>);
+    const void *func = reinterpret_cast<const void *>(&product_tile_kernel<INT8, GATED, A_MN, B_MN, DT>);
     // co-resident pairs, asked for once a device: the query is slow
     static std::mutex mu;
     static int pairs_of[64] = {0};
@@ -424,9 +429,19 @@ int launch_tile(const TileArgs &args, cudaStream_t stream)
     return launch_record(rec, &args, nullptr, stream);
 }
 
+template <int DT>
+int launch_typed(const TileArgs &a, bool int8, bool gated, bool pair, cudaStream_t stream)
+{
+    if (int8) return gated ? launch_tile<true, true, false, false, DT>(a, stream) : launch_tile<true, false, false, false, DT>(a, stream);
+    if (gated) return launch_tile<false, true, false, false, DT>(a, stream);
+    if (pair) return launch_tile<false, false, true, true, DT>(a, stream);
+    return launch_tile<false, false, false, true, DT>(a, stream);
+}
+
 }  // namespace
 
-// 0.285 us a stage (its MMAs at the clock under load), at least the epilogue's time a tile, 7 us around them.
+// 0.285 us a stage (its MMAs at the clock under load) or the epilogue's time, whichever is longer, a round of tiles;
+// the last round's epilogue shows; 7 us around them.
 double tile_estimate(const Product &p)
 {
     const bool gated = p.form == Product::kGated, int8 = p.kind == kProductInt8;
@@ -435,8 +450,8 @@ double tile_estimate(const Product &p)
                          (p.form == Product::kPair ? 2 : 1);
     const double rounds = (double)(int64_t)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
     const double walk = 0.285 * (double)((p.K + block_k - 1) / block_k) * (p.form == Product::kSum ? 2 : 1);
-    const double finish = 2.7 + (int8 ? 0.8 : 0.0) + (int8 && gated ? 0.7 : 0.0) + (p.add[0] ? 2.0 : 0.0) + (p.pre[0] ? 1.5 : 0.0);
-    return 7.0 + rounds * (walk > finish ? walk : finish);
+    const double finish = 2.7 + (int8 ? 0.8 : 0.0) + (int8 && gated ? 0.7 : 0.0) + (p.add[0] ? 3.0 : 0.0) + (p.pre[0] ? 3.0 : 0.0);
+    return 7.0 + (rounds - 1) * (walk > finish ? walk : finish) + walk + finish - 2.7;
 }
 
 int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
@@ -456,6 +471,10 @@ int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
         const Operand &ol = p.lo[i];
         if (ol.p && !encode_map(&a.a[2 + i], ol.p, p.K, p.M, ol.ld, e, 64)) return LORDBA_ECUDA;
     }
+    for (int i = 0; i < 2; ++i) {
+        if (f.vec_out && f.out[i] && !encode_store_map(&a.out[i], f.out[i], f.M, f.N, f.ldo, f.dtype == LORDBA_F32 ? 4 : 2)) return LORDBA_ECUDA;
+        if (f.vec_pre && f.pre[i] && !encode_store_map(&a.pre[i], f.pre[i], f.M, f.N, f.ld_pre, 2)) return LORDBA_ECUDA;
+    }
     const bool a_mn = p.a[0].mn_major, b_mn = p.b[0].mn_major;
     a.f = f;
     a.k_blocks = (int)((p.K + block_k - 1) / block_k);
@@ -469,10 +488,11 @@ int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
     a.status = device_status_word();
     if (!a.status) return LORDBA_ECUDA;
     a.idesc = instr_desc(int8, p.kind == kProductBf16, a_mn, b_mn, 256, 256);
-    if (int8) return gated ? launch_tile<true, true, false, false>(a, stream) : launch_tile<true, false, false, false>(a, stream);
-    if (gated) return launch_tile<false, true, false, false>(a, stream);
-    if (pair) return launch_tile<false, false, true, true>(a, stream);
-    return launch_tile<false, false, false, true>(a, stream);
+    switch (p.dtype) {
+        case LORDBA_BF16: return launch_typed<LORDBA_BF16>(a, int8, gated, pair, stream);
+        case LORDBA_F16: return launch_typed<LORDBA_F16>(a, int8, gated, pair, stream);
+        default: return launch_tile<true, false, false, false, LORDBA_F32>(a, stream);      // 8-bit products only
+    }
 }
 
 }  // namespace lordba
