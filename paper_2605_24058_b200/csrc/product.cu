@@ -100,7 +100,7 @@ Way way_of(const Product &p)
 {
     double copied = 0;
     for (int i = 0; i < 2; ++i) copied += (double)packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + (double)packed_bytes(p.b[i], p.N, p.K, elt_of(p));
-    const double copies = copied > 0 ? 3.0 + copied * 3 / 6.0e6 : 0.0;
+    const double copies = copied > 0 ? 2.5 + copied * 3 / 6.0e6 : 0.0;
     const bool tiles_too = !(p.lo[0].p && p.form == Product::kSum);       // the second terms of a sum: streaming only
     Way best = {!tiles_too, copied > 0};
     double us = tiles_too ? tile_estimate(p) + copies : 1e30;

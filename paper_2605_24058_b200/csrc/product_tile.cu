@@ -131,6 +131,25 @@ __device__ __noinline__ void put_elements(uint32_t patch, uint8_t *q, int64_t ld
     }
 }
 
+// the first n elements of a piece to q
+__device__ __noinline__ void put_tail(uint4 x, uint8_t *q, int n, int e)
+{
+    uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll 1
+    for (int j = 0; j < n; ++j) {
+        if (e == 4) {
+            reinterpret_cast<uint32_t *>(q)[j] = w[0];
+            w[0] = w[1]; w[1] = w[2];
+        } else {
+            reinterpret_cast<uint16_t *>(q)[j] = (uint16_t)w[0];
+            w[0] = __funnelshift_r(w[0], w[1], 16);
+            w[1] = __funnelshift_r(w[1], w[2], 16);
+            w[2] = __funnelshift_r(w[2], w[3], 16);
+            w[3] >>= 16;
+        }
+    }
+}
+
 // A matrix that results go to.
 struct Target {
     const CUtensorMap *map;
@@ -155,7 +174,13 @@ struct Patches {
         fence_proxy_async();
         __syncwarp();
         if (t.vec) {
-            if (lane == 0) store_tile(t.map, patch, (int)n, (int)m0);
+            // the copy engine writes whole 16-byte pieces, so its map ends with the last of them; what the row has
+            // beyond it goes by hand
+            const int piece = 16 / t.e, tail = left < 64 / t.e ? (int)left % piece : 0;
+            if (lane == 0 && left >= piece) store_tile(t.map, patch, (int)n, (int)m0);
+            if (tail && lane < rows)
+                put_tail(load_shared_v4(patch_piece(patch, lane, (int)left / piece)),
+                         static_cast<uint8_t *>(t.p) + ((m0 + lane) * t.ld + n + left - tail) * t.e, tail, t.e);
         } else {
             put_elements(patch, static_cast<uint8_t *>(t.p) + (m0 * t.ld + n) * t.e, t.ld * t.e, rows, left, t.e);
             __syncwarp();
@@ -441,7 +466,7 @@ int launch_typed(const TileArgs &a, bool int8, bool gated, bool pair, cudaStream
 }  // namespace
 
 // 0.285 us a stage (its MMAs at the clock under load) or the epilogue's time, whichever is longer, a round of tiles;
-// the last round's epilogue shows; 7 us around them.
+// the last round's epilogue shows; 5.4 us around them.
 double tile_estimate(const Product &p)
 {
     const bool gated = p.form == Product::kGated, int8 = p.kind == kProductInt8;
@@ -450,8 +475,8 @@ double tile_estimate(const Product &p)
                          (p.form == Product::kPair ? 2 : 1);
     const double rounds = (double)(int64_t)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
     const double walk = 0.285 * (double)((p.K + block_k - 1) / block_k) * (p.form == Product::kSum ? 2 : 1);
-    const double finish = 2.7 + (int8 ? 0.8 : 0.0) + (int8 && gated ? 0.7 : 0.0) + (p.add[0] ? 3.0 : 0.0) + (p.pre[0] ? 3.0 : 0.0);
-    return 7.0 + (rounds - 1) * (walk > finish ? walk : finish) + walk + finish - 2.7;
+    const double finish = 2.7 + (int8 ? 0.8 : 0.0) + (int8 && gated ? 0.7 : 0.0) + (p.add[0] ? 2.0 : 0.0) + (p.pre[0] ? 1.5 : 0.0);
+    return 5.4 + (rounds - 1) * (walk > finish ? walk : finish) + walk + finish - 2.7;
 }
 
 int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
@@ -472,8 +497,11 @@ int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
         if (ol.p && !encode_map(&a.a[2 + i], ol.p, p.K, p.M, ol.ld, e, 64)) return LORDBA_ECUDA;
     }
     for (int i = 0; i < 2; ++i) {
-        if (f.vec_out && f.out[i] && !encode_store_map(&a.out[i], f.out[i], f.M, f.N, f.ldo, f.dtype == LORDBA_F32 ? 4 : 2)) return LORDBA_ECUDA;
-        if (f.vec_pre && f.pre[i] && !encode_store_map(&a.pre[i], f.pre[i], f.M, f.N, f.ld_pre, 2)) return LORDBA_ECUDA;
+        const int eo = f.dtype == LORDBA_F32 ? 4 : 2;
+        const int64_t cols = f.N - f.N % (16 / eo);             // whole 16-byte pieces
+        if (cols == 0) break;
+        if (f.vec_out && f.out[i] && !encode_store_map(&a.out[i], f.out[i], f.M, cols, f.ldo, eo)) return LORDBA_ECUDA;
+        if (f.vec_pre && f.pre[i] && !encode_store_map(&a.pre[i], f.pre[i], f.M, cols, f.ld_pre, 2)) return LORDBA_ECUDA;
     }
     const bool a_mn = p.a[0].mn_major, b_mn = p.b[0].mn_major;
     a.f = f;

@@ -121,7 +121,8 @@ INT8_SIZES = [  # T, d_in, d_out, padx, padw, pady, lead
     (8, 2048, 640, 0, 0, 0, 0), (16, 1000, 257, 8, 24, 1, 0), (17, 4096, 384, 0, 0, 0, 0), (33, 256, 96, 16, 0, 8, 0),
     (64, 1111, 333, 0, 0, 0, 0), (65, 640, 512, 0, 0, 0, 0), (128, 2048, 1024, 0, 0, 0, 0), (129, 160, 2049, 0, 0, 0, 0),
     (256, 512, 256, 0, 0, 0, 0), (300, 1001, 700, 7, 0, 3, 1), (513, 384, 520, 0, 16, 0, 0), (777, 96, 1533, 0, 0, 0, 5),
-    (1025, 1024, 1024, 0, 0, 0, 0), (2048, 64, 4096, 0, 0, 0, 0), (2500, 300, 600, 4, 4, 4, 0)]
+    (1025, 1024, 1024, 0, 0, 0, 0), (2048, 64, 4096, 0, 0, 0, 0), (2500, 300, 600, 4, 4, 4, 0),
+    (600, 256, 1533, 0, 0, 3, 0), (700, 128, 2045, 0, 0, 3, 0)]
 
 
 @pytest.mark.parametrize("T,d_in,d_out,padx,padw,pady,lead", INT8_SIZES)
@@ -194,7 +195,7 @@ def gated_bounds(vx, vg, vu, g, u, act, scale=None):
 GATED_SIZES = [  # T, d_in, d_hidden, pad, lead
     (1, 1, 1, 0, 0), (1, 64, 64, 0, 0), (1, 2048, 700, 0, 0), (2, 128, 128, 0, 0), (8, 512, 1000, 0, 0), (9, 100, 131, 0, 0), (16, 320, 256, 8, 0),
     (17, 77, 333, 5, 1), (40, 1024, 130, 0, 0), (64, 256, 512, 0, 0), (65, 64, 129, 0, 3), (128, 640, 384, 0, 0), (150, 500, 300, 0, 0),
-    (256, 128, 256, 64, 0), (333, 520, 1365, 0, 0), (600, 192, 640, 0, 0), (1100, 256, 520, 0, 0)]
+    (256, 128, 256, 64, 0), (333, 520, 1365, 0, 0), (600, 192, 640, 0, 0), (1100, 256, 520, 0, 0), (600, 192, 635, 5, 0), (900, 64, 2043, 5, 0)]
 
 
 @pytest.mark.parametrize("T,d_in,d_hidden,pad,lead", GATED_SIZES)
