@@ -593,7 +593,8 @@ StreamPlan plan_stream(const Product &p)
     s.smem = fixed + (used > exchange ? used : exchange);
     // The split over a cluster, and over clusters, that takes the least time.  A stage takes a CTA the time of its
     // bytes at what an SM draws from L2 (110 KB/us two CTAs, 80 one; shifted stages 12 - 18); an epilogue of 128 tokens
-    // 5.5 us (gated 12), shared by the cluster; all together no less than the weights at HBM's rate.  Groups write
+    // 5.5 us (gated 12), shared by the cluster; all together no less than the weights at HBM's rate, the shorter of
+    // the two not quite hidden (gated 8 x 4096 -> 11008: clusters of three 32 us, of two 37 us).  Groups write
     // their sums and another kernel reads them.
     const int64_t work = s.row_tiles * s.token_tiles * problems;
     const int blocks = s.k_blocks * s.parts;
@@ -608,7 +609,7 @@ StreamPlan plan_stream(const Product &p)
             const double rounds = (double)((work * g + fit - 1) / fit), steps = (double)((blocks + n * g - 1) / (n * g));
             const double finish = 1.0 + s.tokens / 128.0 * (g > 1 ? 3.0 * sums : gated ? 12.0 : 5.5) / n;
             const double walk = rounds * (steps * stage_us + finish);
-            const double us = (s.loose ? 5.2 : 4.2) + (walk > hbm ? walk : hbm) + (g > 1 ? 4.0 + 2 * g * plane / 4.0e6 : 0.0);
+            const double us = (s.loose ? 5.2 : 4.2) + (walk > hbm ? walk + 0.15 * hbm : hbm + 0.15 * walk) + (g > 1 ? 4.0 + 2 * g * plane / 4.0e6 : 0.0);
             if (s.split == 0 || us < s.us * (g > 1 ? 0.9 : 1.0)) {
                 s.split = n;
                 s.groups = g;
