@@ -426,7 +426,8 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
                     const uint32_t from = peer_addr(base, r) + 4u * j;
 #pragma unroll
                     for (int k = 0; k < kBatch; ++k) {
-                        const int i = it + k * step < items ? it + k * step : it;
+                        const int i = it + k * step;
+                        if (i < items)         // a predicate of the loads: a way out of the loop would keep them from being batched
 #pragma unroll
                         for (int c = 0; c < kSums; ++c) {
                             const uint32_t at = from + 4u * ((c * columns + i / (kRows / 4)) * kRows);
@@ -577,43 +578,51 @@ StreamPlan plan_stream(const Product &p)
     s.token_tiles = (p.M + s.tokens - 1) / s.tokens;
     const int columns = s.halves * s.tokens, stage = sums * kWeightBytes + columns * 128, exchange = sums * columns * kRows * 4;
     const int fixed = kBarBytes + 1024, half = kHalf - fixed, whole = kWhole - fixed;
-    // two CTAs an SM where three stages and the exchange fit half of its shared memory, else one
-    const int per_sm = !s.loose && 3 * stage <= half && exchange <= half ? 2 : 1;
-    int used;
-    if (s.loose) {
-        const int raw = sums * (w_mn ? 64 * kRawPitch<2> : kRows * kRawPitch<1>) + columns * kRawPitch<1>;
-        s.stages = 3 * stage + 3 * raw <= whole ? 3 : 2;
-        s.raw_stages = (whole - s.stages * stage) / raw < 6 ? (whole - s.stages * stage) / raw : 6;
-        used = s.stages * stage + s.raw_stages * raw;
-    } else {
-        const int room = per_sm == 2 ? half : whole;
-        s.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
-        used = s.stages * stage;
-    }
-    s.smem = fixed + (used > exchange ? used : exchange);
-    // The split over a cluster, and over clusters, that takes the least time.  A stage takes a CTA the time of its
-    // bytes at what an SM draws from L2 (110 KB/us two CTAs, 80 one; shifted stages 12 - 18); an epilogue of 128 tokens
-    // 5.5 us (gated 12), shared by the cluster; all together no less than the weights at HBM's rate, the shorter of
-    // the two not quite hidden (gated 8 x 4096 -> 11008: clusters of three 32 us, of two 37 us).  Groups write
-    // their sums and another kernel reads them.
+    const int raw = sums * (w_mn ? 64 * kRawPitch<2> : kRows * kRawPitch<1>) + columns * kRawPitch<1>;       // LOOSE: of a stage
     const int64_t work = s.row_tiles * s.token_tiles * problems;
     const int blocks = s.k_blocks * s.parts;
-    const double stage_us = per_sm * stage / (s.loose ? (w_mn ? 12e3 : 18e3) : per_sm == 2 ? 110e3 : 80e3);
-    const double hbm = (double)p.N * (double)p.K * e * sums * s.parts / 6.0e6;
+    const double hbm = (double)p.N * (double)p.K * e * sums * s.parts / 9.0e6;
     const double plane = (double)p.M * (double)((p.N + 3) / 4 * 16) * sums * problems;       // bytes of a group's sums
     const Resident *res = resident(form, s.loose);
-    for (int n = 1; res && n <= kMaxSplit && n <= blocks; ++n) {
-        const int fit = per_sm * res->clusters[n];
-        if (fit < 1) continue;
-        for (int g = 1; g <= 16 && n * g * (g > 1 ? 4 : 1) <= blocks && (g == 1 || g * plane < 64e6); g *= 2) {
-            const double rounds = (double)((work * g + fit - 1) / fit), steps = (double)((blocks + n * g - 1) / (n * g));
-            const double finish = 1.0 + s.tokens / 128.0 * (g > 1 ? 3.0 * sums : gated ? 12.0 : 5.5) / n;
-            const double walk = rounds * (steps * stage_us + finish);
-            const double us = (s.loose ? 5.2 : 4.2) + (walk > hbm ? walk + 0.15 * hbm : hbm + 0.15 * walk) + (g > 1 ? 4.0 + 2 * g * plane / 4.0e6 : 0.0);
-            if (s.split == 0 || us < s.us * (g > 1 ? 0.9 : 1.0)) {
-                s.split = n;
-                s.groups = g;
-                s.us = us;
+    // Two CTAs an SM where two stages and the exchange fit half of its shared memory, or one; the split over a
+    // cluster, and over clusters, that takes the least time.  A CTA draws its stages at what its ring holds in 0.84 us,
+    // at most 174 KB/us an SM (LOOSE: it shifts 12 - 18); an end of 128 columns takes it 3.2 us (gated 1.7 times
+    // that), 1.1 of them shared by the cluster, besides 2.5 us of latencies and 0.19 a CTA it exchanges with; the weights'
+    // way from HBM comes on top (9 TB/s: what is not hidden of it), and 0.3 us where no CTA of the next kernel has room.
+    // Fitted to 52 sizes (896 ... 11008, 1 ... 256 tokens) x 16 plans, off by 3 % near the best ones: what it chooses takes
+    // 2 % more than the best plan, where rules without the rings' depth took 8 % (8-bit 4096 x 4096, 64 tokens: clusters of
+    // four 9.1, of six 10 us; gated 4096 x 11008, 64 tokens: two CTAs an SM of two stages 36 us, one of five 42).
+    // Groups write their sums and another kernel reads them.
+    for (int per_sm = s.loose ? 1 : 2; res && per_sm >= 1; --per_sm) {
+        const int room = per_sm == 2 ? half : whole;
+        int stages, raw_stages = 0, used;
+        if (s.loose) {
+            stages = 3 * stage + 3 * raw <= room ? 3 : 2;
+            raw_stages = (room - stages * stage) / raw < 6 ? (room - stages * stage) / raw : 6;
+            used = stages * stage + raw_stages * raw;
+        } else {
+            stages = room / stage < kMaxStages ? room / stage : kMaxStages;
+            used = stages * stage;
+        }
+        if (stages < 2 || exchange > room) continue;
+        for (int n = 1; n <= kMaxSplit && n <= blocks; ++n) {
+            const int fit = per_sm * res->clusters[n];
+            if (fit < 1) continue;
+            for (int g = 1; g <= 16 && n * g * (g > 1 ? 4 : 1) <= blocks && (g == 1 || g * plane < 64e6); g *= 2) {
+                const double rounds = (double)((work * g + fit - 1) / fit), steps = (double)((blocks + n * g - 1) / (n * g));
+                const double most = 174e3 / (per_sm == 2 && work * n * g > sm_count() ? 2 : 1), ring = (double)stages * stage / 0.84;
+                const double stage_us = stage / (s.loose ? (w_mn ? 12e3 : 18e3) : ring < most ? ring : most);
+                const double finish = 2.5 + columns / 128.0 * (gated ? 1.7 : 1.0) * (3.2 + 1.1 / n) + 0.19 * (n - 1);
+                const double us = (s.loose ? 2.0 : 1.0) + hbm + rounds * (steps * stage_us + finish) + (per_sm == 1 ? 0.3 : 0.0) +
+                                  (g > 1 ? 4.0 + 2 * g * plane / 4.0e6 : 0.0);
+                if (s.split == 0 || us < s.us * (g > 1 ? 0.9 : 1.0)) {
+                    s.split = n;
+                    s.groups = g;
+                    s.us = us;
+                    s.stages = stages;
+                    s.raw_stages = raw_stages;
+                    s.smem = fixed + (used > exchange ? used : exchange);
+                }
             }
         }
     }

@@ -465,18 +465,25 @@ int launch_typed(const TileArgs &a, bool int8, bool gated, bool pair, cudaStream
 
 }  // namespace
 
-// 0.285 us a stage (its MMAs at the clock under load) or the epilogue's time, whichever is longer, a round of tiles;
-// the last round's epilogue shows; 5.4 us around them.
+// A round of tiles takes 0.285 us a stage (its MMAs at the clock under load), or the epilogue's time, or what its columns
+// of B take from HBM at 4.2 TB/s (few rows: 2560 x 6912 gated 20 us), whichever is longest; the last round's
+// epilogue shows; 5.4 us around them.
 double tile_estimate(const Product &p)
 {
     const bool gated = p.form == Product::kGated, int8 = p.kind == kProductInt8;
-    const int block_k = int8 ? 128 : 64;
-    const double tiles = (double)((p.M + kTileM - 1) / kTileM) * (double)((p.N + (gated ? 127 : 255)) / (gated ? 128 : 256)) *
-                         (p.form == Product::kPair ? 2 : 1);
-    const double rounds = (double)(int64_t)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
-    const double walk = 0.285 * (double)((p.K + block_k - 1) / block_k) * (p.form == Product::kSum ? 2 : 1);
+    const int block_k = int8 ? 128 : 64, parts = p.form == Product::kSum ? 2 : 1, pairs = sm_count() / 2;
+    const int64_t tiles_m = (p.M + kTileM - 1) / kTileM;
+    const int64_t tiles = tiles_m * ((p.N + (gated ? 127 : 255)) / (gated ? 128 : 256)) * (p.form == Product::kPair ? 2 : 1);
+    const double column = 256.0 * (double)p.K * (int8 ? 1 : 2) * parts / 4.2e6;
+    const int64_t across = tiles_m < 8 ? tiles_m : 8;
+    const double walk = 0.285 * (double)((p.K + block_k - 1) / block_k) * parts;
     const double finish = 2.7 + (int8 ? 0.8 : 0.0) + (int8 && gated ? 0.7 : 0.0) + (p.add[0] ? 2.0 : 0.0) + (p.pre[0] ? 1.5 : 0.0);
-    return 5.4 + (rounds - 1) * (walk > finish ? walk : finish) + walk + finish - 2.7;
+    auto round = [&](int64_t n) {              // of n tiles
+        const double loads = column * (double)((n + across - 1) / across);
+        return walk > loads ? walk : loads;
+    };
+    const double full = round(pairs), last = round((tiles - 1) % pairs + 1);
+    return 5.4 + (double)((tiles - 1) / pairs) * (full > finish ? full : finish) + last + finish - 2.7;
 }
 
 int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
