@@ -373,7 +373,7 @@ int lordba_fit_scales(const float *target, int64_t ld, const uint32_t *packed_A,
  *
  * dtype: the type of y (and of the activations that are quantised): LORDBA_BF16, LORDBA_F16 or
  * LORDBA_F32.  Any sizes, pitches and alignments are taken; operands whose base or pitch is not a
- * multiple of 16 bytes are first copied into the workspace.  T = 0 is a no-op.
+ * multiple of 16 bytes cost more time and may be copied into the workspace first.  T = 0 is a no-op.
  */
 #define LORDBA_INT8_MAX_DIN 131071
 typedef struct lordba_int8_proj {
@@ -387,8 +387,9 @@ typedef struct lordba_int8_proj {
 
 int lordba_int8_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scale, int64_t T,
                               int64_t d, int dtype, void *stream);
-/* Bytes of workspace the call needs: [device], 256-byte aligned; 0 when every operand is aligned (the
- * workspace may then be NULL).  LORDBA_EINVAL from the call when the workspace given is shorter. */
+/* Bytes of workspace the call needs: [device], 256-byte aligned; 0 for most calls (the workspace may then be
+ * NULL), not 0 where operands are copied or a long sum with few results is split and joined.  LORDBA_EINVAL
+ * from the call when the workspace given is shorter. */
 size_t lordba_int8_linear_workspace_bytes(const lordba_int8_proj *p, int64_t T);
 int lordba_int8_linear(const lordba_int8_proj *p, int64_t T, int dtype, void *workspace, size_t workspace_bytes,
                        void *stream);

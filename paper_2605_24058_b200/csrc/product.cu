@@ -90,8 +90,8 @@ Product copied_form(const Product &p)
 // Few rows, or few results of long sums: the streaming kernel.  Else tiles.  Unaligned operands are copied for the
 // tiles, and for the streaming kernel where that is quicker than its own shifting (many rows, which shift the
 // weights once for each 128 of them); copies cost a launch and three passes over their bytes.
-// Measured, 8-bit 4096 x 4096: 64 rows 8 us streaming, 16 us in tiles; 512 rows 16 and 17 us; 2048 rows 47 and
-// 31 us.  Gated, 16-bit 4096 x 11008: 64 rows 42 and 51 us, 256 rows 96 and 52 us.
+// Measured, 8-bit 4096 x 4096: 64 rows 9.0 us streaming, 15.5 us in tiles; 256 rows 13.8 and 15.8 us; 2048 rows 44 and
+// 29 us.  Gated, 16-bit 4096 x 11008: 64 rows 36 and 54 us, 128 rows 45 and 54 us, 256 rows 95 and 54 us.
 struct Way {
     bool stream, copy;
 };

@@ -14,8 +14,11 @@
 //               latencies, so two groups of four warps take turns at the tiles, one computing while the other
 //               waits; where every pair has but one tile they share it.
 //
-// Measured: 8-bit 8192 x 11008 -> 4096 230 us (3.2 Pop/s); gated 2048 x 4096 -> 11008 in bf16 with addends and
-// saved pre-activations 271 us (1.36 PFLOP/s, of the 1.39 that a library product sustains under the power cap).
+// Measured, in short bursts and, second, sustained under the power cap: 8-bit 8192 x 11008 -> 4096 230 and 275 us
+// (3.2 and 2.7 Pop/s); gated 2048 x 4096 -> 11008 in bf16 246 and 289 us (1.50 and 1.28 PFLOP/s), with addends and saved
+// pre-activations 286 and 333 us.  A library product of the same size, without gate, takes 239 and 282 us, with an addend
+// 269 and 313 us.  Gradients of the same block: dx 249 and 294 us, both dW 261 and 307 us (library 239 and 276, 246 and
+// 286).  What is left is the loads: 3.1 - 3.7 GB from L2 a product, 13 TB/s, and at 1.4 GHz their power.
 // Sixteen epilogue warps, or 16 columns a step, cost such products 2 - 6 % and gain 5 - 20 % only where the
 // contraction is so short that the epilogue is all there is.
 //

@@ -470,7 +470,7 @@ def int8_linear(x, s_x, w, s_w, y: Optional[torch.Tensor] = None, dtype: torch.d
     """y[t, n] = s_x[t] s_w[n] sum_k x[t, k] w[n, k] for int8 x (T, d_in) and w (d_out, d_in): the frozen base
     projection that an adapter's term is added to.  y (of its own type, or of ``dtype`` when made here) is
     overwritten and returned.  workspace: a uint8 CUDA tensor of lordba_int8_linear_workspace_bytes(), made here
-    if absent; only some calls with operands off 16-byte boundaries need one."""
+    if absent; only some calls need one (operands off 16-byte boundaries, long sums with few results)."""
     return _native().int8_linear(x, s_x, w, s_w, y, dtype, workspace, stream)
 
 
