@@ -165,7 +165,8 @@ struct Patches {
     uint32_t base;
     int which = 0;
 
-    // sixteen words of the lane's row m0 + lane, from column n on
+    // sixteen words of the lane's row m0 + lane, from column n on.  Every call makes one group of stores, also an empty
+    // one, because the wait that frees a patch counts groups: all but the latest is the patch's own and older ones.
     __device__ __forceinline__ void put(const uint32_t w[16], const Target &t, int64_t m0, int64_t n, int rows, int64_t left, int lane)
     {
         const uint32_t patch = base + which * kPatchBytes;
@@ -188,6 +189,7 @@ struct Patches {
             put_elements(patch, static_cast<uint8_t *>(t.p) + (m0 * t.ld + n) * t.e, t.ld * t.e, rows, left, t.e);
             __syncwarp();
         }
+        if (lane == 0) stores_commit();
     }
     // 32 values, in the target's type
     __device__ __forceinline__ void put32(const float v[32], const Target &t, int64_t m0, int64_t n, int rows, int64_t left, int lane, int dtype)

@@ -144,14 +144,15 @@ __device__ __forceinline__ void fetch_wait(int left)
     else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// The tile at `from` to memory; what lies outside of the matrix is left out.  One thread; its earlier stores are
-// counted in groups.
+// The tile at `from` to memory; what lies outside of the matrix is left out.  One thread.
 __device__ __forceinline__ void store_tile(const CUtensorMap *map, uint32_t from, int x, int y)
 {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(from), "r"(x), "r"(y) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
+// The thread's stores since the last call become a group (an empty one where there were none): the waits below
+// count groups.
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void stores_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void stores_complete() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map)
