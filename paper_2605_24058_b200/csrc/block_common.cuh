@@ -134,21 +134,24 @@ __device__ __forceinline__ float logistic(float z)
     return f;
 }
 
+// Beyond |g| = 128 f is 0 or 1 in 32 bits, so a factor beside it may be clamped there without changing a result: an
+// infinity then does not meet that zero (act(-inf) is 0, as for any g below -128), and a NaN still comes through f.
+constexpr float kFlat = 128.0f;
+
 template <int ACT>
 __device__ __forceinline__ float act_gate(float g)
 {
-    return g * logistic(ACT == LORDBA_ACT_SILU ? g : kGelu * g * fmaf(kGeluCubic * g, g, 1.0f));
+    return fmaxf(g, -kFlat) * logistic(ACT == LORDBA_ACT_SILU ? g : kGelu * g * fmaf(kGeluCubic * g, g, 1.0f));
 }
 
-// act(g) and act'(g) = f + g f (1 - f) k'(g).  Beyond |g| = 128 f is 0 or 1 in 32 bits and the second term
-// is 0: g is clamped there, so that infinities do not meet that zero.
+// act(g) and act'(g) = f + g f (1 - f) k'(g)
 template <int ACT>
 __device__ __forceinline__ void act_and_slope(float g, float &value, float &slope)
 {
     const float f = logistic(ACT == LORDBA_ACT_SILU ? g : kGelu * g * fmaf(kGeluCubic * g, g, 1.0f));
-    const float c = fminf(fmaxf(g, -128.0f), 128.0f);
+    const float low = fmaxf(g, -kFlat), c = fminf(low, kFlat);
     const float inner = ACT == LORDBA_ACT_SILU ? 1.0f : kGelu * fmaf(3.0f * kGeluCubic * c, c, 1.0f);
-    value = g * f;
+    value = low * f;
     slope = fmaf(c * f * (1.0f - f), inner, f);
 }
 

@@ -1,0 +1,59 @@
+"""Calls of the operators next to the adapters at the edges of what they take: pre-activations that are not finite."""
+import math
+
+import pytest
+import torch
+
+from paper_2605_24058_b200 import lordba
+
+pytestmark = pytest.mark.gpu
+
+
+# 4 rows are streamed, 300 go through tiles
+@pytest.mark.parametrize("T", [4, 300])
+@pytest.mark.parametrize("act", [lordba.ACT_SILU, lordba.ACT_GELU_TANH])
+@pytest.mark.parametrize("dtype,bits", [(torch.float16, 16), (torch.bfloat16, 16), (torch.float16, 8)])
+def test_a_gate_of_minus_infinity_is_shut(T, act, dtype, bits):
+    """An addend of -inf masks its entry: act(-inf) = 0 and act'(-inf) = 0, forward and backward, and no other entry
+    changes.  +inf and NaN go through as the formulas say."""
+    n, d = 264, 64
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T + bits)
+    x, wg, wu = (torch.randn(r, d, generator=gen, device="cuda").to(dtype) for r in (T, n, n))
+    scales = None
+    if bits == 8:
+        (x, sx), (wg, sg), (wu, su) = (lordba.int8_quantize_rows(t) for t in (x, wg, wu))
+        scales = (sx, sg, su)
+    add = torch.zeros(T, n, dtype=dtype, device="cuda")
+    call = lambda a: lordba.gated_forward(x, wg, wu, act=act, scales=scales, dtype=dtype, gate_add=a, up_add=torch.zeros_like(a), save=True)
+    plain, plain_gate, plain_up = call(add)
+    masked = add.clone()
+    masked[1, 5], masked[2, 263], masked[3, 0], masked[3, 7], masked[0, 100] = -math.inf, -math.inf, math.inf, math.nan, -math.inf
+    shut = masked == -math.inf
+    h, gate, up = call(masked)
+    assert (h[shut] == 0).all() and (gate[shut] == -math.inf).all()
+    assert h[3, 0].abs() == math.inf and h[3, 7].isnan()
+    same = masked == 0
+    assert torch.equal(h[same], plain[same]) and torch.equal(gate[same], plain_gate[same]) and torch.equal(up, plain_up)
+    dh = torch.randn(T, n, generator=gen, device="cuda").to(dtype)
+    gate[3, 0] = gate[3, 7] = 1.0
+    dgate, dup = lordba.gated_backward(dh, gate, up, act=act)[:2]
+    assert (dgate[shut] == 0).all() and (dup[shut] == 0).all()
+    assert dgate.isfinite().all() and dup.isfinite().all()
+
+
+@pytest.mark.parametrize("T", [4, 300])
+def test_a_stored_gate_that_overflowed_float16_has_no_gradient(T):
+    """g = -80000 is -inf in float16; the unrounded forward gives h = 0, and the gradients from the stored value are
+    those of a shut gate: dx and dw stay finite."""
+    n, d = 72, 16
+    x = torch.full((T, d), 100.0, dtype=torch.float16, device="cuda")
+    w = torch.full((n, d), 0.01, dtype=torch.float16, device="cuda")
+    w[3] = -50.0
+    up = torch.full((n, d), 0.01, dtype=torch.float16, device="cuda")
+    h, gate, u = lordba.gated_forward(x, w, up, save=True)
+    assert (gate[:, 3] == -math.inf).all() and (h[:, 3] == 0).all() and (h[:, 4] > 100).all()
+    dh = torch.ones(T, n, dtype=torch.float16, device="cuda")
+    dgate, dup, dx, dwg, dwu = lordba.gated_backward(dh, gate, u, x, w, up)
+    assert (dgate[:, 3] == 0).all() and (dup[:, 3] == 0).all()
+    assert all(t.isfinite().all() for t in (dgate, dup, dx)) and (dwg[3] == 0).all() and (dwu[3] == 0).all()
