@@ -57,6 +57,7 @@ struct StreamArgs {
     int groups;              // more than 1: so many clusters share a tile's contraction and write their sums to
     uint32_t *raw;           // raw, [group][problem or gate, up][M][raw_ld], for finish_kernel to add
     int64_t raw_ld;          // N rounded up to 4
+    uint32_t *whole;         // [blockIdx.z][row tile]: whether the cluster's sums are complete; every cluster says so
     int stages, split;
     int raw_stages;          // LOOSE: stages fetched ahead (2 ... 6)
     int tmem_columns;
@@ -414,6 +415,8 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
         tmem_free<1>(tmem, P.tmem_columns);
     }
 
+    if (P.groups > 1 && rank == 0 && threadIdx.x == 0) P.whole[blockIdx.z * gridDim.y + blockIdx.y] = *abort_flag == 0;
+
     // four weight rows of one token an item, the items dealt to the cluster's threads, kBatch of a thread's at
     // a time: their sums are all on the way before the first is finished
     if (*abort_flag == 0) {
@@ -465,26 +468,41 @@ product_stream_kernel(const __grid_constant__ StreamArgs P)
     }
 }
 
-// Adds what the groups of a product left in raw, in group order, and finishes.  A thread: four columns of a row.
+// What the groups of a product left: their sums, and whether each cluster's are complete.
+struct Joint {
+    const uint32_t *raw, *whole;
+    int64_t ld;                                  // of raw
+    int groups, problems, tokens, token_tiles, row_tiles;
+};
+
+// Adds the groups' sums in group order and finishes.  A thread: four columns of a row.  Where a group gave up a wait
+// its sums are not there, and the results stay as they were.
 template <bool INT8, bool GATED>
 __global__ void __launch_bounds__(256)
-finish_kernel(const __grid_constant__ Finish F, const uint32_t *__restrict__ raw, int64_t ld, int groups, int problems)
+finish_kernel(const __grid_constant__ Finish F, const __grid_constant__ Joint J)
 {
-    const int64_t n = 4 * ((int64_t)blockIdx.x * 64 + threadIdx.x % 64);
-    const int planes = GATED ? 2 : problems, problem = GATED ? 0 : blockIdx.z;
+    const int64_t n = 4 * ((int64_t)blockIdx.x * 64 + threadIdx.x % 64);      // a warp's columns lie in one row tile
+    const int planes = GATED ? 2 : J.problems, problem = GATED ? 0 : blockIdx.z, lane = threadIdx.x % 32;
+    const bool in = n < F.N;
     grid_wait();
     grid_release();
-    if (n >= F.N) return;
+    if (n - 4 * lane >= F.N) return;
     for (int64_t m = (int64_t)blockIdx.y * 4 + threadIdx.x / 64; m < F.M; m += (int64_t)gridDim.y * 4) {
-        uint4 acc[2];
+        // the groups' words, a lane each
+        const int64_t word = (((int64_t)lane * J.problems + problem) * J.token_tiles + (int)m / J.tokens) * J.row_tiles + n / kRows;
+        const bool complete = lane >= J.groups || J.whole[word] != 0;
+        uint4 acc[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        if (in) {
 #pragma unroll
-        for (int c = 0; c < (GATED ? 2 : 1); ++c) {
-            const uint4 *p = reinterpret_cast<const uint4 *>(raw + ((GATED ? c : problem) * F.M + m) * ld + n);
-            const int64_t next = planes * F.M * ld / 4;
-            acc[c] = __ldcs(p);
+            for (int c = 0; c < (GATED ? 2 : 1); ++c) {
+                const uint4 *p = reinterpret_cast<const uint4 *>(J.raw + ((GATED ? c : problem) * F.M + m) * J.ld + n);
+                const int64_t next = planes * F.M * J.ld / 4;
+                acc[c] = __ldcs(p);
 #pragma unroll 4
-            for (int g = 1; g < groups; ++g) acc[c] = add4<INT8>(acc[c], __ldcs(p + g * next));
+                for (int g = 1; g < J.groups; ++g) acc[c] = add4<INT8>(acc[c], __ldcs(p + g * next));
+            }
         }
+        if (!__all_sync(0xffffffffu, complete) || !in) continue;
         const uint4 w = acc[GATED ? 1 : 0];
         const uint32_t g[4] = {acc[0].x, acc[0].y, acc[0].z, acc[0].w}, u[4] = {w.x, w.y, w.z, w.w};
         finish4<INT8, GATED>(F, problem, m, n, g, u);
@@ -560,7 +578,7 @@ struct StreamPlan {
     bool loose;
     int tokens, halves, k_blocks, parts, stages, raw_stages, split, groups, smem;
     int64_t row_tiles, token_tiles;
-    size_t raw_bytes;      // of the sums that groups leave
+    size_t raw_bytes, whole_bytes;      // of the sums that groups leave, and of the words that say whether they are complete
     double us;             // estimate
 };
 
@@ -631,7 +649,10 @@ StreamPlan plan_stream(const Product &p)
             }
         }
     }
-    s.raw_bytes = s.groups > 1 ? (size_t)s.groups * (size_t)plane : 0;
+    if (s.groups > 1) {
+        s.raw_bytes = (size_t)s.groups * (size_t)plane;
+        s.whole_bytes = (size_t)(s.groups * work) * 4;
+    }
     return s;
 }
 
@@ -643,7 +664,11 @@ double stream_estimate(const Product &p)
     return s.split > 0 && s.row_tiles <= 65535 && s.token_tiles <= 65535 / 32 ? s.us : -1.0;
 }
 
-size_t stream_workspace_bytes(const Product &p) { return plan_stream(p).raw_bytes; }
+size_t stream_workspace_bytes(const Product &p)
+{
+    const StreamPlan s = plan_stream(p);
+    return s.raw_bytes + s.whole_bytes;
+}
 
 int launch_product_stream(const Product &p, const Finish &f, void *workspace, cudaStream_t stream)
 {
@@ -665,6 +690,7 @@ int launch_product_stream(const Product &p, const Finish &f, void *workspace, cu
     a.groups = plan.groups;
     a.raw = static_cast<uint32_t *>(workspace);
     a.raw_ld = (p.N + 3) / 4 * 4;
+    a.whole = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(workspace) + plan.raw_bytes);
     a.stages = plan.stages;
     a.raw_stages = plan.raw_stages;
     a.split = plan.split;
@@ -703,7 +729,8 @@ int launch_product_stream(const Product &p, const Finish &f, void *workspace, cu
     const dim3 grid((unsigned)gx, (unsigned)(gy < most ? gy : most), (unsigned)a.problems);
     const auto kernel = int8 ? (gated ? finish_kernel<true, true> : finish_kernel<true, false>)
                              : (gated ? finish_kernel<false, true> : finish_kernel<false, false>);
-    return launch_kernel(kernel, grid, 256, 0, stream, f, static_cast<const uint32_t *>(a.raw), a.raw_ld, plan.groups, a.problems);
+    const Joint joint{a.raw, a.whole, a.raw_ld, plan.groups, a.problems, plan.tokens, a.token_tiles, (int)plan.row_tiles};
+    return launch_kernel(kernel, grid, 256, 0, stream, f, joint);
 }
 
 }  // namespace lordba
