@@ -439,7 +439,7 @@ int lordba_gated_forward(const lordba_gated *g, int64_t T, int dtype, void *work
  * not read), dw_gate / dw_up when both of theirs are (x is then not read).  Every sum is float32.  dgate
  * and dup enter the products in the matrices' type, because that is what the tensor cores take: as written
  * for more than 64 tokens, with the rest that their rounding left as a second term up to there (where it
- * costs nothing).  The result is the same from run to run.  T = 0 writes zeros into dw_gate and dw_up.
+ * costs nothing; dx of more than 65535 * 128 columns goes without).  The result is the same from run to run.  T = 0 writes zeros into dw_gate and dw_up.
  * dtype: LORDBA_BF16 or LORDBA_F16.
  */
 typedef struct lordba_gated_grad {

@@ -147,7 +147,8 @@ struct Product {
     ProductKind kind;
     int64_t M, N, K;
     Operand a[2], b[2];
-    Operand lo[2];       // added to a[0], a[1] (kSum with at most kLoTokens rows, kPair), or null: A in twice the bits
+    Operand lo[2];       // added to a[0], a[1] (kSum with at most kLoTokens rows, kPair), or null: A in twice the bits.
+                         // A kSum of more columns than the streaming kernel can take goes without.
     // kSingle: D = A0 B0.  kSum: D = A0 B0 + A1 B1.  kGated: gate = A0 B0, up = A0 B1.
     // kPair: two products A0 B0 and A1 B0 with an output each.
     enum Form { kSingle, kSum, kGated, kPair } form;

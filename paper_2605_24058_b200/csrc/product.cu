@@ -96,14 +96,17 @@ struct Way {
     bool stream, copy;
 };
 
+// Whether tiles would take the product without the rest of its entries' rounding.
+bool drops_rest(const Product &p) { return p.lo[0].p && p.form == Product::kSum; }
+
 Way way_of(const Product &p)
 {
     double copied = 0;
     for (int i = 0; i < 2; ++i) copied += (double)packed_bytes(p.a[i], p.M, p.K, elt_of(p)) + (double)packed_bytes(p.b[i], p.N, p.K, elt_of(p));
     const double copies = copied > 0 ? 2.5 + copied * 3 / 6.0e6 : 0.0;
-    const bool tiles_too = !(p.lo[0].p && p.form == Product::kSum);       // the second terms of a sum: streaming only
-    Way best = {!tiles_too, copied > 0};
-    double us = tiles_too ? tile_estimate(p) + copies : 1e30;
+    // the second terms of a sum: streaming, and tiles, without them, only where that cannot be had
+    Way best = {false, copied > 0};
+    double us = drops_rest(p) ? 1e30 : tile_estimate(p) + copies;
     if (copied > 0) {
         const double t = stream_estimate(copied_form(p));
         if (t >= 0 && t + copies <= us) { best = Way{true, true}; us = t + copies; }
@@ -132,6 +135,7 @@ int launch_product(const Product &given, void *workspace, cudaStream_t stream)
     uint8_t *next = static_cast<uint8_t *>(workspace);
     RepackList list = {};
     const Way way = way_of(p);
+    if (!way.stream && drops_rest(p)) p.lo[0] = p.lo[1] = Operand{};
     for (int i = 0; i < 4; ++i) {
         Operand &o = i < 2 ? p.a[i] : p.b[i - 2];
         const int64_t mn = i < 2 ? p.M : p.N;

@@ -1,4 +1,5 @@
-"""Calls of the operators next to the adapters at the edges of what they take: pre-activations that are not finite."""
+"""Calls of the operators next to the adapters at the edges of what they take: pre-activations that are not finite, very many
+columns."""
 import math
 
 import pytest
@@ -57,3 +58,24 @@ def test_a_stored_gate_that_overflowed_float16_has_no_gradient(T):
     dgate, dup, dx, dwg, dwu = lordba.gated_backward(dh, gate, u, x, w, up)
     assert (dgate[:, 3] == 0).all() and (dup[:, 3] == 0).all()
     assert all(t.isfinite().all() for t in (dgate, dup, dx)) and (dwg[3] == 0).all() and (dwu[3] == 0).all()
+
+
+def test_dx_of_few_tokens_and_very_many_columns():
+    """More columns than the streaming kernel's grid holds (65535 tiles of 128): tiles take over, also up to 64 tokens, where
+    the gradient's entries otherwise enter as two terms.  dgate and dup are held to the formula elsewhere; dx to the
+    float64 product of the returned entries: 2 d_hidden additions of 2^-23, one rounding to bfloat16 (2^-8)."""
+    n, d = 8, 65535 * 128 + 8
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    for T in (1, 3, 65):
+        dh, gate, up = (torch.randn(T, n, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(3))
+        wg, wu = (torch.randn(n, d, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+        dgate, dup, dx, _, _ = lordba.gated_backward(dh, gate, up, None, wg, wu)
+        assert lordba.device_status() == 0
+        for first in range(0, d, 1 << 20):
+            a, b = wg[:, first:first + (1 << 20)].double(), wu[:, first:first + (1 << 20)].double()
+            want = dgate.double() @ a + dup.double() @ b
+            size = dgate.double().abs() @ a.abs() + dup.double().abs() @ b.abs()
+            tol = 2 * n * 2.0 ** -23 * size
+            tol = tol + 2.0 ** -8 * (want.abs() + tol)
+            assert ((dx[:, first:first + (1 << 20)].double() - want).abs() <= tol).all()
