@@ -18,6 +18,7 @@ std::mutex g_status_mutex;
 int *g_status_ptr[64] = {nullptr};
 #ifdef LORDBA_TEST_HOOKS
 std::atomic<int> g_test_skip_item{-1};
+std::atomic<bool> g_test_fail_queries{false};
 #endif
 }  // namespace
 
@@ -42,6 +43,15 @@ int test_skip_item()
     return g_test_skip_item.load(std::memory_order_relaxed);
 #else
     return -1;
+#endif
+}
+
+bool test_fail_queries()
+{
+#ifdef LORDBA_TEST_HOOKS
+    return g_test_fail_queries.load(std::memory_order_relaxed);
+#else
+    return false;
 #endif
 }
 
@@ -461,6 +471,13 @@ int lordba_adapter_forward_planned(const void *plan, void *stream)
 int lordba_test_skip_item(int item)
 {
     g_test_skip_item.store(item, std::memory_order_relaxed);
+    return LORDBA_OK;
+}
+
+// Test-hooks build only: while on, the streaming product kernel's residency queries answer as if they had failed.
+int lordba_test_fail_queries(int on)
+{
+    g_test_fail_queries.store(on != 0, std::memory_order_relaxed);
     return LORDBA_OK;
 }
 #endif

@@ -33,6 +33,10 @@ constexpr long long kWaitLimitCycles = 1500000000LL;
 // nothing in flight.  Always -1 in the product library.
 int test_skip_item();
 
+// Test-hooks build only: whether the streaming product kernel's residency queries are to be taken as failed.  Always
+// false in the product library.
+bool test_fail_queries();
+
 // Every kernel launch of the library goes through this counter.
 void count_launch(int n = 1);
 

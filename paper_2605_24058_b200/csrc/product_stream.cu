@@ -533,27 +533,29 @@ const void *kernel_of(Form form, bool loose)
     }
 }
 
-// Clusters of 1 ... 8 CTAs, one CTA an SM, that fit the device at once ([split]; 0: the query failed).  For a
-// kernel that allocates TMEM the query never counts more than one CTA an SM, whatever its size; two of this
-// kernel's were seen to run side by side where its shared memory allows it, so the caller multiplies.  The query
-// is slow: asked once for each device and kernel.
+// Clusters of 1 ... 8 CTAs, one CTA an SM, that fit the device at once ([split]; 0: none, or the query failed).  For a
+// kernel that allocates TMEM the query never counts more than one CTA an SM, whatever its size; two of this kernel's
+// were seen to run side by side where its shared memory allows it, so the caller multiplies.  The query is slow, so its
+// answers are kept for each device and kernel; a failure is not kept, the next call asks again.
 struct Resident {
     int clusters[kMaxSplit + 1];
 };
 
-const Resident *resident(Form form, bool loose)
+Resident resident(Form form, bool loose)
 {
     static std::mutex mu;
     static Resident known[64][2 * (kPair16 + 1)];
-    static std::atomic<bool> asked[64][2 * (kPair16 + 1)];
+    static std::atomic<bool> answered[64][2 * (kPair16 + 1)];
+    Resident r = {};
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-    Resident &r = known[dev][2 * form + loose];
-    std::atomic<bool> &done = asked[dev][2 * form + loose];
-    if (done.load(std::memory_order_acquire)) return &r;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return r;
+    Resident &kept = known[dev][2 * form + loose];
+    std::atomic<bool> &done = answered[dev][2 * form + loose];
+    if (done.load(std::memory_order_acquire)) return kept;
     std::lock_guard<std::mutex> lock(mu);
-    if (done.load(std::memory_order_relaxed)) return &r;
+    if (done.load(std::memory_order_relaxed)) return kept;
     const void *func = kernel_of(form, loose);
+    bool all = true;
     for (int split = 1; split <= kMaxSplit; ++split) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)split, 1, 1);
@@ -564,14 +566,18 @@ const Resident *resident(Form form, bool loose)
         attr.val.clusterDim.x = (unsigned)split; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, kWhole) != cudaSuccess ||
+        if (test_fail_queries() || cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, kWhole) != cudaSuccess ||
             cudaOccupancyMaxActiveClusters(&r.clusters[split], func, &cfg) != cudaSuccess) {
             cudaGetLastError();
             r.clusters[split] = 0;
+            all = false;
         }
     }
-    done.store(true, std::memory_order_release);
-    return &r;
+    if (all) {
+        kept = r;
+        done.store(true, std::memory_order_release);
+    }
+    return r;
 }
 
 struct StreamPlan {
@@ -605,7 +611,7 @@ StreamPlan plan_stream(const Product &p)
     const int blocks = s.k_blocks * s.parts;
     const double hbm = (double)p.N * (double)p.K * e * sums * s.parts / 9.0e6;
     const double plane = (double)p.M * (double)((p.N + 3) / 4 * 16) * sums * problems;       // bytes of a group's sums
-    const Resident *res = resident(form, s.loose);
+    const Resident res = resident(form, s.loose);
     // Two CTAs an SM where two stages and the exchange fit half of its shared memory, or one; the split over a
     // cluster, and over clusters, that takes the least time.  A CTA draws its stages at what its ring holds in 0.84 us,
     // at most 174 KB/us an SM (LOOSE: it shifts 12 - 18); an end of 128 columns takes it 3.2 us (gated 1.7 times
@@ -616,7 +622,7 @@ StreamPlan plan_stream(const Product &p)
     // four 9.1, of six 10 us; gated 4096 x 11008, 64 tokens: two CTAs an SM of two stages 36 us, one of five 42).  The
     // worst choices found: gated 2560 x 6912, 64 tokens, 22 us where 18 were possible; dx of 4096 x 11008, one token, 38 and 33 us.
     // Groups write their sums and another kernel reads them.
-    for (int per_sm = s.loose ? 1 : 2; res && per_sm >= 1; --per_sm) {
+    for (int per_sm = s.loose ? 1 : 2; per_sm >= 1; --per_sm) {
         const int room = per_sm == 2 ? half : whole;
         int stages, raw_stages = 0, used;
         if (s.loose) {
@@ -629,7 +635,7 @@ StreamPlan plan_stream(const Product &p)
         }
         if (stages < 2 || exchange > room) continue;
         for (int n = 1; n <= kMaxSplit && n <= blocks; ++n) {
-            const int fit = per_sm * res->clusters[n];
+            const int fit = per_sm * res.clusters[n];
             if (fit < 1) continue;
             for (int g = 1; g <= 16 && n * g * (g > 1 ? 4 : 1) <= blocks && (g == 1 || g * plane < 64e6); g *= 2) {
                 const double rounds = (double)((work * g + fit - 1) / fit), steps = (double)((blocks + n * g - 1) / (n * g));
