@@ -92,7 +92,7 @@ typedef enum {
 } lordba_variant;
 
 /* One adapted projection for the _ex and _batched entry points.  ldx / ldy are
- * row pitches in elements (ldx >= d_in, ldy >= d_out). */
+ * row pitches in elements (ldx >= d_in, ldy >= d_out).  Elements of y behind a row's d_out are not written. */
 typedef struct lordba_proj {
     const void     *x;          /* [device] T x d_in,  pitch ldx                */
     const uint32_t *packed_A;   /* [device] role-0 words of A_sign (r x d_in)   */

@@ -25,7 +25,8 @@
 //               lone CTA writes z = s_r * u straight into its own buffer.
 //               After stage 2 (two groups of four warps on alternate chunks): y
 //               tile (already in the slot) += s_out * V in fp32, rounded once to
-//               bf16 in place, TMA-stored from the same slot.
+//               bf16 in place, TMA-stored from the same slot (a row's last d_out % 8
+//               elements, less than the copy engine writes at a time, by hand).
 //
 // Two-envelope adapters (Def. 1 / Eq. 4, ell = 2, ell * r <= 64) run in the instantiation L = 2:
 // both envelopes use the same carriers, so W1 carries every sign under each envelope's s_in
@@ -62,7 +63,7 @@ constexpr int kGenGroups = 2;             // the groups take alternate chunks, s
 constexpr int kGenThreads = kGenGroups * kGenGroupThreads;   // warps 2-9
 constexpr int kEpiThreads = 256;          // warps 10-17
 constexpr int kThreads = 64 + kGenThreads + kEpiThreads;
-constexpr int kMaxTcBatch = 96;          // 96 x 320 bytes of descriptors: inside the 32 KiB of kernel parameters
+constexpr int kMaxTcBatch = 96;          // 96 x 336 bytes of descriptors: inside the 32 KiB of kernel parameters
 constexpr int kMaxTcEll = 2;            // envelopes per adapter this kernel takes (ell * r <= kMaxRank)
 constexpr int kTmemU = 0;               // stage-1 accumulator columns [0, 2 ell r)
 constexpr int kTmemV = 128;             // stage-2 accumulators: two buffers of ell x 64 columns
@@ -90,8 +91,17 @@ struct alignas(64) TcProj {
     int tile_start;        // index of this projection's first tile among the launch's tiles
 };
 
+// The copy engine writes whole 16-byte pieces.  Where d_out is no multiple of 8 the maps of y end with the last
+// whole piece of a row, and the elements beyond it are read and written one by one: what lies behind the row stays.
+struct TcTail {
+    uint16_t *y;
+    uint32_t ldy8;         // row pitch of y / 8 elements
+    int rows;              // token rows
+};
+
 struct TcBatch {
     TcProj p[kMaxTcBatch];
+    TcTail tail[kMaxTcBatch];      // used where d_out % 8 != 0
     int n_proj;
     int total_tiles;       // projections may differ in their token counts (tile_start of each)
     int r;                 // rank, multiple of 8
@@ -105,6 +115,8 @@ struct TcBatch {
     int skip_item;         // -1; the test-hooks build can name one chunk whose copy requests are left out
     int *status;
 };
+
+static_assert(sizeof(TcBatch) <= 32764, "kernel parameters");
 
 // ---- shared-memory plan (offsets from a 1024-byte aligned base), same on host and device ----
 constexpr int kOps = 3;    // operand buffers (generated W1 / W2 tiles), a ring of their own
@@ -381,6 +393,28 @@ __device__ __forceinline__ void split_range(int n, int parts, int idx, int &begi
     const int base = n / parts, rem = n % parts;
     begin = idx * base + (idx < rem ? idx : rem);
     end = begin + base + (idx < rem ? 1 : 0);
+}
+
+// The last elements of a row of y, which the maps leave out: from memory into their 16-byte piece of the slot, and back.
+__device__ __forceinline__ uint4 *tail_piece(uint8_t *ytile, int row, int d_out)
+{
+    return reinterpret_cast<uint4 *>(ytile + row * 128 + (((d_out % kChunk / 8) ^ (row & 7)) * 16));
+}
+__device__ __noinline__ void tail_load(uint8_t *ytile, int row, const TcTail &q, int t0, int d_out)
+{
+    const uint16_t *y = q.y + (int64_t)(t0 + row) * 8 * q.ldy8 + d_out / 8 * 8;
+    uint16_t v[8];
+    for (int i = 0; i < 8; ++i) v[i] = i < d_out % 8 ? y[i] : (uint16_t)0;
+    *tail_piece(ytile, row, d_out) = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
+                                                v[6] | (uint32_t)v[7] << 16);
+}
+__device__ __noinline__ void tail_store(uint8_t *ytile, int row, const TcTail &q, int t0, int d_out)
+{
+    uint16_t *y = q.y + (int64_t)(t0 + row) * 8 * q.ldy8 + d_out / 8 * 8;
+    const uint4 w = *tail_piece(ytile, row, d_out);
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    for (int i = 0; i < 8; ++i)
+        if (i < d_out % 8) y[i] = (uint16_t)(v[i / 2] >> 16 * (i & 1));
 }
 
 // ------------------------------------------------------------------------------------ the kernel
@@ -857,6 +891,10 @@ tc_forward_kernel(const __grid_constant__ TcBatch B)
             // buffer g.  A thread handles all 64 columns of its token row.
             const int egroup = chalf;
             const bool store_thread = (e & (kEpiThreads / 2 - 1)) == 0;
+            // the chunk in which the row has elements that the maps leave out; the one in which it has no others
+            const bool has_tail = (P.d_out & 7) != 0;
+            const int tail_chunk = has_tail && row_valid && t0 + row < B.tail[pi].rows ? P.d_out / kChunk : -1;
+            const int bare_chunk = has_tail && P.d_out % kChunk < 8 ? P.d_out / kChunk : -1;
             int prev_slot = -1;
             RingPos rp;
             rp.set(it, S);
@@ -870,6 +908,7 @@ tc_forward_kernel(const __grid_constant__ TcBatch B)
                 tc_fence_after();
                 uint8_t *ytile = sm + s * plan.slot_stride;
                 const float *so = reinterpret_cast<const float *>(ytile + plan.slot_data);
+                if (c == tail_chunk) tail_load(ytile, row, B.tail[pi], t0, P.d_out);
                 if (warp_has_rows && L == 2) {
                     // two envelopes: y += s_out[0] * V_0 + s_out[1] * V_1, 16 columns at a time
 #pragma unroll
@@ -958,13 +997,14 @@ tc_forward_kernel(const __grid_constant__ TcBatch B)
                 } else {
                     mbar_arrive(bar_v_empty(vb));
                 }
+                if (c == tail_chunk && !*abort_flag) tail_store(ytile, row, B.tail[pi], t0, P.d_out);
                 fence_proxy_async();
                 asm volatile("bar.sync %0, %1;" ::"r"(1 + 3 * egroup), "n"(kEpiThreads / 2) : "memory");
                 if (store_thread) {
                     // a CTA in which any wait gave up writes nothing more: what sits in the slot may be
                     // built on incomplete sums (the flag was raised before anything that depends on the
                     // missing data could reach this point)
-                    if (!*abort_flag) tma_store_2d(&P.y_map, sm_base + s * plan.slot_stride, c * kChunk, t0);
+                    if (!*abort_flag && c != bare_chunk) tma_store_2d(&P.y_map, sm_base + s * plan.slot_stride, c * kChunk, t0);
                     bulk_commit();
                     if (prev_slot >= 0) {
                         bulk_wait_read_1();
@@ -1156,6 +1196,7 @@ bool tc_supported(const lordba_proj &p, int64_t T, int dtype)
     if (p.d_in > (1 << 30) || p.d_out > (1 << 30) || T > (1 << 30)) return false;
     if (reinterpret_cast<uintptr_t>(p.x) % 16 || reinterpret_cast<uintptr_t>(p.y) % 16) return false;
     if (p.ldx % 8 || p.ldy % 8) return false;
+    if (p.d_out % 8 && p.ldy / 8 > UINT32_MAX) return false;      // TcTail
     // the raw scales and sign bytes of a chunk travel as bulk copies: 16-byte aligned sources
     if (reinterpret_cast<uintptr_t>(p.s_in) % 16 || reinterpret_cast<uintptr_t>(p.s_out) % 16 ||
         reinterpret_cast<uintptr_t>(p.packed_A) % 16 || reinterpret_cast<uintptr_t>(p.packed_B) % 16)
@@ -1264,8 +1305,9 @@ int launch_forward_tc(const lordba_proj *projs, const int64_t *tokens, int64_t T
                 const int64_t rows = rows_of(tokens, T, all[first + k]);
                 TcProj &t = b.p[k];
                 if (!make_map(&t.x_map, q.x, rows, q.d_in, q.ldx, shape.tile_rows) ||
-                    !make_map(&t.y_map, q.y, rows, q.d_out, q.ldy, shape.tile_rows))
+                    !make_map(&t.y_map, q.y, rows, q.d_out / 8 * 8, q.ldy, shape.tile_rows))
                     return LORDBA_EUNSUPPORTED;
+                if (q.d_out % 8) b.tail[k] = TcTail{static_cast<uint16_t *>(q.y), (uint32_t)(q.ldy / 8), (int)rows};
                 t.packed_A = q.packed_A; t.packed_B = q.packed_B;
                 t.s_in = q.s_in; t.s_r = q.s_r; t.s_out = q.s_out;
                 t.d_in = (int)q.d_in; t.d_out = (int)q.d_out;
