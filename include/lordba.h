@@ -389,7 +389,12 @@ int lordba_int8_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ldq
                               int64_t d, int dtype, void *stream);
 /* Bytes of workspace the call needs: [device], 256-byte aligned; 0 for most calls (the workspace may then be
  * NULL), not 0 where operands are copied or a long sum with few results is split and joined.  LORDBA_EINVAL
- * from the call when the workspace given is shorter. */
+ * from the call when the workspace given is shorter.
+ *
+ * The answer holds for the very call: the query wants the struct as the call will get it, every pointer (NULL counts as
+ * aligned, and what is NULL is not made) and every pitch, with the same current device.  Another slice of the same
+ * shape may need another size, because alignment decides on copies and on the kernel.  This goes for the queries of
+ * lordba_gated_forward and lordba_gated_backward too. */
 size_t lordba_int8_linear_workspace_bytes(const lordba_int8_proj *p, int64_t T);
 int lordba_int8_linear(const lordba_int8_proj *p, int64_t T, int dtype, void *workspace, size_t workspace_bytes,
                        void *stream);
