@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -51,10 +52,16 @@ void check(int status, const char *where)
 
 using at::Tensor;
 
+// The calls record no graph: as torch's own functions with an output argument, they refuse a tensor that asks for a
+// gradient while gradients are recorded, rather than lose it.
 const Tensor &tensor(PyObject *o, const char *what)
 {
     if (!THPVariable_Check(o)) type_error(std::string(what) + " must be a tensor");
-    return THPVariable_Unpack(o);
+    const Tensor &t = THPVariable_Unpack(o);
+    if (t.requires_grad() && at::GradMode::is_enabled())
+        throw Refusal{PyExc_RuntimeError, std::string(what) + " requires a gradient, and this call records none: make it under "
+                                              "torch.no_grad(), in a torch.autograd.Function, or on detached tensors"};
+    return t;
 }
 std::optional<Tensor> optional_tensor(PyObject *o, const char *what)
 {
@@ -181,6 +188,14 @@ struct Workspace {
     }
 };
 
+// Autograd's note that a tensor was written, for the caller's own ones (those made here have not been seen by it).
+void written(PyObject *o)
+{
+    if (o == Py_None) return;
+    const Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 void *data(const std::optional<Tensor> &t) { return t ? t->data_ptr() : nullptr; }
 
 int64_t integer(PyObject *o)
@@ -234,6 +249,7 @@ PyObject *int8_quantize_rows(PyObject *const *a)
     vector(*scale, T, at, "scale");
     check(lib.quantize(x.data_ptr(), ldx, static_cast<int8_t *>(q->data_ptr()), ldq, static_cast<float *>(scale->data_ptr()), T, d,
                        dtype, at.stream), "lordba_int8_quantize_rows");
+    for (int i : {1, 2}) written(a[i]);
     return tuple_of(q, scale);
 }
 
@@ -261,6 +277,7 @@ PyObject *int8_linear(PyObject *const *a)
     p.y = y->data_ptr();
     const Workspace ws(lib.linear_bytes(&p, T), a[6], at);
     check(lib.linear(&p, T, code, ws.p, ws.bytes, at.stream), "lordba_int8_linear");
+    written(a[4]);
     return wrapped(y);
 }
 
@@ -311,6 +328,7 @@ PyObject *gated_forward(PyObject *const *a)
     g.gate_add = data(gate_add); g.up_add = data(up_add); g.gate = data(gate); g.up = data(up); g.h = h->data_ptr();
     const Workspace ws(lib.gated_bytes(&g, T), a[12], at);
     check(lib.gated(&g, T, code, ws.p, ws.bytes, at.stream), "lordba_gated_forward");
+    for (int i : {3, 9, 10}) written(a[i]);
     return tuple_of(h, gate, up);
 }
 
@@ -364,6 +382,7 @@ PyObject *gated_backward(PyObject *const *a)
     g.dgate = data(dgate); g.dup = data(dup); g.dx = data(dx); g.dw_gate = data(dw_gate); g.dw_up = data(dw_up);
     const Workspace ws(lib.grad_bytes(&g, T), a[12], at);
     check(lib.grad(&g, T, code, ws.p, ws.bytes, at.stream), "lordba_gated_backward");
+    for (int i : {6, 7, 8, 9, 10}) written(a[i]);
     return tuple_of(dgate, dup, dx, dw_gate, dw_up);
 }
 
@@ -385,6 +404,7 @@ PyObject *dropout(PyObject *const *a)
     const int64_t ldo = pitch(*out, T, d, type, at, "out");
     check(lib.dropout(x.data_ptr(), ldx, data(residual), ldr, out->data_ptr(), ldo, T, d, (float)p, seed, offset, code, at.stream),
           "lordba_dropout");
+    written(a[5]);
     return wrapped(out);
 }
 

@@ -461,7 +461,10 @@ def int8_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale:
     """Activations (T, d) in bfloat16, float16 or float32 -> (q, scale): int8 rows and one float32 scale a row,
     scale = max|row| / 127, q = round(row * 127 / max|row|) (ties to even).  q and scale are made here if absent
     (q with rows on 16-byte boundaries, as int8_linear likes them best) and belong, like all tensors that the calls
-    below make, to the stream the call runs on."""
+    below make, to the stream the call runs on.
+
+    This call and the ones below record no graph: while gradients are recorded they refuse tensors that require one
+    (RuntimeError), and autograd is told of the given tensors that they write."""
     return _native().int8_quantize_rows(x, q, scale, stream)
 
 

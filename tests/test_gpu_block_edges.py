@@ -1,5 +1,5 @@
 """Calls of the operators next to the adapters at the edges of what they take: pre-activations that are not finite, very many
-columns."""
+columns, tensors that autograd watches."""
 import math
 
 import pytest
@@ -79,3 +79,51 @@ def test_dx_of_few_tokens_and_very_many_columns():
             tol = 2 * n * 2.0 ** -23 * size
             tol = tol + 2.0 ** -8 * (want.abs() + tol)
             assert ((dx[:, first:first + (1 << 20)].double() - want).abs() <= tol).all()
+
+
+# ------------------------------------------------------------------------------ autograd
+
+def test_calls_do_not_lose_a_gradient_silently():
+    """The calls record no graph: with gradients on they refuse tensors that ask for one, as torch's functions with an
+    output argument do; without, and on detached tensors, they run."""
+    w = torch.randn(32, 64, device="cuda").to(torch.bfloat16)
+    x = torch.randn(4, 64, device="cuda").to(torch.bfloat16)
+    h = torch.zeros(4, 32, dtype=torch.bfloat16, device="cuda")
+    asks = lambda t: t.detach().clone().requires_grad_(True)
+    q, s = lordba.int8_quantize_rows(x)
+    w8, sw = lordba.int8_quantize_rows(w)
+    calls = [lambda f: lordba.gated_forward(f(x), w, w), lambda f: lordba.gated_forward(x, f(w), w), lambda f: lordba.gated_forward(x, w, w, gate_add=h, up_add=f(h)),
+             lambda f: lordba.gated_forward(q, w8, w8, scales=(s, f(sw), sw)), lambda f: lordba.gated_backward(h, h, f(h)), lambda f: lordba.dropout(f(x), 0.1, 1),
+             lambda f: lordba.dropout(x, 0.1, 1, out=f(x)), lambda f: lordba.int8_quantize_rows(f(x)), lambda f: lordba.int8_linear(q, s, w8, f(sw))]
+    for call in calls:
+        with pytest.raises(RuntimeError):
+            call(asks)
+        with torch.no_grad():
+            call(asks)
+        call(lambda t: t.detach().clone())
+
+
+def test_writes_into_given_buffers_are_seen_by_autograd():
+    """A tensor that autograd keeps and a call overwrites: torch's own check finds it."""
+    x = torch.randn(4, 64, device="cuda")
+    leaf = torch.randn(4, 64, device="cuda", requires_grad=True)
+    y = (leaf * x).sum()
+    before = x._version
+    lordba.dropout(x, 0.5, 1, out=x)
+    assert x._version > before
+    with pytest.raises(RuntimeError):
+        y.backward()
+    b = lambda *shape: torch.zeros(*shape, dtype=torch.bfloat16, device="cuda")
+    q8, s4 = torch.zeros(4, 64, dtype=torch.int8, device="cuda"), torch.zeros(4, device="cuda")
+    w8, s32 = torch.ones(32, 64, dtype=torch.int8, device="cuda"), torch.ones(32, device="cuda")
+    h, g, u, y8 = b(4, 32), b(4, 32), b(4, 32), b(4, 32)
+    dg, du, dx, dwg, dwu = b(4, 32), b(4, 32), b(4, 64), b(32, 64), b(32, 64)
+    lordba.int8_quantize_rows(b(4, 64), q=q8, scale=s4)
+    lordba.int8_linear(q8, s4, w8, s32, y8)
+    lordba.gated_forward(b(4, 64), b(32, 64), b(32, 64), h=h, gate=g, up=u)
+    lordba.gated_backward(h, g, u, b(4, 64), b(32, 64), b(32, 64), dg, du, dx, dwg, dwu)
+    assert all(t._version == 1 for t in (h, g, u, y8, q8, s4, dg, du, dx, dwg, dwu))
+    with torch.inference_mode():
+        lordba.dropout(torch.ones(4, 8, device="cuda"), 0.5, 1, out=torch.ones(4, 8, device="cuda"))
+        kept = torch.ones(4, 8, device="cuda")
+    lordba.dropout(torch.ones(4, 8, device="cuda"), 0.5, 1, out=kept)             # an inference tensor has no version
