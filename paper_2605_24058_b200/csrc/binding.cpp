@@ -69,6 +69,12 @@ std::optional<Tensor> optional_tensor(PyObject *o, const char *what)
     return tensor(o, what);
 }
 
+at::ScalarType dtype_of(PyObject *o)
+{
+    if (!THPDtype_Check(o)) type_error("dtype must be a torch.dtype");
+    return reinterpret_cast<THPDtype *>(o)->scalar_type;
+}
+
 std::string name_of(at::ScalarType t) { return c10::toString(t); }
 
 int code_of(at::ScalarType t, const char *what)
@@ -257,12 +263,12 @@ PyObject *int8_linear(PyObject *const *a)
 {
     const Tensor &x = tensor(a[0], "x"), &s_x = tensor(a[1], "s_x"), &w = tensor(a[2], "w"), &s_w = tensor(a[3], "s_w");
     std::optional<Tensor> y = optional_tensor(a[4], "y");
-    if (!THPDtype_Check(a[5])) type_error("dtype must be a torch.dtype");
+    const at::ScalarType wanted = dtype_of(a[5]);
     const Where at(a[7]);
     check_matrix(x, "x");
     check_matrix(w, "w");
     const int64_t T = x.size(0), d_in = x.size(1), d_out = w.size(0);
-    const at::ScalarType type = y ? y->scalar_type() : reinterpret_cast<THPDtype *>(a[5])->scalar_type;
+    const at::ScalarType type = y ? y->scalar_type() : wanted;
     const int code = code_of(type, "y");
     lordba_int8_proj p = {};
     p.d_in = d_in; p.d_out = d_out;
@@ -302,15 +308,10 @@ PyObject *gated_forward(PyObject *const *a)
         g.s_gate = vector(tensor(PyTuple_GET_ITEM(a[5], 1), "s_gate"), n, at, "s_gate");
         g.s_up = vector(tensor(PyTuple_GET_ITEM(a[5], 2), "s_up"), n, at, "s_up");
         g.flags = LORDBA_GATED_INT8;
-        if (h) {
-            type = h->scalar_type();
-        } else if (a[6] == Py_None) {
-            type = at::kBFloat16;
-        } else {
-            if (!THPDtype_Check(a[6])) type_error("dtype must be a torch.dtype");
-            type = reinterpret_cast<THPDtype *>(a[6])->scalar_type;
-        }
+        type = h ? h->scalar_type() : a[6] != Py_None ? dtype_of(a[6]) : at::kBFloat16;
     }
+    if (a[6] != Py_None && dtype_of(a[6]) != type)
+        type_error("dtype is " + name_of(dtype_of(a[6])) + ", but h is " + name_of(type) + (h ? "" : ", like x"));
     const int code = code_of(type, "h");
     g.d_in = d_in; g.d_hidden = n;
     g.act = (int32_t)integer(a[4]);

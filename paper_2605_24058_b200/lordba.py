@@ -483,7 +483,8 @@ def gated_forward(x, w_gate, w_up, h: Optional[torch.Tensor] = None, act: int = 
     """(h, gate, up) with g = x w_gate^T + gate_add, u = x w_up^T + up_add, h = act(g) u, in one kernel.
 
     x (T, d_in), w_gate and w_up (d_hidden, d_in): bfloat16 or float16, or int8 with ``scales`` = (s_x, s_gate,
-    s_up) and ``dtype`` the type of the rest (bfloat16 if not given).  gate_add / up_add: what the adapters of the
+    s_up) and ``dtype`` the type of the rest (h's if it is given, else bfloat16 if not given); a ``dtype`` that the
+    result will not have is refused.  gate_add / up_add: what the adapters of the
     two projections add.  save=True (or gate and up given) stores g and u for gated_backward; otherwise gate and
     up come back as None."""
     return _native().gated_forward(x, w_gate, w_up, h, act, scales, dtype, gate_add, up_add, gate, up, save, workspace, stream)

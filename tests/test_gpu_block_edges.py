@@ -127,3 +127,18 @@ def test_writes_into_given_buffers_are_seen_by_autograd():
         lordba.dropout(torch.ones(4, 8, device="cuda"), 0.5, 1, out=torch.ones(4, 8, device="cuda"))
         kept = torch.ones(4, 8, device="cuda")
     lordba.dropout(torch.ones(4, 8, device="cuda"), 0.5, 1, out=kept)             # an inference tensor has no version
+
+
+def test_a_type_that_the_result_will_not_have_is_refused():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros(32, 64, dtype=torch.bfloat16, device="cuda")
+    assert lordba.gated_forward(x, w, w, dtype=torch.bfloat16)[0].dtype == torch.bfloat16
+    with pytest.raises(TypeError):
+        lordba.gated_forward(x, w, w, dtype=torch.float16)
+    (q, s), (w8, sw) = lordba.int8_quantize_rows(x), lordba.int8_quantize_rows(w)
+    h = torch.zeros(4, 32, dtype=torch.float16, device="cuda")
+    assert lordba.gated_forward(q, w8, w8, h=h, scales=(s, sw, sw))[0] is h
+    with pytest.raises(TypeError):
+        lordba.gated_forward(q, w8, w8, h=h, scales=(s, sw, sw), dtype=torch.bfloat16)
+    with pytest.raises(TypeError):
+        lordba.gated_forward(x, w, w, dtype="bfloat16")
