@@ -477,4 +477,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods, nul
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__block(void) { return PyModule_Create(&module); }
+// made_for: the interpreter and the torch that the module was compiled against
+PyMODINIT_FUNC PyInit__block(void)
+{
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "made_for", MADE_FOR) != 0) Py_CLEAR(m);
+    return m;
+}

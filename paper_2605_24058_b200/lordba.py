@@ -151,7 +151,14 @@ def _native():
     global _block
     if _block is None:
         load()
-        from . import _block as module
+        again = "run `python -m paper_2605_24058_b200.build`"
+        try:
+            from . import _block as module
+        except ImportError as e:
+            raise RuntimeError("the module _block is not built for this Python and torch (%s); %s" % (e, again)) from e
+        from . import build
+        if module.made_for != build.binding_made_for():
+            raise RuntimeError("the module _block was built for %s, this is %s; %s" % (module.made_for, build.binding_made_for(), again))
         module.bind(LIB_PATH, LordbaError)
         _block = module
     return _block
