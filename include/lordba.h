@@ -480,6 +480,173 @@ int lordba_gated_backward(const lordba_gated_grad *g, int64_t T, int dtype, void
 int lordba_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr, void *out, int64_t ldo, int64_t T,
                    int64_t d, float p, uint64_t seed, uint64_t offset, int dtype, void *stream);
 
+/*
+ * ---- The frozen base projection in 4-bit integers with group scales --------------------------------
+ *
+ * w[n,k] = scale[n, k/group] * (u[n,k] - zero[n, k/group]),  u = 0 ... 15, zero = 8 where it is NULL: a
+ * weight matrix (d_out x d_in) of which `group` neighbouring columns of a row share a scale.
+ *
+ *     lordba_int4_linear             y[t,n]  = sum_k x[t,k] w[n,k]
+ *     lordba_int4_linear_backward    dx[t,k] = sum_n dy[t,n] w[n,k]
+ *
+ * The first is a base output of Eq. 2 over a 4-bit base, to which the adapter forward adds its term; the
+ * second is the gradient that the frozen projection hands down to its input.
+ *
+ * The carrier q: blocks of 128 columns, 64 bytes each, ceil(d_in / 128) blocks a row.  A block is sixteen
+ * little-endian 32-bit words; word 4 t + j (t, j = 0 ... 3) holds columns 32 j + 8 t ... 32 j + 8 t + 7 of
+ * the block, column c of these eight in bits 4 (c / 2) + 16 (c % 2) ... + 3.  So a 16-byte piece holds
+ * every fourth run of eight columns, and a word masked with 0x000f000f << 4 i is a pair of neighbours.
+ * What stands in columns from d_in on is not looked at.  q lies on a 16-byte boundary and its pitch is a
+ * multiple of 16 bytes (LORDBA_EALIGN).
+ *
+ * group: a power of two, at least 32; a group of at least d_in columns is one scale a row.  scale and zero
+ * are d_out x ceil(d_in / group), row-major with pitches of their own.  scale has the type of x and y; of
+ * a zero's byte the low four bits count.
+ *
+ * dtype: LORDBA_BF16 or LORDBA_F16, the type of the activations, the results and the scales (LORDBA_F32 is
+ * LORDBA_EUNSUPPORTED).  Every sum is float32, results are rounded once.  A call of few tokens multiplies
+ * the integers themselves (they are exact in 16 bits) and scales the sum of each group; one of many tokens
+ * multiplies weights that were rounded to the type of x, because that is what the tensor cores take (the
+ * error of y is then up to 1.4 times that of rounding y alone).  A scale that is not finite spoils its
+ * row of y (of dx: the columns of its group) and nothing else.  T = 0 is a no-op.
+ */
+typedef struct lordba_int4_proj {
+    const void    *in;          /* [device] x, T x d_in  (backward: dy, T x d_out), pitch ld_in                  */
+    void          *out;         /* [device] y, T x d_out (backward: dx, T x d_in), pitch ld_out, overwritten     */
+    const uint8_t *q;           /* [device] carrier, d_out rows, pitch ldq bytes                                 */
+    const void    *scale;       /* [device] d_out x groups, pitch ld_scale                                       */
+    const uint8_t *zero;        /* [device] d_out x groups, pitch ld_zero, or NULL                               */
+    int64_t d_in, d_out, ld_in, ld_out, ldq, ld_scale, ld_zero;
+    int32_t group, flags;       /* flags: 0                                                                      */
+} lordba_int4_proj;
+
+/* Bytes of a row of the carrier: 64 for each 128 columns begun (-1 on a bad size). */
+int64_t lordba_int4_row_bytes(int64_t d_in);
+
+/* values (d_out x d_in bytes, of which the low four bits count) -> the carrier. */
+int lordba_int4_pack(const uint8_t *values, int64_t ldv, uint8_t *q, int64_t ldq, int64_t d_out, int64_t d_in, void *stream);
+
+/*
+ * Weights -> carrier, scales and, where zero is not NULL, zeros; wdtype: the type of w, dtype that of scale
+ * (LORDBA_BF16 or LORDBA_F16).  Of a group, in float32:
+ *
+ *     without zeros   scale = max |w| / 7               u = 8 + rint(w / scale)
+ *     with zeros      scale = (max(w, 0) - min(w, 0)) / 15,  zero = rint(-min(w, 0) / scale),  u = zero + rint(w / scale)
+ *
+ * scale is rounded to its type first, zero and u are what the rounded scale gives (exact quotients, ties to
+ * even), clamped to 0 ... 15.  A group whose scale rounds to zero gets u = 8 (zero = 8) throughout, and scale 0; one
+ * that holds an infinity or a NaN, or whose scale overflows, the same with scale NaN.
+ */
+int lordba_int4_quantize(const void *w, int64_t ldw, int wdtype, uint8_t *q, int64_t ldq, void *scale, int64_t ld_scale,
+                         uint8_t *zero, int64_t ld_zero, int64_t d_out, int64_t d_in, int group, int dtype, void *stream);
+
+/* The weights that p's carrier, scales and zeros stand for, rounded to dtype: out is d_out x d_in, pitch ld_out (in is
+ * not looked at).  A base's rest, which an adapter is fitted to, is the original less these. */
+int lordba_int4_dequantize(const lordba_int4_proj *p, int dtype, void *stream);
+
+/* Workspace as for lordba_int8_linear: the queries answer for the call with the very pointers and pitches. */
+size_t lordba_int4_linear_workspace_bytes(const lordba_int4_proj *p, int64_t T);
+int lordba_int4_linear(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t lordba_int4_linear_backward_workspace_bytes(const lordba_int4_proj *p, int64_t T);
+int lordba_int4_linear_backward(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
+/*
+ * ---- Norms of queries and keys, and the rotation by position -----------------------------------------
+ *
+ * What happens to the results of the query and key projections before attention, for every head vector x of
+ * d entries (queries and keys in one launch):
+ *
+ *     n_i = x_i w_i / sqrt(mean_j x_j^2 + eps)                          (LORDBA_ROPE_NO_NORM: n = x)
+ *     y_a = n_a cos(f) - n_b sin(f),  y_b = n_b cos(f) + n_a sin(f),    f = positions[t] * inv_freq[i]
+ *
+ * for the pairs (a, b) = (i, i + rotary/2), or (2 i, 2 i + 1) with LORDBA_ROPE_INTERLEAVED, i < rotary/2;
+ * y = n from entry `rotary` on.  rotary = 0 is the norm alone.  The angle is the exact product, reduced in
+ * 64 bits: positions of any size are good.  Everything else is float32, y is rounded once.
+ *
+ * Tensors are [token][head][entry] with any distances between tokens and between heads and the entries
+ * side by side (slices of a joint projection's output are read in place).  q_out may be q and k_out may be
+ * k with the same distances; otherwise outputs meet nothing.  heads_k = 0: there are no keys, and
+ * nothing of theirs is looked at.  w_q, w_k: d values of type w_dtype, or NULL for ones.  d <= LORDBA_ROPE_MAX_D.
+ * dtype: all of q, k, q_out, k_out: LORDBA_BF16, LORDBA_F16 or LORDBA_F32.  T = 0 is a no-op.
+ */
+#define LORDBA_ROPE_MAX_D 512
+#define LORDBA_ROPE_NO_NORM 1
+#define LORDBA_ROPE_INTERLEAVED 2
+typedef struct lordba_heads {           /* head vectors of T tokens; distances in entries */
+    const void *p;
+    int64_t token, head;
+} lordba_heads;
+typedef struct lordba_norm_rope_args {
+    lordba_heads q, k, q_out, k_out;         /* [device]                                            */
+    const void *w_q, *w_k;                   /* [device] d values of w_dtype, or NULL               */
+    const int64_t *positions;                /* [device] T, may be negative                         */
+    const float *inv_freq;                   /* [device] rotary/2                                   */
+    int32_t heads_q, heads_k, d, rotary, w_dtype, flags;
+    float eps;
+} lordba_norm_rope_args;
+int lordba_norm_rope(const lordba_norm_rope_args *a, int64_t T, int dtype, void *stream);
+
+/*
+ * Its backward pass: f.q, f.k are the inputs of the forward call, f.q_out, f.k_out the gradients of its
+ * results (read), dq, dk receive the gradients of q and k, and dw_q, dw_k (float32, d values each, NULL where
+ * not wanted) those of w_q and w_k, summed over all tokens and heads in a fixed order and overwritten.
+ *
+ *     g = the gradient turned back by -f,  r = 1 / sqrt(mean x^2 + eps)
+ *     dw_i = sum g_i x_i r        dx = r (g w - x r^2 mean(g w x))       (without norm: dx = g)
+ *
+ * dq may be q or the gradient q_out (same distances), and dk likewise.  dw_q and dw_k need the norm (with
+ * LORDBA_ROPE_NO_NORM they must be NULL).  The workspace holds the partial sums of dw: [device], 256-byte
+ * aligned, 0 bytes where no dw is wanted.  T = 0 writes zeros into dw_q and dw_k.
+ */
+typedef struct lordba_norm_rope_grad_args {
+    lordba_norm_rope_args f;
+    lordba_heads dq, dk;
+    float *dw_q, *dw_k;
+} lordba_norm_rope_grad_args;
+size_t lordba_norm_rope_backward_workspace_bytes(const lordba_norm_rope_grad_args *a, int64_t T);
+int lordba_norm_rope_backward(const lordba_norm_rope_grad_args *a, int64_t T, int dtype, void *workspace, size_t workspace_bytes,
+                              void *stream);
+
+/*
+ * ---- Distillation from a teacher's top logits ----------------------------------------------------------
+ *
+ * The loss that an adapter over a quantised base is trained with: the divergence of the student's
+ * distribution over `vocab` classes from the teacher's, of which the `top` largest logits were kept.
+ *
+ *     p = softmax of the row's present teacher logits / temperature      lse[t] = log sum_i exp(logits[t,i] / temperature)
+ *     loss[t] = weight[t] temperature^2 sum_j p_j (log p_j - logits[t, ids[t,j]] / temperature + lse[t])
+ *     dlogits[t,i] = weight[t] temperature (exp(logits[t,i] / temperature - lse[t]) - sum over j with ids[t,j] = i of p_j)
+ *
+ * An entry is present where 0 <= ids[t,j] < vocab; an index may stand in a row more than once.  An entry
+ * of teacher logit minus infinity has p = 0 and adds nothing, whatever the student's logit.  A row without
+ * an entry of p > 0, and one of weight 0, has loss 0 and gradient 0, whatever stands in its logits.  A
+ * student's logit of minus infinity has probability 0.  Sums and exponents are float32.
+ *
+ * lordba_distill_loss writes loss and lse and, where dlogits is not NULL, the gradient in the same pass
+ * over the logits (the weights of the rows, such as 1 over the number of tokens, are then the gradients of
+ * the losses).  lordba_distill_backward makes dlogits from lse and the gradients of the losses, which it takes
+ * in `weight`; loss is not looked at.  weight may be NULL: ones.  dlogits may be logits (same pitch).
+ *
+ * dtype: logits and dlogits; teacher_dtype: teacher.  Each LORDBA_BF16, LORDBA_F16 or LORDBA_F32.  1 <= top <=
+ * LORDBA_DISTILL_MAX_TOP.  temperature > 0.  T = 0 is a no-op.
+ */
+#define LORDBA_DISTILL_MAX_TOP 256
+#define LORDBA_DISTILL_IDS_64 1
+typedef struct lordba_distill {
+    const void  *logits;        /* [device] T x vocab, pitch ld_logits                                           */
+    const void  *ids;           /* [device] T x top, pitch ld_ids: int32, or int64 with LORDBA_DISTILL_IDS_64    */
+    const void  *teacher;       /* [device] T x top, pitch ld_teacher                                            */
+    const float *weight;        /* [device] T, or NULL                                                           */
+    float       *loss, *lse;    /* [device] T (lse is read by the backward call)                                 */
+    void        *dlogits;       /* [device] T x vocab, pitch ld_dlogits, or NULL                                 */
+    int64_t vocab, top, ld_logits, ld_ids, ld_teacher, ld_dlogits;
+    float   temperature;
+    int32_t teacher_dtype, flags;
+} lordba_distill;
+int lordba_distill_loss(const lordba_distill *d, int64_t T, int dtype, void *stream);
+int lordba_distill_backward(const lordba_distill *d, int64_t T, int dtype, void *stream);
+
 /* Storage of one adapter in bits, Eq. 5: r(d_in+d_out) + 16 ell (d_in+r+d_out). */
 int64_t lordba_adapter_bits(int64_t d_in, int64_t d_out, int r, int ell);
 

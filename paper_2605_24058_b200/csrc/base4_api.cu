@@ -1,0 +1,375 @@
+// C ABI of the operators around a 4-bit base: products with 4-bit weights, norms of queries and keys with the rotation,
+// distillation.  Argument checks on the host, then launches; include/lordba.h states every contract.
+#include <cmath>
+#include <cstring>
+
+#include "block_checks.h"
+
+namespace lordba {
+namespace {
+
+// ---- 4-bit weights -----------------------------------------------------------------------------------------------
+int64_t carrier_bytes(int64_t d_in) { return (d_in + 127) / 128 * 64; }
+bool bad_group(int group) { return group < 32 || (group & (group - 1)); }
+int64_t groups_of(int64_t d_in, int group) { return (d_in + group - 1) / group; }
+
+struct Carrier {
+    Matrix q, scale, zero;
+};
+
+Carrier carrier_of(const lordba_int4_proj &p)
+{
+    const int64_t g = groups_of(p.d_in, p.group);
+    return Carrier{Matrix{p.q, p.d_out, carrier_bytes(p.d_in), p.ldq, 1}, Matrix{p.scale, p.d_out, g, p.ld_scale, 2},
+                   Matrix{p.zero, p.d_out, g, p.ld_zero, 1}};
+}
+
+int check_carrier(const lordba_int4_proj &p)
+{
+    if (bad_size(p.d_out, p.d_in) || p.d_out < 1 || bad_group(p.group) || p.flags) return LORDBA_EINVAL;
+    const int64_t g = groups_of(p.d_in, p.group);
+    if (p.ldq < carrier_bytes(p.d_in) || p.ld_scale < g || (p.zero && p.ld_zero < g)) return LORDBA_EINVAL;
+    return LORDBA_OK;
+}
+
+int check_carrier_pointers(const Carrier &c)
+{
+    int rc = check_matrix(c.q);
+    if (rc == LORDBA_OK) rc = check_matrix(c.scale);
+    if (rc != LORDBA_OK) return rc;
+    return aligned(c.q.p, 16) && c.q.ld % 16 == 0 ? LORDBA_OK : LORDBA_EALIGN;
+}
+
+int check_int4(const lordba_int4_proj &p, int64_t T, int dtype, bool backward)
+{
+    if (dtype != LORDBA_BF16 && dtype != LORDBA_F16) return LORDBA_EUNSUPPORTED;
+    int rc = check_carrier(p);
+    if (rc != LORDBA_OK) return rc;
+    const int64_t n_in = backward ? p.d_out : p.d_in, n_out = backward ? p.d_in : p.d_out;
+    if (T < 0 || T > kMaxRows || p.ld_in < n_in || p.ld_out < n_out) return LORDBA_EINVAL;
+    if (T == 0) return LORDBA_OK;
+    const Carrier c = carrier_of(p);
+    const Matrix in{p.in, T, n_in, p.ld_in, 2}, out{p.out, T, n_out, p.ld_out, 2};
+    rc = check_carrier_pointers(c);
+    if (rc == LORDBA_OK) rc = check_matrix(in);
+    if (rc == LORDBA_OK) rc = check_matrix(out);
+    if (rc != LORDBA_OK) return rc;
+    return meet(out, in) || meet(out, c.q) || meet(out, c.scale) || meet(out, c.zero) ? LORDBA_EINVAL : LORDBA_OK;
+}
+
+// The product that follows where the weights were laid out in 16 bits first (w, pitch ldw).
+Product int4_product(const lordba_int4_proj &p, int64_t T, int dtype, bool backward, const void *w, int64_t ldw)
+{
+    Product q = {};
+    q.kind = dtype == LORDBA_BF16 ? kProductBf16 : kProductF16;
+    q.form = Product::kSingle;
+    q.M = T;
+    q.N = backward ? p.d_in : p.d_out;
+    q.K = backward ? p.d_out : p.d_in;
+    q.a[0] = Operand{p.in, p.ld_in, false};
+    q.b[0] = Operand{w, ldw, backward};
+    q.out[0] = p.out; q.ldo = p.ld_out; q.dtype = dtype;
+    return q;
+}
+
+struct Int4Workspace {
+    size_t weights, bytes;       // of the weights in 16 bits; in all
+    int64_t ldw;
+};
+
+Int4Workspace int4_workspace(const lordba_int4_proj &p, int64_t T, int dtype, bool backward)
+{
+    Int4Workspace w = {};
+    w.ldw = (p.d_in + 7) / 8 * 8;
+    w.weights = ((size_t)p.d_out * (size_t)w.ldw * 2 + 255) / 256 * 256;
+    // the weights' place says only that they lie aligned
+    w.bytes = w.weights + product_workspace_bytes(int4_product(p, T, dtype, backward, reinterpret_cast<const void *>(uintptr_t(256)), w.ldw));
+    return w;
+}
+
+size_t int4_bytes(const lordba_int4_proj *p, int64_t T, bool backward)
+{
+    if (!p || check_carrier(*p) != LORDBA_OK || T <= 0 || T > kMaxRows) return 0;
+    return int4_workspace(*p, T, LORDBA_BF16, backward).bytes;
+}
+
+int int4_call(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream, bool backward)
+{
+    if (!p) return LORDBA_EINVAL;
+    int rc = check_int4(*p, T, dtype, backward);
+    if (rc != LORDBA_OK || T == 0) return rc;
+    const Int4Workspace w = int4_workspace(*p, T, dtype, backward);
+    rc = check_workspace(w.bytes, workspace, workspace_bytes);
+    if (rc != LORDBA_OK) return rc;
+    lordba_int4_proj wide = *p;
+    wide.out = workspace;
+    wide.ld_out = w.ldw;
+    rc = launch_int4_dequantize(wide, dtype, static_cast<cudaStream_t>(stream));
+    if (rc != LORDBA_OK) return rc;
+    return launch_product(int4_product(*p, T, dtype, backward, workspace, w.ldw), static_cast<uint8_t *>(workspace) + w.weights,
+                          static_cast<cudaStream_t>(stream));
+}
+
+// ---- heads --------------------------------------------------------------------------------------------------------
+// Head vectors as a matrix: a row a token (or, head by head, a row a head), from the first entry to the last.  One that is
+// neither, such as heads that share their entries, is a single row.  clear: no two vectors share an entry.
+struct Heads {
+    Matrix m;
+    bool clear;
+};
+
+Heads heads_of(const lordba_heads &h, int64_t T, int64_t heads, int64_t d, size_t e)
+{
+    const int64_t token = T > 1 ? h.token : 0, head = heads > 1 ? h.head : 0;
+    const int64_t by_token = (heads - 1) * head + d, by_head = (T - 1) * token + d;
+    if ((heads == 1 || head >= d) && (T == 1 || token >= by_token)) return Heads{Matrix{h.p, T, by_token, T > 1 ? token : by_token, e}, true};
+    if ((T == 1 || token >= d) && (heads == 1 || head >= by_head)) return Heads{Matrix{h.p, heads, by_head, heads > 1 ? head : by_head, e}, true};
+    const int64_t all = (T - 1) * token + (heads - 1) * head + d;
+    return Heads{Matrix{h.p, 1, all, all, e}, false};
+}
+
+bool same_heads(const lordba_heads &a, const lordba_heads &b, int64_t T, int64_t heads)
+{
+    return a.p == b.p && (T <= 1 || a.token == b.token) && (heads <= 1 || a.head == b.head);
+}
+
+int check_norm_rope(const lordba_norm_rope_args &a, int64_t T, int dtype)
+{
+    if (!known_dtype(dtype)) return LORDBA_EUNSUPPORTED;
+    if (a.flags & ~(LORDBA_ROPE_NO_NORM | LORDBA_ROPE_INTERLEAVED)) return LORDBA_EINVAL;
+    if (a.d < 1 || a.heads_q < 1 || a.heads_k < 0 || a.rotary < 0 || a.rotary > a.d || a.rotary % 2) return LORDBA_EINVAL;
+    if (a.d > LORDBA_ROPE_MAX_D || a.heads_q > (1 << 20) || a.heads_k > (1 << 20)) return LORDBA_EUNSUPPORTED;
+    if ((a.w_q || a.w_k) && !known_dtype(a.w_dtype)) return LORDBA_EUNSUPPORTED;
+    if ((a.flags & LORDBA_ROPE_NO_NORM) && (a.w_q || a.w_k)) return LORDBA_EINVAL;
+    if (!(a.eps >= 0.0f) || std::isinf(a.eps)) return LORDBA_EINVAL;
+    if (T < 0 || T > kMaxRows) return LORDBA_EINVAL;
+    return LORDBA_OK;
+}
+
+// Vectors read and written by a call, and plain vectors read.
+struct RopeCall {
+    struct Item {
+        const lordba_heads *h;
+        int64_t heads;
+        int side;                 // 0: queries, 1: keys
+    };
+    Item in[4], out[2];
+    int n_in, n_out;
+};
+
+int check_heads(const RopeCall &c, const lordba_norm_rope_args &a, int64_t T, int dtype, float *const *dw)
+{
+    const size_t e = elt(dtype), ew = elt(a.w_dtype);
+    constexpr int64_t kFar = int64_t(1) << 40;            // keeps every product of sizes inside 64 bits
+    for (int i = 0; i < c.n_in + c.n_out; ++i) {
+        const lordba_heads &h = i < c.n_in ? *c.in[i].h : *c.out[i - c.n_in].h;
+        if (!h.p || h.token < 0 || h.head < 0 || h.token > kFar || h.head > kFar) return LORDBA_EINVAL;
+        if (!aligned(h.p, e)) return LORDBA_EALIGN;
+    }
+    if (!a.positions || (a.rotary && !a.inv_freq)) return LORDBA_EINVAL;
+    if (!aligned(a.positions, 8) || !aligned(a.inv_freq, 4)) return LORDBA_EALIGN;
+    if ((a.w_q && !aligned(a.w_q, ew)) || (a.w_k && !aligned(a.w_k, ew))) return LORDBA_EALIGN;
+    const Matrix flat[4] = {Matrix{a.positions, 1, T, T, 8}, Matrix{a.rotary ? a.inv_freq : nullptr, 1, a.rotary / 2, a.rotary / 2, 4},
+                            Matrix{a.w_q, 1, a.d, a.d, ew}, Matrix{a.w_k, 1, a.d, a.d, ew}};
+    Matrix outs[4];
+    int n = 0;
+    for (int i = 0; i < c.n_out; ++i) {
+        const Heads h = heads_of(*c.out[i].h, T, c.out[i].heads, a.d, e);
+        if (!h.clear) return LORDBA_EINVAL;
+        outs[n++] = h.m;
+        for (int j = 0; j < c.n_in; ++j) {
+            // an input of the same side may be the output's very place
+            if (c.in[j].side == c.out[i].side && same_heads(*c.out[i].h, *c.in[j].h, T, c.out[i].heads)) continue;
+            if (meet(h.m, heads_of(*c.in[j].h, T, c.in[j].heads, a.d, e).m)) return LORDBA_EINVAL;
+        }
+    }
+    for (int i = 0; dw && i < 2; ++i)
+        if (dw[i]) {
+            if (!aligned(dw[i], 4)) return LORDBA_EALIGN;
+            const Matrix m{dw[i], 1, a.d, a.d, 4};
+            for (int j = 0; j < c.n_in; ++j)
+                if (meet(m, heads_of(*c.in[j].h, T, c.in[j].heads, a.d, e).m)) return LORDBA_EINVAL;
+            outs[n++] = m;
+        }
+    for (int i = 0; i < n; ++i) {
+        for (int j = i + 1; j < n; ++j)
+            if (meet(outs[i], outs[j])) return LORDBA_EINVAL;
+        for (const Matrix &m : flat)
+            if (meet(outs[i], m)) return LORDBA_EINVAL;
+    }
+    return LORDBA_OK;
+}
+
+int check_rope_grad(const lordba_norm_rope_grad_args &a, int64_t T, int dtype)
+{
+    const int rc = check_norm_rope(a.f, T, dtype);
+    if (rc != LORDBA_OK) return rc;
+    if (a.dw_k && !a.f.heads_k) return LORDBA_EINVAL;
+    if ((a.f.flags & LORDBA_ROPE_NO_NORM) && (a.dw_q || a.dw_k)) return LORDBA_EINVAL;
+    return LORDBA_OK;
+}
+
+// ---- distillation ---------------------------------------------------------------------------------------------------
+int check_distill(const lordba_distill &d, int64_t T, int dtype, bool backward)
+{
+    if (!known_dtype(dtype) || !known_dtype(d.teacher_dtype)) return LORDBA_EUNSUPPORTED;
+    if (d.flags & ~LORDBA_DISTILL_IDS_64) return LORDBA_EINVAL;
+    if (bad_size(T, d.vocab) || d.top < 1 || d.ld_logits < d.vocab || d.ld_ids < d.top || d.ld_teacher < d.top) return LORDBA_EINVAL;
+    if (d.top > LORDBA_DISTILL_MAX_TOP) return LORDBA_EUNSUPPORTED;
+    // its inverse, in powers of two, is a number too
+    if (!(d.temperature > 0.0f) || std::isinf(d.temperature) || std::isinf((float)(1.4426950408889634 / (double)d.temperature))) return LORDBA_EINVAL;
+    if (backward && !d.dlogits) return LORDBA_EINVAL;
+    if (d.dlogits && d.ld_dlogits < d.vocab) return LORDBA_EINVAL;
+    if (T == 0) return LORDBA_OK;
+    const size_t e = elt(dtype);
+    const Matrix z{d.logits, T, d.vocab, d.ld_logits, e}, ids{d.ids, T, d.top, d.ld_ids, size_t(d.flags & LORDBA_DISTILL_IDS_64 ? 8 : 4)},
+        teacher{d.teacher, T, d.top, d.ld_teacher, elt(d.teacher_dtype)}, lse{d.lse, 1, T, T, 4};
+    const Matrix weight{d.weight, 1, T, T, 4}, loss{backward ? nullptr : d.loss, 1, T, T, 4}, dz{d.dlogits, T, d.vocab, d.ld_dlogits, e};
+    for (const Matrix *m : {&z, &ids, &teacher, &lse, &weight, &loss, &dz}) {
+        if (!m->p && (m == &weight || (m == &loss && backward) || m == &dz)) continue;
+        const int rc = check_matrix(*m);
+        if (rc != LORDBA_OK) return rc;
+    }
+    const Matrix none{};
+    const Matrix outs[3] = {dz, loss, backward ? none : lse};
+    const Matrix ins[5] = {z, ids, teacher, weight, backward ? lse : none};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = i + 1; j < 3; ++j)
+            if (meet(outs[i], outs[j])) return LORDBA_EINVAL;
+        for (int j = 0; j < 5; ++j)
+            if (meet(outs[i], ins[j]) && !(i == 0 && j == 0 && same(dz, z))) return LORDBA_EINVAL;
+    }
+    return LORDBA_OK;
+}
+
+}  // namespace
+}  // namespace lordba
+
+using namespace lordba;
+
+extern "C" {
+
+int64_t lordba_int4_row_bytes(int64_t d_in) { return d_in < 1 || d_in > kMaxRows ? -1 : carrier_bytes(d_in); }
+
+int lordba_int4_pack(const uint8_t *values, int64_t ldv, uint8_t *q, int64_t ldq, int64_t d_out, int64_t d_in, void *stream)
+{
+    if (bad_size(d_out, d_in) || ldv < d_in || ldq < carrier_bytes(d_in)) return LORDBA_EINVAL;
+    if (d_out == 0) return LORDBA_OK;
+    const Matrix v{values, d_out, d_in, ldv, 1}, c{q, d_out, carrier_bytes(d_in), ldq, 1};
+    if (!v.p || !c.p) return LORDBA_EINVAL;
+    if (!aligned(q, 16) || ldq % 16) return LORDBA_EALIGN;
+    if (meet(v, c)) return LORDBA_EINVAL;
+    return launch_int4_pack(values, ldv, q, ldq, d_out, d_in, static_cast<cudaStream_t>(stream));
+}
+
+int lordba_int4_quantize(const void *w, int64_t ldw, int wdtype, uint8_t *q, int64_t ldq, void *scale, int64_t ld_scale, uint8_t *zero,
+                         int64_t ld_zero, int64_t d_out, int64_t d_in, int group, int dtype, void *stream)
+{
+    if (!known_dtype(wdtype) || (dtype != LORDBA_BF16 && dtype != LORDBA_F16)) return LORDBA_EUNSUPPORTED;
+    lordba_int4_proj p = {};
+    p.q = q; p.scale = scale; p.zero = zero;
+    p.d_in = d_in; p.d_out = d_out < 1 ? 1 : d_out; p.ldq = ldq; p.ld_scale = ld_scale; p.ld_zero = ld_zero; p.group = group;
+    int rc = check_carrier(p);
+    if (rc != LORDBA_OK) return rc;
+    if (d_out < 0 || ldw < d_in) return LORDBA_EINVAL;
+    if (d_out == 0) return LORDBA_OK;
+    const Carrier c = carrier_of(p);
+    const Matrix m{w, d_out, d_in, ldw, elt(wdtype)};
+    rc = check_carrier_pointers(c);
+    if (rc == LORDBA_OK) rc = check_matrix(m);
+    if (rc != LORDBA_OK) return rc;
+    if (meet(m, c.q) || meet(m, c.scale) || meet(m, c.zero) || meet(c.q, c.scale) || meet(c.q, c.zero) || meet(c.scale, c.zero)) return LORDBA_EINVAL;
+    return launch_int4_quantize(w, ldw, wdtype, q, ldq, scale, ld_scale, zero, ld_zero, d_out, d_in, group, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int lordba_int4_dequantize(const lordba_int4_proj *p, int dtype, void *stream)
+{
+    if (!p) return LORDBA_EINVAL;
+    if (dtype != LORDBA_BF16 && dtype != LORDBA_F16) return LORDBA_EUNSUPPORTED;
+    int rc = check_carrier(*p);
+    if (rc != LORDBA_OK) return rc;
+    if (p->ld_out < p->d_in) return LORDBA_EINVAL;
+    const Carrier c = carrier_of(*p);
+    const Matrix out{p->out, p->d_out, p->d_in, p->ld_out, 2};
+    rc = check_carrier_pointers(c);
+    if (rc == LORDBA_OK) rc = check_matrix(out);
+    if (rc != LORDBA_OK) return rc;
+    if (meet(out, c.q) || meet(out, c.scale) || meet(out, c.zero)) return LORDBA_EINVAL;
+    return launch_int4_dequantize(*p, dtype, static_cast<cudaStream_t>(stream));
+}
+
+size_t lordba_int4_linear_workspace_bytes(const lordba_int4_proj *p, int64_t T) { return int4_bytes(p, T, false); }
+
+int lordba_int4_linear(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return int4_call(p, T, dtype, workspace, workspace_bytes, stream, false);
+}
+
+size_t lordba_int4_linear_backward_workspace_bytes(const lordba_int4_proj *p, int64_t T) { return int4_bytes(p, T, true); }
+
+int lordba_int4_linear_backward(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return int4_call(p, T, dtype, workspace, workspace_bytes, stream, true);
+}
+
+int lordba_norm_rope(const lordba_norm_rope_args *a, int64_t T, int dtype, void *stream)
+{
+    if (!a) return LORDBA_EINVAL;
+    int rc = check_norm_rope(*a, T, dtype);
+    if (rc != LORDBA_OK || T == 0) return rc;
+    const int sides = a->heads_k ? 2 : 1;
+    const RopeCall c{{{&a->q, a->heads_q, 0}, {&a->k, a->heads_k, 1}, {}, {}}, {{&a->q_out, a->heads_q, 0}, {&a->k_out, a->heads_k, 1}}, sides, sides};
+    rc = check_heads(c, *a, T, dtype, nullptr);
+    return rc != LORDBA_OK ? rc : launch_norm_rope(*a, T, dtype, static_cast<cudaStream_t>(stream));
+}
+
+size_t lordba_norm_rope_backward_workspace_bytes(const lordba_norm_rope_grad_args *a, int64_t T)
+{
+    if (!a || check_rope_grad(*a, T, LORDBA_F32) != LORDBA_OK || T == 0) return 0;
+    return norm_rope_backward_bytes(*a, T);
+}
+
+int lordba_norm_rope_backward(const lordba_norm_rope_grad_args *a, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!a) return LORDBA_EINVAL;
+    int rc = check_rope_grad(*a, T, dtype);
+    if (rc != LORDBA_OK) return rc;
+    const lordba_norm_rope_args &f = a->f;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        // sums over no token
+        for (float *dw : {a->dw_q, a->dw_k}) {
+            if (!dw) continue;
+            if (!aligned(dw, 4)) return LORDBA_EALIGN;
+            if (cudaMemsetAsync(dw, 0, (size_t)f.d * 4, s) != cudaSuccess) {
+                cudaGetLastError();
+                return LORDBA_ECUDA;
+            }
+        }
+        return LORDBA_OK;
+    }
+    const int sides = f.heads_k ? 2 : 1;
+    const RopeCall c{{{&f.q, f.heads_q, 0}, {&f.q_out, f.heads_q, 0}, {&f.k, f.heads_k, 1}, {&f.k_out, f.heads_k, 1}},
+                     {{&a->dq, f.heads_q, 0}, {&a->dk, f.heads_k, 1}}, 2 * sides, sides};
+    float *const dw[2] = {a->dw_q, a->dw_k};
+    rc = check_heads(c, f, T, dtype, dw);
+    if (rc != LORDBA_OK) return rc;
+    rc = check_workspace(norm_rope_backward_bytes(*a, T), workspace, workspace_bytes);
+    return rc != LORDBA_OK ? rc : launch_norm_rope_backward(*a, T, dtype, workspace, s);
+}
+
+int lordba_distill_loss(const lordba_distill *d, int64_t T, int dtype, void *stream)
+{
+    if (!d) return LORDBA_EINVAL;
+    const int rc = check_distill(*d, T, dtype, false);
+    return rc != LORDBA_OK || T == 0 ? rc : launch_distill(*d, T, dtype, false, static_cast<cudaStream_t>(stream));
+}
+
+int lordba_distill_backward(const lordba_distill *d, int64_t T, int dtype, void *stream)
+{
+    if (!d) return LORDBA_EINVAL;
+    const int rc = check_distill(*d, T, dtype, true);
+    return rc != LORDBA_OK || T == 0 ? rc : launch_distill(*d, T, dtype, true, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -33,6 +33,16 @@ struct Library {
     decltype(&lordba_gated_backward_workspace_bytes) grad_bytes;
     decltype(&lordba_gated_backward) grad;
     decltype(&lordba_dropout) dropout;
+    decltype(&lordba_int4_row_bytes) int4_row_bytes;
+    decltype(&lordba_int4_pack) int4_pack;
+    decltype(&lordba_int4_quantize) int4_quantize;
+    decltype(&lordba_int4_dequantize) int4_dequantize;
+    decltype(&lordba_int4_linear_workspace_bytes) int4_bytes[2];      // forward, backward
+    decltype(&lordba_int4_linear) int4[2];
+    decltype(&lordba_norm_rope) rope;
+    decltype(&lordba_norm_rope_backward_workspace_bytes) rope_bytes;
+    decltype(&lordba_norm_rope_backward) rope_grad;
+    decltype(&lordba_distill_loss) distill[2];
 };
 Library lib = {};
 PyObject *status_error = nullptr;      // LordbaError
@@ -122,6 +132,8 @@ struct Where {
         return make({r, c}, {(c + step - 1) / step * step, 1}, t);
     }
     Tensor values(int64_t n, at::ScalarType t) const { return make({n}, {1}, t); }
+    Tensor plain(int64_t r, int64_t c, at::ScalarType t) const { return make({r, c}, {c, 1}, t); }
+    Tensor heads(int64_t T, int64_t h, int64_t d, at::ScalarType t) const { return make({T, h, d}, {h * d, d, 1}, t); }
 
 private:
     Tensor make(at::IntArrayRef size, at::IntArrayRef stride, at::ScalarType t) const
@@ -409,6 +421,298 @@ PyObject *dropout(PyObject *const *a)
     return wrapped(out);
 }
 
+// ---- 4-bit weights ----------------------------------------------------------------------------------------------
+
+// A carrier: its rows' pitch in bytes.
+int64_t carrier(const Tensor &q, int64_t rows, int64_t d_in, const Where &at)
+{
+    const int64_t bytes = lib.int4_row_bytes(d_in);
+    if (bytes < 0) value_error("d_in must be positive");
+    return pitch(q, rows, bytes, at::kByte, at, "q");
+}
+int64_t groups_of(int64_t d_in, int64_t group)
+{
+    if (group < 32 || group > (int64_t(1) << 30) || (group & (group - 1))) value_error("group must be a power of two, at least 32");
+    return (d_in + group - 1) / group;
+}
+// Scales and zeros of a matrix (d_out, d_in) in a call of activations of a type.
+void weights(lordba_int4_proj &p, const Tensor &q, const Tensor &scale, const std::optional<Tensor> &zero, int64_t d_in, int64_t group,
+             at::ScalarType type, const Where &at)
+{
+    check_matrix(q, "q");
+    p.d_in = d_in; p.d_out = q.size(0); p.group = (int32_t)group;
+    const int64_t g = groups_of(d_in, group);
+    p.ldq = carrier(q, p.d_out, d_in, at);
+    p.ld_scale = pitch(scale, p.d_out, g, type, at, "scale");
+    if (zero) p.ld_zero = pitch(*zero, p.d_out, g, at::kByte, at, "zero");
+    p.q = static_cast<const uint8_t *>(q.data_ptr());
+    p.scale = scale.data_ptr();
+    p.zero = static_cast<const uint8_t *>(data(zero));
+}
+
+PyObject *int4_pack(PyObject *const *a)
+{
+    const Tensor &values = tensor(a[0], "values");
+    std::optional<Tensor> q = optional_tensor(a[1], "q");
+    const Where at(a[2]);
+    check_matrix(values, "values");
+    const int64_t n = values.size(0), d = values.size(1);
+    const int64_t ldv = pitch(values, n, d, at::kByte, at, "values");
+    if (d < 1) value_error("values must have columns");
+    if (!q) q = at.rows(n, lib.int4_row_bytes(d), at::kByte);
+    const int64_t ldq = carrier(*q, n, d, at);
+    check(lib.int4_pack(static_cast<const uint8_t *>(values.data_ptr()), ldv, static_cast<uint8_t *>(q->data_ptr()), ldq, n, d, at.stream),
+          "lordba_int4_pack");
+    written(a[1]);
+    return wrapped(q);
+}
+
+PyObject *int4_quantize(PyObject *const *a)
+{
+    const Tensor &w = tensor(a[0], "w");
+    const int64_t group = integer(a[1]);
+    const int zeros = PyObject_IsTrue(a[2]);
+    if (zeros < 0) throw python_error();
+    std::optional<Tensor> q = optional_tensor(a[4], "q"), scale = optional_tensor(a[5], "scale"), zero = optional_tensor(a[6], "zero");
+    const Where at(a[7]);
+    check_matrix(w, "w");
+    const int64_t n = w.size(0), d = w.size(1), g = groups_of(d, group);
+    if (d < 1) value_error("w must have columns");
+    const int code = code_of(w.scalar_type(), "w");
+    at::ScalarType type = scale ? scale->scalar_type() : a[3] != Py_None ? dtype_of(a[3]) : w.scalar_type() == at::kHalf ? at::kHalf : at::kBFloat16;
+    if (a[3] != Py_None && dtype_of(a[3]) != type) type_error("dtype is " + name_of(dtype_of(a[3])) + ", but scale is " + name_of(type));
+    const int64_t ldw = pitch(w, n, d, w.scalar_type(), at, "w");
+    if (!q) q = at.rows(n, lib.int4_row_bytes(d), at::kByte);
+    if (!scale) scale = at.plain(n, g, type);
+    if (zeros && !zero) zero = at.plain(n, g, at::kByte);
+    const int64_t ldq = carrier(*q, n, d, at), ld_scale = pitch(*scale, n, g, type, at, "scale"), ld_zero = zero ? pitch(*zero, n, g, at::kByte, at, "zero") : 0;
+    check(lib.int4_quantize(w.data_ptr(), ldw, code, static_cast<uint8_t *>(q->data_ptr()), ldq, scale->data_ptr(), ld_scale,
+                            static_cast<uint8_t *>(data(zero)), ld_zero, n, d, (int)group, code_of(type, "scale"), at.stream), "lordba_int4_quantize");
+    for (int i : {4, 5, 6}) written(a[i]);
+    return tuple_of(q, scale, zero);
+}
+
+PyObject *int4_dequantize(PyObject *const *a)
+{
+    const Tensor &q = tensor(a[0], "q"), &scale = tensor(a[1], "scale");
+    const int64_t d_in = integer(a[2]);
+    const std::optional<Tensor> zero = optional_tensor(a[3], "zero");
+    std::optional<Tensor> w = optional_tensor(a[5], "w");
+    const Where at(a[6]);
+    const at::ScalarType type = scale.scalar_type();
+    lordba_int4_proj p = {};
+    weights(p, q, scale, zero, d_in, integer(a[4]), type, at);
+    if (!w) w = at.rows(p.d_out, d_in, type);
+    p.ld_out = pitch(*w, p.d_out, d_in, type, at, "w");
+    p.out = w->data_ptr();
+    if (p.d_out) check(lib.int4_dequantize(&p, code_of(type, "scale"), at.stream), "lordba_int4_dequantize");
+    written(a[5]);
+    return wrapped(w);
+}
+
+// in: x or dy; backward: 1 for the gradient
+PyObject *int4_product(const Tensor &in, const char *in_name, const Tensor &q, const Tensor &scale, int64_t d_in, const std::optional<Tensor> &zero,
+                       int64_t group, PyObject *out_given, const char *out_name, PyObject *workspace, PyObject *stream, int backward)
+{
+    std::optional<Tensor> out = optional_tensor(out_given, out_name);
+    const Where at(stream);
+    check_matrix(in, in_name);
+    const at::ScalarType type = in.scalar_type();
+    const int code = code_of(type, in_name);
+    lordba_int4_proj p = {};
+    weights(p, q, scale, zero, d_in, group, type, at);
+    const int64_t T = in.size(0), n = backward ? d_in : p.d_out;
+    p.ld_in = pitch(in, T, backward ? p.d_out : d_in, type, at, in_name);
+    if (!out) out = at.rows(T, n, type);
+    p.ld_out = pitch(*out, T, n, type, at, out_name);
+    p.in = in.data_ptr();
+    p.out = out->data_ptr();
+    const Workspace ws(lib.int4_bytes[backward](&p, T), workspace, at);
+    check(lib.int4[backward](&p, T, code, ws.p, ws.bytes, at.stream), backward ? "lordba_int4_linear_backward" : "lordba_int4_linear");
+    written(out_given);
+    return wrapped(out);
+}
+
+PyObject *int4_linear(PyObject *const *a)
+{
+    const Tensor &x = tensor(a[0], "x"), &q = tensor(a[1], "q"), &scale = tensor(a[2], "scale");
+    check_matrix(x, "x");
+    return int4_product(x, "x", q, scale, x.size(1), optional_tensor(a[3], "zero"), integer(a[4]), a[5], "y", a[6], a[7], 0);
+}
+
+PyObject *int4_linear_backward(PyObject *const *a)
+{
+    const Tensor &dy = tensor(a[0], "dy"), &q = tensor(a[1], "q"), &scale = tensor(a[2], "scale");
+    return int4_product(dy, "dy", q, scale, integer(a[3]), optional_tensor(a[4], "zero"), integer(a[5]), a[6], "dx", a[7], a[8], 1);
+}
+
+// ---- norms of queries and keys, rotation --------------------------------------------------------------------------
+
+// Head vectors (T, heads, d) with contiguous entries.
+lordba_heads heads_of(const Tensor &t, int64_t T, int64_t heads, int64_t d, at::ScalarType type, const Where &at, const char *what)
+{
+    if (t.scalar_type() != type) type_error(std::string(what) + " must be " + name_of(type) + ", got " + name_of(t.scalar_type()));
+    check_device(t, at, what);
+    if (t.dim() != 3 || t.size(0) != T || t.size(1) != heads || t.size(2) != d)
+        value_error(std::string(what) + " must be (" + std::to_string(T) + ", " + std::to_string(heads) + ", " + std::to_string(d) + ")");
+    if (t.stride(2) != 1 && d > 1) value_error(std::string("entries of ") + what + " must be contiguous");
+    return lordba_heads{t.data_ptr(), t.stride(0), t.stride(1)};
+}
+
+struct RopeTensors {
+    at::ScalarType type;
+    int64_t T, heads_q, heads_k, d;
+    bool keys;
+};
+
+// What both directions take: queries, keys (or None), positions, inv_freq, w_q, w_k, eps, norm, interleaved.
+RopeTensors rope_inputs(lordba_norm_rope_args &f, PyObject *q_given, PyObject *k_given, PyObject *const *a, const Where &at)
+{
+    const Tensor &q = tensor(q_given, "q"), &positions = tensor(a[0], "positions"), &inv_freq = tensor(a[1], "inv_freq");
+    const std::optional<Tensor> k = optional_tensor(k_given, "k"), w_q = optional_tensor(a[2], "w_q"), w_k = optional_tensor(a[3], "w_k");
+    if (q.dim() != 3) value_error("q must have three dimensions (tokens, heads, entries)");
+    if (k && k->dim() != 3) value_error("k must have three dimensions (tokens, heads, entries)");
+    RopeTensors r{q.scalar_type(), q.size(0), q.size(1), k ? k->size(1) : 0, q.size(2), (bool)k};
+    f.q = heads_of(q, r.T, r.heads_q, r.d, r.type, at, "q");
+    if (k) f.k = heads_of(*k, r.T, r.heads_k, r.d, r.type, at, "k");
+    check_device(positions, at, "positions");
+    if (positions.scalar_type() != at::kLong || positions.dim() != 1 || positions.size(0) != r.T || (r.T > 1 && positions.stride(0) != 1))
+        type_error("positions must be " + std::to_string(r.T) + " contiguous int64 values");
+    check_device(inv_freq, at, "inv_freq");
+    if (inv_freq.scalar_type() != at::kFloat || inv_freq.dim() != 1 || !inv_freq.is_contiguous()) type_error("inv_freq must be contiguous float32 values");
+    if (2 * inv_freq.size(0) > r.d) value_error("inv_freq must have at most half as many values as a head has entries");
+    f.positions = static_cast<const int64_t *>(positions.data_ptr());
+    f.inv_freq = static_cast<const float *>(inv_freq.data_ptr());
+    f.rotary = (int32_t)(2 * inv_freq.size(0));
+    if (r.heads_q > (1 << 20) || r.heads_k > (1 << 20) || r.d > (1 << 20)) value_error("too many heads, or entries of a head");
+    f.heads_q = (int32_t)r.heads_q; f.heads_k = (int32_t)r.heads_k; f.d = (int32_t)r.d;
+    if (w_k && !k) value_error("w_k needs k");
+    for (const auto *w : {&w_q, &w_k}) {
+        if (!*w) continue;
+        const char *what = w == &w_q ? "w_q" : "w_k";
+        check_device(**w, at, what);
+        if ((*w)->dim() != 1 || (*w)->size(0) != r.d || !(*w)->is_contiguous()) value_error(std::string(what) + " must be " + std::to_string(r.d) + " contiguous values");
+    }
+    if (w_q && w_k && w_q->scalar_type() != w_k->scalar_type()) type_error("w_q and w_k must have one type");
+    if (w_q || w_k) f.w_dtype = code_of(w_q ? w_q->scalar_type() : w_k->scalar_type(), "w_q and w_k");
+    f.w_q = data(w_q); f.w_k = data(w_k);
+    f.eps = (float)PyFloat_AsDouble(a[4]);
+    if (PyErr_Occurred()) throw python_error();
+    const int norm = PyObject_IsTrue(a[5]), interleaved = PyObject_IsTrue(a[6]);
+    if (norm < 0 || interleaved < 0) throw python_error();
+    f.flags = (norm ? 0 : LORDBA_ROPE_NO_NORM) | (interleaved ? LORDBA_ROPE_INTERLEAVED : 0);
+    return r;
+}
+
+PyObject *norm_rope(PyObject *const *a)
+{
+    std::optional<Tensor> q_out = optional_tensor(a[9], "q_out"), k_out = optional_tensor(a[10], "k_out");
+    const Where at(a[11]);
+    lordba_norm_rope_args f = {};
+    const RopeTensors r = rope_inputs(f, a[0], a[1], a + 2, at);
+    if (!r.keys && k_out) value_error("k_out needs k");
+    if (!q_out) q_out = at.heads(r.T, r.heads_q, r.d, r.type);
+    if (r.keys && !k_out) k_out = at.heads(r.T, r.heads_k, r.d, r.type);
+    f.q_out = heads_of(*q_out, r.T, r.heads_q, r.d, r.type, at, "q_out");
+    if (r.keys) f.k_out = heads_of(*k_out, r.T, r.heads_k, r.d, r.type, at, "k_out");
+    // no token, or no entry at all: nothing to look at
+    if (r.T) check(lib.rope(&f, r.T, code_of(r.type, "q"), at.stream), "lordba_norm_rope");
+    for (int i : {9, 10}) written(a[i]);
+    return tuple_of(q_out, k_out);
+}
+
+PyObject *norm_rope_backward(PyObject *const *a)
+{
+    const Tensor &dq_out = tensor(a[0], "dq_out");
+    const std::optional<Tensor> dk_out = optional_tensor(a[1], "dk_out");
+    std::optional<Tensor> dq = optional_tensor(a[11], "dq"), dk = optional_tensor(a[12], "dk"), dw_q = optional_tensor(a[13], "dw_q"),
+                          dw_k = optional_tensor(a[14], "dw_k");
+    const Where at(a[16]);
+    lordba_norm_rope_grad_args g = {};
+    const RopeTensors r = rope_inputs(g.f, a[2], a[3], a + 4, at);
+    if (r.keys != (bool)dk_out) value_error("k and dk_out come together");
+    if (!r.keys && (dk || dw_k)) value_error("dk and dw_k need k");
+    g.f.q_out = heads_of(dq_out, r.T, r.heads_q, r.d, r.type, at, "dq_out");
+    if (r.keys) g.f.k_out = heads_of(*dk_out, r.T, r.heads_k, r.d, r.type, at, "dk_out");
+    if (!dq) dq = at.heads(r.T, r.heads_q, r.d, r.type);
+    if (r.keys && !dk) dk = at.heads(r.T, r.heads_k, r.d, r.type);
+    g.dq = heads_of(*dq, r.T, r.heads_q, r.d, r.type, at, "dq");
+    if (r.keys) g.dk = heads_of(*dk, r.T, r.heads_k, r.d, r.type, at, "dk");
+    if (g.f.w_q && !dw_q) dw_q = at.values(r.d, at::kFloat);
+    if (g.f.w_k && !dw_k) dw_k = at.values(r.d, at::kFloat);
+    if (dw_q) g.dw_q = const_cast<float *>(vector(*dw_q, r.d, at, "dw_q"));
+    if (dw_k) g.dw_k = const_cast<float *>(vector(*dw_k, r.d, at, "dw_k"));
+    const Workspace ws(lib.rope_bytes(&g, r.T), a[15], at);
+    check(lib.rope_grad(&g, r.T, code_of(r.type, "q"), ws.p, ws.bytes, at.stream), "lordba_norm_rope_backward");
+    for (int i : {11, 12, 13, 14}) written(a[i]);
+    return tuple_of(dq, dk, dw_q, dw_k);
+}
+
+// ---- distillation ---------------------------------------------------------------------------------------------------
+
+int64_t distill_inputs(lordba_distill &d, const Tensor &logits, PyObject *ids_given, PyObject *teacher_given, PyObject *temperature,
+                       const std::optional<Tensor> &weight, const char *weight_name, const Where &at)
+{
+    const Tensor &ids = tensor(ids_given, "ids"), &teacher = tensor(teacher_given, "teacher");
+    check_matrix(logits, "logits");
+    check_matrix(ids, "ids");
+    const int64_t T = logits.size(0), top = ids.size(1);
+    d.vocab = logits.size(1);
+    d.top = top;
+    d.ld_logits = pitch(logits, T, d.vocab, logits.scalar_type(), at, "logits");
+    if (ids.scalar_type() != at::kLong && ids.scalar_type() != at::kInt) type_error("ids must be int64 or int32, got " + name_of(ids.scalar_type()));
+    d.ld_ids = pitch(ids, T, top, ids.scalar_type(), at, "ids");
+    d.flags = ids.scalar_type() == at::kLong ? LORDBA_DISTILL_IDS_64 : 0;
+    d.teacher_dtype = code_of(teacher.scalar_type(), "teacher");
+    d.ld_teacher = pitch(teacher, T, top, teacher.scalar_type(), at, "teacher");
+    const double tau = PyFloat_AsDouble(temperature);
+    if (tau == -1.0 && PyErr_Occurred()) throw python_error();
+    d.temperature = (float)tau;
+    d.logits = logits.data_ptr(); d.ids = ids.data_ptr(); d.teacher = teacher.data_ptr();
+    if (weight) d.weight = vector(*weight, T, at, weight_name);
+    return T;
+}
+
+PyObject *distill_loss(PyObject *const *a)
+{
+    const Tensor &logits = tensor(a[0], "logits");
+    const std::optional<Tensor> weight = optional_tensor(a[4], "weight");
+    std::optional<Tensor> loss = optional_tensor(a[5], "loss"), lse = optional_tensor(a[6], "lse"), dlogits = optional_tensor(a[7], "dlogits");
+    const int grad = PyObject_IsTrue(a[8]);
+    if (grad < 0) throw python_error();
+    const Where at(a[9]);
+    const int code = code_of(logits.scalar_type(), "logits");
+    lordba_distill d = {};
+    const int64_t T = distill_inputs(d, logits, a[1], a[2], a[3], weight, "weight", at);
+    if (!loss) loss = at.values(T, at::kFloat);
+    if (!lse) lse = at.values(T, at::kFloat);
+    if (grad && !dlogits) dlogits = at.rows(T, d.vocab, logits.scalar_type());
+    if (dlogits) d.ld_dlogits = pitch(*dlogits, T, d.vocab, logits.scalar_type(), at, "dlogits");
+    d.loss = const_cast<float *>(vector(*loss, T, at, "loss"));
+    d.lse = const_cast<float *>(vector(*lse, T, at, "lse"));
+    d.dlogits = data(dlogits);
+    check(lib.distill[0](&d, T, code, at.stream), "lordba_distill_loss");
+    for (int i : {5, 6, 7}) written(a[i]);
+    return tuple_of(loss, lse, dlogits);
+}
+
+PyObject *distill_backward(PyObject *const *a)
+{
+    const Tensor &dloss = tensor(a[0], "dloss"), &logits = tensor(a[1], "logits"), &lse = tensor(a[4], "lse");
+    std::optional<Tensor> dlogits = optional_tensor(a[6], "dlogits");
+    const Where at(a[7]);
+    const int code = code_of(logits.scalar_type(), "logits");
+    lordba_distill d = {};
+    const int64_t T = distill_inputs(d, logits, a[2], a[3], a[5], dloss, "dloss", at);
+    if (!dlogits) dlogits = at.rows(T, d.vocab, logits.scalar_type());
+    d.ld_dlogits = pitch(*dlogits, T, d.vocab, logits.scalar_type(), at, "dlogits");
+    d.lse = const_cast<float *>(vector(lse, T, at, "lse"));
+    d.dlogits = dlogits->data_ptr();
+    check(lib.distill[1](&d, T, code, at.stream), "lordba_distill_backward");
+    written(a[6]);
+    return wrapped(dlogits);
+}
+
 // bind(path, LordbaError): take the entry points from a build of the library.
 PyObject *bind(PyObject *const *a)
 {
@@ -429,6 +733,19 @@ PyObject *bind(PyObject *const *a)
     find(found.grad_bytes, "lordba_gated_backward_workspace_bytes");
     find(found.grad, "lordba_gated_backward");
     find(found.dropout, "lordba_dropout");
+    find(found.int4_row_bytes, "lordba_int4_row_bytes");
+    find(found.int4_pack, "lordba_int4_pack");
+    find(found.int4_quantize, "lordba_int4_quantize");
+    find(found.int4_dequantize, "lordba_int4_dequantize");
+    find(found.int4_bytes[0], "lordba_int4_linear_workspace_bytes");
+    find(found.int4_bytes[1], "lordba_int4_linear_backward_workspace_bytes");
+    find(found.int4[0], "lordba_int4_linear");
+    find(found.int4[1], "lordba_int4_linear_backward");
+    find(found.rope, "lordba_norm_rope");
+    find(found.rope_bytes, "lordba_norm_rope_backward_workspace_bytes");
+    find(found.rope_grad, "lordba_norm_rope_backward");
+    find(found.distill[0], "lordba_distill_loss");
+    find(found.distill[1], "lordba_distill_backward");
     lib = found;
     Py_INCREF(a[1]);
     Py_XSETREF(status_error, a[1]);
@@ -472,6 +789,15 @@ PyMethodDef methods[] = {method<bind, 2>("bind"),
                          method<gated_forward, 14>("gated_forward"),
                          method<gated_backward, 14>("gated_backward"),
                          method<dropout, 7>("dropout"),
+                         method<int4_pack, 3>("int4_pack"),
+                         method<int4_quantize, 8>("int4_quantize"),
+                         method<int4_dequantize, 7>("int4_dequantize"),
+                         method<int4_linear, 8>("int4_linear"),
+                         method<int4_linear_backward, 9>("int4_linear_backward"),
+                         method<norm_rope, 12>("norm_rope"),
+                         method<norm_rope_backward, 17>("norm_rope_backward"),
+                         method<distill_loss, 10>("distill_loss"),
+                         method<distill_backward, 8>("distill_backward"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,4 +1,4 @@
-// Element access shared by the kernels next to the adapters (elementwise.cu, product.cu).
+// Element access shared by the kernels next to the adapters.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -110,6 +110,68 @@ __device__ __forceinline__ uint4 load_bytes16(uintptr_t at, uintptr_t end)
         w[i] &= bytes >= 4 ? 0xffffffffu : bytes <= 0 ? 0u : (1u << 8 * bytes) - 1u;
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Columns 8 g ... 8 g + 7 of a row of d elements; what lies past d reads as zero.  (Dropout may run in place:
+// these are ordinary loads.)
+template <typename E>
+__device__ __noinline__ Group8<E> load8_last(const E *row, int64_t g, int64_t d)
+{
+    Group8<E> v;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + 8 * g), end = reinterpret_cast<uintptr_t>(row + d);
+    v.w = load_bytes16<false>(at, end);
+    if constexpr (sizeof(E) == 4) v.w2 = at + 16 < end ? load_bytes16<false>(at + 16, end) : make_uint4(0, 0, 0, 0);
+    return v;
+}
+
+template <typename E>
+__device__ __forceinline__ Group8<E> load8(const E *row, int64_t g, int64_t d, bool vec)
+{
+    if (8 * g + 8 > d) return load8_last(row, g, d);
+    if (vec) return load_group(row + 8 * g);
+    // a whole group, off the 16-byte grid: the aligned pieces that hold it all hold bytes of it
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + 8 * g);
+    const uint4 *p = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
+    const uint32_t by = (uint32_t)at & 15u;
+    constexpr int kWhole = sizeof(Group8<E>) / 16;
+    uint4 x[kWhole + 1];
+#pragma unroll
+    for (int i = 0; i < kWhole; ++i) x[i] = p[i];
+    x[kWhole] = p[by ? kWhole : 0];
+    Group8<E> v;
+    v.w = join_pieces(x[0], x[1], by);
+    if constexpr (sizeof(E) == 4) v.w2 = join_pieces(x[1], x[2], by);
+    return v;
+}
+
+template <typename E>
+__device__ __noinline__ void store8_parts(E *row, int64_t g, int64_t d, float v0, float v1, float v2, float v3, float v4, float v5,
+                                          float v6, float v7)
+{
+    const float v[8] = {v0, v1, v2, v3, v4, v5, v6, v7};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (8 * g + i < d) row[8 * g + i] = from_float<E>(v[i]);
+}
+
+template <typename E>
+__device__ __forceinline__ void store8(E *row, int64_t g, int64_t d, bool vec, const float v[8])
+{
+    if (vec && 8 * g + 8 <= d) store_group<E>(row + 8 * g, v);
+    else store8_parts(row, g, d, v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]);
+}
+
+// FULL: every matrix allows 16-byte accesses and d is a multiple of 8, so nothing is looked at per access
+template <bool FULL, typename E>
+__device__ __forceinline__ Group8<E> load_either(const E *row, int64_t g, int64_t d, bool vec)
+{
+    return FULL ? load_group(row + 8 * g) : load8(row, g, d, vec);
+}
+template <bool FULL, typename E>
+__device__ __forceinline__ void store_either(E *row, int64_t g, int64_t d, bool vec, const float v[8])
+{
+    if (FULL) store_group<E>(row + 8 * g, v);
+    else store8(row, g, d, vec, v);
 }
 
 // Programmatic dependent launch: a kernel's first global access comes after grid_wait(), so that the

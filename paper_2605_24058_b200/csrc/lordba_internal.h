@@ -136,6 +136,20 @@ struct RepackList {
 };
 int launch_repack(const RepackList &list, cudaStream_t stream);
 
+// --- int4.cu -----------------------------------------------------------------
+int launch_int4_pack(const uint8_t *values, int64_t ldv, uint8_t *q, int64_t ldq, int64_t d_out, int64_t d_in, cudaStream_t stream);
+int launch_int4_quantize(const void *w, int64_t ldw, int wdtype, uint8_t *q, int64_t ldq, void *scale, int64_t ld_scale, uint8_t *zero,
+                         int64_t ld_zero, int64_t d_out, int64_t d_in, int group, int dtype, cudaStream_t stream);
+int launch_int4_dequantize(const lordba_int4_proj &p, int dtype, cudaStream_t stream);      // to p.out
+
+// --- rope.cu -----------------------------------------------------------------
+int launch_norm_rope(const lordba_norm_rope_args &f, int64_t T, int dtype, cudaStream_t stream);
+size_t norm_rope_backward_bytes(const lordba_norm_rope_grad_args &a, int64_t T);
+int launch_norm_rope_backward(const lordba_norm_rope_grad_args &a, int64_t T, int dtype, void *workspace, cudaStream_t stream);
+
+// --- distill.cu --------------------------------------------------------------
+int launch_distill(const lordba_distill &d, int64_t T, int dtype, bool backward, cudaStream_t stream);
+
 // --- product.cu --------------------------------------------------------------
 // D[m,n] = sum_k A[m,k] B[n,k], then an epilogue.  An operand is a row-major matrix; its rows run along m
 // (n) with the contraction contiguous, or, mn_major, along the contraction with m (n) contiguous.

@@ -510,11 +510,12 @@ finish_kernel(const __grid_constant__ Finish F, const __grid_constant__ Joint J)
 }
 
 // The instantiations, by number.
-enum Form { kLinear8, kGated8, kGated16, kSum16, kPair16 };
+enum Form { kLinear8, kGated8, kGated16, kSum16, kPair16, kLinear16 };
 
 Form form_of(const Product &p)
 {
     if (p.kind == kProductInt8) return p.form == Product::kGated ? kGated8 : kLinear8;
+    if (p.form == Product::kSingle) return p.b[0].mn_major ? kSum16 : kLinear16;      // a sum of one product
     return p.form == Product::kGated ? kGated16 : p.form == Product::kPair ? kPair16 : kSum16;
 }
 
@@ -529,6 +530,8 @@ const void *kernel_of(Form form, bool loose)
                                     : (const void *)&product_stream_kernel<false, true, false, false, false>;
         case kSum16: return loose ? (const void *)&product_stream_kernel<false, false, true, false, true>
                                   : (const void *)&product_stream_kernel<false, false, true, false, false>;
+        case kLinear16: return loose ? (const void *)&product_stream_kernel<false, false, false, false, true>
+                                     : (const void *)&product_stream_kernel<false, false, false, false, false>;
         default: return (const void *)&product_stream_kernel<false, false, true, true, false>;
     }
 }
@@ -544,8 +547,8 @@ struct Resident {
 Resident resident(Form form, bool loose)
 {
     static std::mutex mu;
-    static Resident known[64][2 * (kPair16 + 1)];
-    static std::atomic<bool> answered[64][2 * (kPair16 + 1)];
+    static Resident known[64][2 * (kLinear16 + 1)];
+    static std::atomic<bool> answered[64][2 * (kLinear16 + 1)];
     Resident r = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return r;

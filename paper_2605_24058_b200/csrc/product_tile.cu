@@ -460,12 +460,12 @@ int launch_tile(const TileArgs &args, cudaStream_t stream)
 }
 
 template <int DT>
-int launch_typed(const TileArgs &a, bool int8, bool gated, bool pair, cudaStream_t stream)
+int launch_typed(const TileArgs &a, bool int8, bool gated, bool pair, bool b_mn, cudaStream_t stream)
 {
     if (int8) return gated ? launch_tile<true, true, false, false, DT>(a, stream) : launch_tile<true, false, false, false, DT>(a, stream);
     if (gated) return launch_tile<false, true, false, false, DT>(a, stream);
     if (pair) return launch_tile<false, false, true, true, DT>(a, stream);
-    return launch_tile<false, false, false, true, DT>(a, stream);
+    return b_mn ? launch_tile<false, false, false, true, DT>(a, stream) : launch_tile<false, false, false, false, DT>(a, stream);
 }
 
 }  // namespace
@@ -529,8 +529,8 @@ int launch_product_tile(const Product &p, const Finish &f, cudaStream_t stream)
     if (!a.status) return LORDBA_ECUDA;
     a.idesc = instr_desc(int8, p.kind == kProductBf16, a_mn, b_mn, 256, 256);
     switch (p.dtype) {
-        case LORDBA_BF16: return launch_typed<LORDBA_BF16>(a, int8, gated, pair, stream);
-        case LORDBA_F16: return launch_typed<LORDBA_F16>(a, int8, gated, pair, stream);
+        case LORDBA_BF16: return launch_typed<LORDBA_BF16>(a, int8, gated, pair, b_mn, stream);
+        case LORDBA_F16: return launch_typed<LORDBA_F16>(a, int8, gated, pair, b_mn, stream);
         default: return launch_tile<true, false, false, false, LORDBA_F32>(a, stream);      // 8-bit products only
     }
 }

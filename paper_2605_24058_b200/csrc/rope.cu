@@ -1,0 +1,438 @@
+// Norms of queries and keys for each head, the rotation by position, and the gradients of both: one launch for queries
+// and keys (the gradients of the norms' weights add the join of their partial sums).
+//
+// Bound: HBM, each head vector is read once and written once.  A head vector of d entries lies in ceil(d / 16) lanes of a
+// warp, in registers from its load to its store; a lane holds eight of the pairs that are rotated together, so norm and
+// rotation need nothing of another lane but the sum of squares.  A warp takes 32 / width heads of a token at a time and
+// walks over the token's heads: the token's angles are worked out once for all of them.
+//
+// Angles.  f = position * inv_freq, in turns, in 64 bits, less its whole turns; what is left is exact to 2^-24 of a turn
+// for positions up to 2^31, where a product in 32 bits would be off by 8e-3 already at position 131072.
+#include <cstring>
+
+#include "block_checks.h"
+#include "block_common.cuh"
+
+namespace lordba {
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kMaxPairs = LORDBA_ROPE_MAX_D / 2;
+
+// Queries, or keys.  Distances in entries.
+struct Side {
+    const void *x, *g;             // the vectors; backward: the gradients of the results
+    void *out;
+    int64_t x_token, x_head, g_token, g_head, out_token, out_head;
+    const void *w;
+    float *part;                   // backward: a row of d partial sums for each block, or null
+    int heads;
+    int steps, per_unit;           // steps of a token (a warp's heads each), and of a unit
+    int chunks;                    // units of a token
+    int blocks;
+};
+
+struct RopeArgs {
+    Side side[2];
+    const int64_t *positions;
+    const float *inv_freq;
+    int64_t T;
+    int d, half, width, w_dtype, norm;      // half: pairs that are rotated; width: lanes of a head vector
+    float eps, inv_d;
+};
+
+// A lane's eight pairs: pair p is entries (p, p + half) where pairs are halves and rotated, else (2 p, 2 p + 1).  VEC: the
+// lane holds pairs 8 l ... 8 l + 7, so that its entries are two runs of eight (16 bytes each of a 16-bit type); of halves that
+// are not rotated any eight pairs do, and it takes entries 16 l ... 16 l + 15 as two runs.  Otherwise neighbouring lanes hold
+// neighbouring pairs.
+template <bool INTERLEAVED, bool VEC>
+struct Place {
+    int l, width, half, d;
+    bool turned;                   // VEC: whether the lane's pairs are rotated halves
+
+    __device__ __forceinline__ Place(int lane, const RopeArgs &A) : l(lane % A.width), width(A.width), half(A.half), d(A.d)
+    {
+        turned = !INTERLEAVED && 8 * l < half;
+    }
+    __device__ __forceinline__ int pair(int j) const { return VEC ? 8 * l + j : l + width * j; }
+    __device__ __forceinline__ bool has(int j) const { return VEC ? 16 * l < d : first(j) < d; }
+    __device__ __forceinline__ int run(int r) const { return turned ? 8 * l + r * half : 16 * l + 8 * r; }
+    __device__ __forceinline__ int first(int j) const
+    {
+        if (VEC) return INTERLEAVED ? 16 * l + 2 * j : run(0) + j;
+        const int p = pair(j);
+        return !INTERLEAVED && p < half ? p : 2 * p;
+    }
+    __device__ __forceinline__ int second(int j) const
+    {
+        if (VEC) return INTERLEAVED ? 16 * l + 2 * j + 1 : run(1) + j;
+        const int p = pair(j);
+        return !INTERLEAVED && p < half ? p + half : 2 * p + 1;
+    }
+};
+
+// What a lane holds of a head vector, as it lies in memory.
+template <typename E, bool VEC> struct Raw;
+template <typename E> struct Raw<E, true> { Group8<E> r[2]; };
+template <typename E> struct Raw<E, false> { E a[8], b[8]; };
+
+template <typename E, bool INTERLEAVED, bool VEC>
+__device__ __forceinline__ Raw<E, VEC> load_heads(const E *p, const Place<INTERLEAVED, VEC> &at, bool in)
+{
+    Raw<E, VEC> v;
+    std::memset(&v, 0, sizeof(v));
+    if (!in) return v;
+    if constexpr (VEC) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            if (at.run(r) < at.d) v.r[r] = load_group(p + at.run(r));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (at.first(j) < at.d) v.a[j] = p[at.first(j)];
+            if (at.second(j) < at.d) v.b[j] = p[at.second(j)];
+        }
+    }
+    return v;
+}
+
+template <typename E, bool INTERLEAVED, bool VEC>
+__device__ __forceinline__ void unpack(const Raw<E, VEC> &v, float a[8], float b[8])
+{
+    if constexpr (VEC) {
+        float x[16];
+        unpack_group<E>(v.r[0], x);
+        unpack_group<E>(v.r[1], x + 8);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            a[j] = x[INTERLEAVED ? 2 * j : j];
+            b[j] = x[INTERLEAVED ? 2 * j + 1 : 8 + j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { a[j] = to_float(v.a[j]); b[j] = to_float(v.b[j]); }
+    }
+}
+
+template <typename E, bool INTERLEAVED, bool VEC>
+__device__ __forceinline__ void store_heads(E *p, const Place<INTERLEAVED, VEC> &at, const float a[8], const float b[8])
+{
+    if constexpr (VEC) {
+        float x[16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[INTERLEAVED ? 2 * j : j] = a[j];
+            x[INTERLEAVED ? 2 * j + 1 : 8 + j] = b[j];
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            if (at.run(r) < at.d) store_group<E>(p + at.run(r), x + 8 * r);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (at.first(j) < at.d) p[at.first(j)] = from_float<E>(a[j]);
+            if (at.second(j) < at.d) p[at.second(j)] = from_float<E>(b[j]);
+        }
+    }
+}
+
+__device__ __forceinline__ float weight_at(const void *w, int dtype, int i)
+{
+    if (dtype == LORDBA_F32) return static_cast<const float *>(w)[i];
+    return dtype == LORDBA_BF16 ? to_float(static_cast<const __nv_bfloat16 *>(w)[i]) : to_float(static_cast<const __half *>(w)[i]);
+}
+
+// The sum over the lanes of a head vector.
+__device__ __forceinline__ float over_head(float v, int width)
+{
+#pragma unroll
+    for (int o = 16; o; o /= 2)
+        if (o < width) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+template <typename E, bool BACK, bool INTERLEAVED, bool VEC>
+__global__ void __launch_bounds__(kThreads, BACK ? 2 : 3)
+norm_rope_kernel(const __grid_constant__ RopeArgs A)
+{
+    __shared__ float2 table[kWarps][kMaxPairs];          // cosine and sine of the warp's token
+    __shared__ float sums[BACK ? kWarps : 1][LORDBA_ROPE_MAX_D];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int which = (int)blockIdx.x >= A.side[0].blocks;
+    const Side &S = A.side[which];
+    const int block = blockIdx.x - (which ? A.side[0].blocks : 0);
+    const Place<INTERLEAVED, VEC> at(lane, A);
+    const int per = 32 / A.width, mine = lane / A.width;
+    grid_wait();
+    grid_release();
+
+    float wa[8], wb[8], da[8], db[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        wa[j] = S.w && at.first(j) < A.d ? weight_at(S.w, A.w_dtype, at.first(j)) : 1.0f;
+        wb[j] = S.w && at.second(j) < A.d ? weight_at(S.w, A.w_dtype, at.second(j)) : 1.0f;
+        da[j] = db[j] = 0.0f;
+    }
+    const int64_t units = A.T * S.chunks;
+    for (int64_t u = (int64_t)block * kWarps + warp; u < units; u += (int64_t)S.blocks * kWarps) {
+        const int64_t t = S.chunks == 1 ? u : u / S.chunks;
+        const int s0 = (int)(u - t * S.chunks) * S.per_unit, s1 = s0 + S.per_unit < S.steps ? s0 + S.per_unit : S.steps;
+        const E *x = static_cast<const E *>(S.x) + t * S.x_token, *g = static_cast<const E *>(S.g) + (BACK ? t * S.g_token : 0);
+        E *out = static_cast<E *>(S.out) + t * S.out_token;
+        // the first heads are on their way while the angles are worked out
+        int h = s0 * per + mine;
+        bool in = h < S.heads && at.has(0);
+        Raw<E, VEC> rx = load_heads<E>(x + h * S.x_head, at, in && (!BACK || A.norm)), rg;
+        if (BACK) rg = load_heads<E>(g + h * S.g_head, at, in);
+        if (A.half) {
+            const double turns_of = (double)A.positions[t] * 0.15915494309189533577;       // 1 / (2 pi)
+            __syncwarp();                                   // the table's last readers
+            for (int i = lane; i < A.half; i += 32) {
+                double turns = turns_of * (double)A.inv_freq[i];
+                turns -= rint(turns);
+                float sine, cosine;
+                sincospif(2.0f * (float)turns, &sine, &cosine);
+                table[warp][i] = make_float2(cosine, BACK ? -sine : sine);
+            }
+            __syncwarp();
+        }
+        float c[8], s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool turned = at.pair(j) < A.half;
+            const float2 v = turned ? table[warp][at.pair(j)] : make_float2(1.0f, 0.0f);
+            c[j] = v.x; s[j] = v.y;
+        }
+        for (int step = s0; step < s1; ++step) {
+            const int h_now = h;
+            const bool in_now = in;
+            float a[8], b[8], ga[8], gb[8];
+            unpack<E, INTERLEAVED, VEC>(rx, a, b);
+            if (BACK) unpack<E, INTERLEAVED, VEC>(rg, ga, gb);
+            if (step + 1 < s1) {                            // the next heads' loads
+                h += per;
+                in = h < S.heads && at.has(0);
+                rx = load_heads<E>(x + h * S.x_head, at, in && (!BACK || A.norm));
+                if (BACK) rg = load_heads<E>(g + h * S.g_head, at, in);
+            }
+            float r = 1.0f;
+            if (A.norm) {
+                float q = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q += a[j] * a[j] + b[j] * b[j];
+                r = rsqrtf(over_head(q, A.width) * A.inv_d + A.eps);
+            }
+            if (!BACK) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float na = A.norm ? a[j] * r * wa[j] : a[j], nb = A.norm ? b[j] * r * wb[j] : b[j];
+                    // an unrotated entry goes through as it is: 0 times an infinity would not
+                    const bool turned = at.pair(j) < A.half;
+                    a[j] = turned ? na * c[j] - nb * s[j] : na;
+                    b[j] = turned ? nb * c[j] + na * s[j] : nb;
+                }
+            } else {
+                float dot = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool turned = at.pair(j) < A.half;
+                    const float ta = turned ? ga[j] * c[j] - gb[j] * s[j] : ga[j], tb = turned ? gb[j] * c[j] + ga[j] * s[j] : gb[j];
+                    ga[j] = ta; gb[j] = tb;
+                    if (A.norm) {
+                        a[j] *= r; b[j] *= r;
+                        da[j] += ta * a[j]; db[j] += tb * b[j];
+                        ga[j] *= wa[j]; gb[j] *= wb[j];
+                        dot += ga[j] * a[j] + gb[j] * b[j];
+                    }
+                }
+                if (A.norm) {
+                    dot = over_head(dot, A.width) * A.inv_d;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) { a[j] = r * (ga[j] - a[j] * dot); b[j] = r * (gb[j] - b[j] * dot); }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) { a[j] = ga[j]; b[j] = gb[j]; }
+                }
+            }
+            if (in_now) store_heads<E>(out + h_now * S.out_head, at, a, b);
+        }
+    }
+    if (BACK && S.part) {
+        // lanes of one place, then warps, in a fixed order
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+            for (int o = 16; o; o /= 2)
+                if (o >= A.width) {
+                    da[j] += __shfl_xor_sync(0xffffffffu, da[j], o);
+                    db[j] += __shfl_xor_sync(0xffffffffu, db[j], o);
+                }
+            if (mine == 0 && at.first(j) < A.d) sums[warp][at.first(j)] = da[j];
+            if (mine == 0 && at.second(j) < A.d) sums[warp][at.second(j)] = db[j];
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < A.d; i += kThreads) {
+            float v = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) v += sums[BACK ? k : 0][i];
+            S.part[(int64_t)block * A.d + i] = v;
+        }
+    }
+}
+
+struct JoinArgs {
+    const float *part[2];
+    float *dw[2];
+    int blocks[2], d;
+};
+
+// dw of one side: 32 columns a block, its eight warps take every eighth row of partial sums each.
+__global__ void __launch_bounds__(kThreads)
+norm_rope_join_kernel(const __grid_constant__ JoinArgs J)
+{
+    __shared__ float sums[kWarps][32];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, i = blockIdx.x * 32 + lane, side = blockIdx.y;
+    grid_wait();
+    grid_release();
+    if (!J.dw[side]) return;
+    float v = 0.0f;
+    if (i < J.d)
+#pragma unroll 8
+        for (int b = warp; b < J.blocks[side]; b += kWarps) v += J.part[side][(int64_t)b * J.d + i];
+    sums[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && i < J.d) {
+        v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) v += sums[k][lane];
+        J.dw[side][i] = v;
+    }
+}
+
+constexpr int kBackBlocks = 148 * 2;       // at most, of both sides: what is resident at once
+
+// How a call's heads are dealt out: blocks of both sides, units.
+void plan(RopeArgs &A, const lordba_norm_rope_args &f, int64_t T, bool back)
+{
+    A.T = T;
+    A.d = f.d;
+    A.half = f.rotary / 2;
+    A.width = 1;
+    while (A.width * 16 < f.d) A.width *= 2;
+    const int per = 32 / A.width;
+    int64_t all = 0;
+    for (int i = 0; i < 2; ++i) {
+        Side &S = A.side[i];
+        S.heads = i ? f.heads_k : f.heads_q;
+        S.steps = (S.heads + per - 1) / per;
+        all += S.steps;
+    }
+    // a unit is a token's heads, or fewer of them while the GPU has idle warps (16 an SM are enough)
+    const int64_t warps = 148 * 16, most_blocks = back ? kBackBlocks : 148 * 16;
+    for (int i = 0; i < 2; ++i) {
+        Side &S = A.side[i];
+        if (S.steps == 0) continue;
+        const int64_t want = (T * all + warps - 1) / warps;
+        S.per_unit = (int)(want < S.steps ? want : S.steps);
+        S.chunks = (S.steps + S.per_unit - 1) / S.per_unit;
+        const int64_t need = (T * S.chunks + kWarps - 1) / kWarps;
+        int64_t share = most_blocks * S.steps / all;
+        if (share < 1) share = 1;
+        S.blocks = (int)(need < share ? need : share);
+    }
+}
+
+bool vec_heads(const lordba_heads &h, size_t e) { return aligned(h.p, 16) && (h.token * e) % 16 == 0 && (h.head * e) % 16 == 0; }
+
+void take(Side &S, const lordba_heads &x, const lordba_heads &g, const lordba_heads &out, const void *w)
+{
+    S.x = x.p; S.x_token = x.token; S.x_head = x.head;
+    S.g = g.p; S.g_token = g.token; S.g_head = g.head;
+    S.out = const_cast<void *>(out.p); S.out_token = out.token; S.out_head = out.head;
+    S.w = w;
+}
+
+template <typename E, bool BACK>
+int launch_typed(const RopeArgs &A, bool interleaved, bool vec, cudaStream_t stream)
+{
+    const auto kernel = interleaved ? (vec ? norm_rope_kernel<E, BACK, true, true> : norm_rope_kernel<E, BACK, true, false>)
+                                    : (vec ? norm_rope_kernel<E, BACK, false, true> : norm_rope_kernel<E, BACK, false, false>);
+    return launch_kernel(kernel, dim3((unsigned)(A.side[0].blocks + A.side[1].blocks), 1, 1), kThreads, 0, stream, A);
+}
+
+template <bool BACK>
+int launch(const RopeArgs &A, int dtype, bool interleaved, bool vec, cudaStream_t stream)
+{
+    switch (dtype) {
+        case LORDBA_BF16: return launch_typed<__nv_bfloat16, BACK>(A, interleaved, vec, stream);
+        case LORDBA_F16: return launch_typed<__half, BACK>(A, interleaved, vec, stream);
+        default: return launch_typed<float, BACK>(A, interleaved, vec, stream);
+    }
+}
+
+void common(RopeArgs &A, const lordba_norm_rope_args &f)
+{
+    A.positions = f.positions;
+    A.inv_freq = f.inv_freq;
+    A.w_dtype = f.w_dtype;
+    A.norm = !(f.flags & LORDBA_ROPE_NO_NORM);
+    A.eps = f.eps;
+    A.inv_d = 1.0f / (float)f.d;
+}
+
+// Whether a lane's pairs are two runs of eight entries on 16-byte boundaries.
+bool vec_shape(const lordba_norm_rope_args &f) { return f.d % 8 == 0 && ((f.flags & LORDBA_ROPE_INTERLEAVED) || f.rotary % 16 == 0); }
+
+}  // namespace
+
+int launch_norm_rope(const lordba_norm_rope_args &f, int64_t T, int dtype, cudaStream_t stream)
+{
+    RopeArgs A;
+    std::memset(&A, 0, sizeof(A));
+    plan(A, f, T, false);
+    common(A, f);
+    const lordba_heads none{nullptr, 0, 0};
+    take(A.side[0], f.q, none, f.q_out, f.w_q);
+    take(A.side[1], f.k, none, f.k_out, f.w_k);
+    const size_t e = elt(dtype);
+    const bool vec = vec_shape(f) && vec_heads(f.q, e) && vec_heads(f.q_out, e) && (!f.heads_k || (vec_heads(f.k, e) && vec_heads(f.k_out, e)));
+    return launch<false>(A, dtype, f.flags & LORDBA_ROPE_INTERLEAVED, vec, stream);
+}
+
+size_t norm_rope_backward_bytes(const lordba_norm_rope_grad_args &a, int64_t T)
+{
+    if (!a.dw_q && !a.dw_k) return 0;
+    RopeArgs A;
+    std::memset(&A, 0, sizeof(A));
+    plan(A, a.f, T, true);
+    return ((size_t)(A.side[0].blocks + A.side[1].blocks) * a.f.d * 4 + 255) / 256 * 256;
+}
+
+int launch_norm_rope_backward(const lordba_norm_rope_grad_args &a, int64_t T, int dtype, void *workspace, cudaStream_t stream)
+{
+    const lordba_norm_rope_args &f = a.f;
+    RopeArgs A;
+    std::memset(&A, 0, sizeof(A));
+    plan(A, f, T, true);
+    common(A, f);
+    take(A.side[0], f.q, f.q_out, a.dq, f.w_q);
+    take(A.side[1], f.k, f.k_out, a.dk, f.w_k);
+    float *part = static_cast<float *>(workspace);
+    if (a.dw_q) A.side[0].part = part;
+    if (a.dw_k) A.side[1].part = part + (int64_t)A.side[0].blocks * f.d;
+    const size_t e = elt(dtype);
+    const bool vec = vec_shape(f) && vec_heads(f.q, e) && vec_heads(f.q_out, e) && vec_heads(a.dq, e) &&
+                     (!f.heads_k || (vec_heads(f.k, e) && vec_heads(f.k_out, e) && vec_heads(a.dk, e)));
+    const int rc = launch<true>(A, dtype, f.flags & LORDBA_ROPE_INTERLEAVED, vec, stream);
+    if (rc != LORDBA_OK || (!a.dw_q && !a.dw_k)) return rc;
+    JoinArgs J = {};
+    J.d = f.d;
+    for (int i = 0; i < 2; ++i) {
+        J.part[i] = A.side[i].part;
+        J.dw[i] = i ? a.dw_k : a.dw_q;
+        J.blocks[i] = A.side[i].blocks;
+    }
+    return launch_kernel(norm_rope_join_kernel, dim3((unsigned)((f.d + 31) / 32), 2, 1), kThreads, 0, stream, J);
+}
+
+}  // namespace lordba

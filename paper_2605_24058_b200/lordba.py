@@ -28,6 +28,8 @@ FIT_ALPHA, FIT_BETA, FIT_GAMMA, FIT_ALL = 1, 2, 4, 7
 ACT_SILU, ACT_GELU_TANH = 0, 1
 GATED_INT8 = 1
 INT8_MAX_DIN = 131071
+ROPE_NO_NORM, ROPE_INTERLEAVED, ROPE_MAX_D = 1, 2, 512
+DISTILL_IDS_64, DISTILL_MAX_TOP = 1, 256
 
 
 def proj_ell(ell: int) -> int:
@@ -71,6 +73,36 @@ class GatedGrad(ctypes.Structure):
         ("act", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
+class Int4Proj(ctypes.Structure):
+    """Mirror of ``lordba_int4_proj`` (``input``: its member ``in``)."""
+    _fields_ = [("input", _vp), ("out", _vp), ("q", _vp), ("scale", _vp), ("zero", _vp)] + [
+        (n, _i64) for n in ("d_in", "d_out", "ld_in", "ld_out", "ldq", "ld_scale", "ld_zero")] + [
+        ("group", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class Heads(ctypes.Structure):
+    """Mirror of ``lordba_heads``."""
+    _fields_ = [("p", _vp), ("token", _i64), ("head", _i64)]
+
+
+class NormRope(ctypes.Structure):
+    """Mirror of ``lordba_norm_rope_args``."""
+    _fields_ = [(n, Heads) for n in ("q", "k", "q_out", "k_out")] + [(n, _vp) for n in ("w_q", "w_k", "positions", "inv_freq")] + [
+        (n, ctypes.c_int32) for n in ("heads_q", "heads_k", "d", "rotary", "w_dtype", "flags")] + [("eps", ctypes.c_float)]
+
+
+class NormRopeGrad(ctypes.Structure):
+    """Mirror of ``lordba_norm_rope_grad_args``."""
+    _fields_ = [("f", NormRope), ("dq", Heads), ("dk", Heads), ("dw_q", _vp), ("dw_k", _vp)]
+
+
+class Distill(ctypes.Structure):
+    """Mirror of ``lordba_distill``."""
+    _fields_ = [(n, _vp) for n in ("logits", "ids", "teacher", "weight", "loss", "lse", "dlogits")] + [
+        (n, _i64) for n in ("vocab", "top", "ld_logits", "ld_ids", "ld_teacher", "ld_dlogits")] + [
+        ("temperature", ctypes.c_float), ("teacher_dtype", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
 _SIGNATURES = {
     "lordba_packed_words": (_i64, [_i64, _i64, ctypes.c_int]),
     "lordba_pack_signs": (ctypes.c_int, [_vp, _i64, _i64, ctypes.c_int, _vp, _vp]),
@@ -110,6 +142,20 @@ _SIGNATURES = {
     "lordba_gated_backward": (ctypes.c_int, [ctypes.POINTER(GatedGrad), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
     "lordba_dropout": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, ctypes.c_float, ctypes.c_uint64,
                                       ctypes.c_uint64, ctypes.c_int, _vp]),
+    "lordba_int4_row_bytes": (_i64, [_i64]),
+    "lordba_int4_pack": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i64, _i64, _vp]),
+    "lordba_int4_quantize": (ctypes.c_int, [_vp, _i64, ctypes.c_int, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, ctypes.c_int,
+                                            ctypes.c_int, _vp]),
+    "lordba_int4_dequantize": (ctypes.c_int, [ctypes.POINTER(Int4Proj), ctypes.c_int, _vp]),
+    "lordba_int4_linear_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Int4Proj), _i64]),
+    "lordba_int4_linear": (ctypes.c_int, [ctypes.POINTER(Int4Proj), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "lordba_int4_linear_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Int4Proj), _i64]),
+    "lordba_int4_linear_backward": (ctypes.c_int, [ctypes.POINTER(Int4Proj), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "lordba_norm_rope": (ctypes.c_int, [ctypes.POINTER(NormRope), _i64, ctypes.c_int, _vp]),
+    "lordba_norm_rope_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(NormRopeGrad), _i64]),
+    "lordba_norm_rope_backward": (ctypes.c_int, [ctypes.POINTER(NormRopeGrad), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "lordba_distill_loss": (ctypes.c_int, [ctypes.POINTER(Distill), _i64, ctypes.c_int, _vp]),
+    "lordba_distill_backward": (ctypes.c_int, [ctypes.POINTER(Distill), _i64, ctypes.c_int, _vp]),
     "lordba_adapter_bits": (_i64, [_i64, _i64, ctypes.c_int, ctypes.c_int]),
     "lordba_set_variant": (ctypes.c_int, [ctypes.c_int]),
     "lordba_get_variant": (ctypes.c_int, []),
@@ -511,6 +557,87 @@ def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out: Optiona
     """out = residual + (keep ? x / (1 - p) : 0), p to the nearest 1/65536; keep follows from (row, column, seed,
     offset), so the same call on the gradient (without a residual) is the backward pass.  out may be x or residual."""
     return _native().dropout(x, p, seed, offset, residual, out, stream)
+
+
+def int4_row_bytes(d_in: int) -> int:
+    return int(load().lordba_int4_row_bytes(d_in))
+
+
+def int4_pack(values: torch.Tensor, q: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """uint8 values (d_out, d_in), of which the low four bits count -> the 4-bit carrier, uint8 (d_out, int4_row_bytes(d_in)):
+    for integers that another program quantised.  ``include/lordba.h`` states the carrier's layout."""
+    return _native().int4_pack(values, q, stream)
+
+
+def int4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, dtype: Optional[torch.dtype] = None,
+                  q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, zero: Optional[torch.Tensor] = None, stream=None):
+    """Weights (d_out, d_in) in bfloat16, float16 or float32 -> (q, scale, zero): the 4-bit carrier, one scale for ``group``
+    neighbouring columns of a row (bfloat16 or float16: ``dtype``, or as w; bfloat16 for float32 weights) and, with zeros=True,
+    as many zero points in uint8; zero comes back as None without them (8 then stands for a zero weight)."""
+    return _native().int4_quantize(w, group, zeros, dtype, q, scale, zero, stream)
+
+
+def int4_dequantize(q, scale, d_in: int, zero=None, group: int = 128, w: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The weights (d_out, d_in) that a carrier stands for, in the type of scale; original less these is what an adapter
+    over the 4-bit base can be fitted to."""
+    return _native().int4_dequantize(q, scale, d_in, zero, group, w, stream)
+
+
+def int4_linear(x, q, scale, zero=None, group: int = 128, y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                stream=None) -> torch.Tensor:
+    """y[t, n] = sum_k x[t, k] w[n, k] with the 4-bit weights w[n, k] = scale[n, k // group] (u[n, k] - zero[n, k // group]): the
+    frozen base projection that an adapter's term is added to.  x (T, d_in), scale and y are bfloat16 or float16; y is
+    overwritten and returned.  workspace: a uint8 CUDA tensor of lordba_int4_linear_workspace_bytes(), made here if absent."""
+    return _native().int4_linear(x, q, scale, zero, group, y, workspace, stream)
+
+
+def int4_linear_backward(dy, q, scale, d_in: int, zero=None, group: int = 128, dx: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dx[t, k] = sum_n dy[t, n] w[n, k]: the gradient that a frozen 4-bit projection hands down to its input."""
+    return _native().int4_linear_backward(dy, q, scale, d_in, zero, group, dx, workspace, stream)
+
+
+def norm_rope(q, k, positions, inv_freq, w_q=None, w_k=None, eps: float = 1e-6, norm: bool = True, interleaved: bool = False,
+              q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """(q_out, k_out): queries (T, heads, d) and keys (T, key heads, d), each head vector divided by its root mean square and
+    multiplied by w_q or w_k (ones if absent; norm=False leaves the vectors as they are), then rotated by position.
+
+    positions (T): int64.  inv_freq (rotary / 2): float32; pair i of a head, entries (i, i + rotary / 2) or, interleaved, (2 i,
+    2 i + 1), turns by positions[t] * inv_freq[i]; entries from ``rotary`` on are not rotated.  Tokens and heads may lie any
+    distance apart (slices of a joint projection's output), entries side by side.  k may be None (k_out is then None).  q_out
+    and k_out may be q and k."""
+    return _native().norm_rope(q, k, positions, inv_freq, w_q, w_k, eps, norm, interleaved, q_out, k_out, stream)
+
+
+def norm_rope_backward(dq_out, dk_out, q, k, positions, inv_freq, w_q=None, w_k=None, eps: float = 1e-6, norm: bool = True,
+                       interleaved: bool = False, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                       dw_q: Optional[torch.Tensor] = None, dw_k: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dq, dk, dw_q, dw_k) from the gradients dq_out, dk_out of norm_rope's results and its inputs.  dw_q and dw_k (float32,
+    summed over tokens and heads) are made where w_q and w_k are given; what is not made comes back as None."""
+    return _native().norm_rope_backward(dq_out, dk_out, q, k, positions, inv_freq, w_q, w_k, eps, norm, interleaved, dq, dk, dw_q, dw_k,
+                                        workspace, stream)
+
+
+def distill_loss(logits, ids, teacher, temperature: float = 1.0, weight: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, grad: bool = False, stream=None):
+    """(loss, lse, dlogits): the divergence of the student's distribution from the teacher's, of which the largest logits
+    were kept.
+
+    logits (T, vocab): the student's.  ids, teacher (T, top): the classes (int64 or int32; one outside of the vocabulary is an
+    absent entry) and the teacher's logits there.  With p the softmax of teacher / temperature over a row's present entries and
+    lse the log-sum of exp(logits / temperature), loss = weight * temperature^2 * sum p (log p - logits[ids] / temperature + lse).
+    weight (T, float32; ones if absent): a row of weight 0, or without an entry, has loss 0 and gradient 0.
+
+    grad=True (or dlogits given) makes the gradient of sum(loss) in the same pass over the logits; dlogits may be the logits.
+    Otherwise dlogits comes back as None, and distill_backward makes it from lse."""
+    return _native().distill_loss(logits, ids, teacher, temperature, weight, loss, lse, dlogits, grad, stream)
+
+
+def distill_backward(dloss, logits, ids, teacher, lse, temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The gradient to the logits from those of the losses (dloss, T float32; times the weight, where distill_loss had one) and
+    the lse that distill_loss returned.  dlogits may be the logits."""
+    return _native().distill_backward(dloss, logits, ids, teacher, lse, temperature, dlogits, stream)
 
 
 def adapter_bits(d_in: int, d_out: int, r: int, ell: int = 1) -> int:
