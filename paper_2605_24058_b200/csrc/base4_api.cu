@@ -80,6 +80,11 @@ struct Int4Workspace {
 Int4Workspace int4_workspace(const lordba_int4_proj &p, int64_t T, int dtype, bool backward)
 {
     Int4Workspace w = {};
+    if (!backward && T <= kInt4Few) {
+        // activations off 16-byte boundaries are copied first
+        if (!aligned(p.in, 16) || p.ld_in % 8) w.bytes = ((size_t)T * (size_t)((p.d_in + 7) / 8 * 8) * 2 + 255) / 256 * 256;
+        return w;
+    }
     w.ldw = (p.d_in + 7) / 8 * 8;
     w.weights = ((size_t)p.d_out * (size_t)w.ldw * 2 + 255) / 256 * 256;
     // the weights' place says only that they lie aligned
@@ -102,6 +107,17 @@ int int4_call(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, 
     rc = check_workspace(w.bytes, workspace, workspace_bytes);
     if (rc != LORDBA_OK) return rc;
     lordba_int4_proj wide = *p;
+    if (!backward && T <= kInt4Few) {
+        if (w.bytes) {
+            wide.in = workspace;
+            wide.ld_in = (p->d_in + 7) / 8 * 8;
+            RepackList list = {};
+            list.item[list.n++] = RepackList::Item{p->in, workspace, p->ld_in * 2, wide.ld_in * 2, T, p->d_in * 2};
+            rc = launch_repack(list, static_cast<cudaStream_t>(stream));
+            if (rc != LORDBA_OK) return rc;
+        }
+        return launch_int4_few(wide, T, dtype, static_cast<cudaStream_t>(stream));
+    }
     wide.out = workspace;
     wide.ld_out = w.ldw;
     rc = launch_int4_dequantize(wide, dtype, static_cast<cudaStream_t>(stream));

@@ -142,6 +142,10 @@ int launch_int4_quantize(const void *w, int64_t ldw, int wdtype, uint8_t *q, int
                          int64_t ld_zero, int64_t d_out, int64_t d_in, int group, int dtype, cudaStream_t stream);
 int launch_int4_dequantize(const lordba_int4_proj &p, int dtype, cudaStream_t stream);      // to p.out
 
+// --- int4_few.cu -------------------------------------------------------------
+constexpr int64_t kInt4Few = 16;        // tokens it takes at most
+int launch_int4_few(const lordba_int4_proj &p, int64_t T, int dtype, cudaStream_t stream);
+
 // --- rope.cu -----------------------------------------------------------------
 int launch_norm_rope(const lordba_norm_rope_args &f, int64_t T, int dtype, cudaStream_t stream);
 size_t norm_rope_backward_bytes(const lordba_norm_rope_grad_args &a, int64_t T);
