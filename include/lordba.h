@@ -629,7 +629,8 @@ int lordba_norm_rope_backward(const lordba_norm_rope_grad_args *a, int64_t T, in
  * in `weight`; loss is not looked at.  weight may be NULL: ones.  dlogits may be logits (same pitch).
  *
  * dtype: logits and dlogits; teacher_dtype: teacher.  Each LORDBA_BF16, LORDBA_F16 or LORDBA_F32.  1 <= top <=
- * LORDBA_DISTILL_MAX_TOP.  temperature > 0.  T = 0 is a no-op.
+ * LORDBA_DISTILL_MAX_TOP.  temperature > 0.  T = 0 is a no-op.  The workspace (the same for both calls, 0 bytes for few
+ * rows) holds the teacher's part of every row: [device], 256-byte aligned.
  */
 #define LORDBA_DISTILL_MAX_TOP 256
 #define LORDBA_DISTILL_IDS_64 1
@@ -644,8 +645,9 @@ typedef struct lordba_distill {
     float   temperature;
     int32_t teacher_dtype, flags;
 } lordba_distill;
-int lordba_distill_loss(const lordba_distill *d, int64_t T, int dtype, void *stream);
-int lordba_distill_backward(const lordba_distill *d, int64_t T, int dtype, void *stream);
+size_t lordba_distill_workspace_bytes(const lordba_distill *d, int64_t T);
+int lordba_distill_loss(const lordba_distill *d, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+int lordba_distill_backward(const lordba_distill *d, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Storage of one adapter in bits, Eq. 5: r(d_in+d_out) + 16 ell (d_in+r+d_out). */
 int64_t lordba_adapter_bits(int64_t d_in, int64_t d_out, int r, int ell);

@@ -258,6 +258,15 @@ int check_distill(const lordba_distill &d, int64_t T, int dtype, bool backward)
     return LORDBA_OK;
 }
 
+int distill_call(const lordba_distill *d, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream, bool backward)
+{
+    if (!d) return LORDBA_EINVAL;
+    int rc = check_distill(*d, T, dtype, backward);
+    if (rc != LORDBA_OK || T == 0) return rc;
+    rc = check_workspace(distill_bytes(*d, T), workspace, workspace_bytes);
+    return rc != LORDBA_OK ? rc : launch_distill(*d, T, dtype, backward, workspace, static_cast<cudaStream_t>(stream));
+}
+
 }  // namespace
 }  // namespace lordba
 
@@ -374,18 +383,20 @@ int lordba_norm_rope_backward(const lordba_norm_rope_grad_args *a, int64_t T, in
     return rc != LORDBA_OK ? rc : launch_norm_rope_backward(*a, T, dtype, workspace, s);
 }
 
-int lordba_distill_loss(const lordba_distill *d, int64_t T, int dtype, void *stream)
+size_t lordba_distill_workspace_bytes(const lordba_distill *d, int64_t T)
 {
-    if (!d) return LORDBA_EINVAL;
-    const int rc = check_distill(*d, T, dtype, false);
-    return rc != LORDBA_OK || T == 0 ? rc : launch_distill(*d, T, dtype, false, static_cast<cudaStream_t>(stream));
+    if (!d || bad_size(T, d->vocab) || d->top < 1 || d->top > LORDBA_DISTILL_MAX_TOP) return 0;
+    return distill_bytes(*d, T);
 }
 
-int lordba_distill_backward(const lordba_distill *d, int64_t T, int dtype, void *stream)
+int lordba_distill_loss(const lordba_distill *d, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!d) return LORDBA_EINVAL;
-    const int rc = check_distill(*d, T, dtype, true);
-    return rc != LORDBA_OK || T == 0 ? rc : launch_distill(*d, T, dtype, true, static_cast<cudaStream_t>(stream));
+    return distill_call(d, T, dtype, workspace, workspace_bytes, stream, false);
+}
+
+int lordba_distill_backward(const lordba_distill *d, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return distill_call(d, T, dtype, workspace, workspace_bytes, stream, true);
 }
 
 }  // extern "C"

@@ -42,6 +42,7 @@ struct Library {
     decltype(&lordba_norm_rope) rope;
     decltype(&lordba_norm_rope_backward_workspace_bytes) rope_bytes;
     decltype(&lordba_norm_rope_backward) rope_grad;
+    decltype(&lordba_distill_workspace_bytes) distill_bytes;
     decltype(&lordba_distill_loss) distill[2];
 };
 Library lib = {};
@@ -680,7 +681,7 @@ PyObject *distill_loss(PyObject *const *a)
     std::optional<Tensor> loss = optional_tensor(a[5], "loss"), lse = optional_tensor(a[6], "lse"), dlogits = optional_tensor(a[7], "dlogits");
     const int grad = PyObject_IsTrue(a[8]);
     if (grad < 0) throw python_error();
-    const Where at(a[9]);
+    const Where at(a[10]);
     const int code = code_of(logits.scalar_type(), "logits");
     lordba_distill d = {};
     const int64_t T = distill_inputs(d, logits, a[1], a[2], a[3], weight, "weight", at);
@@ -691,7 +692,8 @@ PyObject *distill_loss(PyObject *const *a)
     d.loss = const_cast<float *>(vector(*loss, T, at, "loss"));
     d.lse = const_cast<float *>(vector(*lse, T, at, "lse"));
     d.dlogits = data(dlogits);
-    check(lib.distill[0](&d, T, code, at.stream), "lordba_distill_loss");
+    const Workspace ws(lib.distill_bytes(&d, T), a[9], at);
+    check(lib.distill[0](&d, T, code, ws.p, ws.bytes, at.stream), "lordba_distill_loss");
     for (int i : {5, 6, 7}) written(a[i]);
     return tuple_of(loss, lse, dlogits);
 }
@@ -700,7 +702,7 @@ PyObject *distill_backward(PyObject *const *a)
 {
     const Tensor &dloss = tensor(a[0], "dloss"), &logits = tensor(a[1], "logits"), &lse = tensor(a[4], "lse");
     std::optional<Tensor> dlogits = optional_tensor(a[6], "dlogits");
-    const Where at(a[7]);
+    const Where at(a[8]);
     const int code = code_of(logits.scalar_type(), "logits");
     lordba_distill d = {};
     const int64_t T = distill_inputs(d, logits, a[2], a[3], a[5], dloss, "dloss", at);
@@ -708,7 +710,8 @@ PyObject *distill_backward(PyObject *const *a)
     d.ld_dlogits = pitch(*dlogits, T, d.vocab, logits.scalar_type(), at, "dlogits");
     d.lse = const_cast<float *>(vector(lse, T, at, "lse"));
     d.dlogits = dlogits->data_ptr();
-    check(lib.distill[1](&d, T, code, at.stream), "lordba_distill_backward");
+    const Workspace ws(lib.distill_bytes(&d, T), a[7], at);
+    check(lib.distill[1](&d, T, code, ws.p, ws.bytes, at.stream), "lordba_distill_backward");
     written(a[6]);
     return wrapped(dlogits);
 }
@@ -744,6 +747,7 @@ PyObject *bind(PyObject *const *a)
     find(found.rope, "lordba_norm_rope");
     find(found.rope_bytes, "lordba_norm_rope_backward_workspace_bytes");
     find(found.rope_grad, "lordba_norm_rope_backward");
+    find(found.distill_bytes, "lordba_distill_workspace_bytes");
     find(found.distill[0], "lordba_distill_loss");
     find(found.distill[1], "lordba_distill_backward");
     lib = found;
@@ -796,8 +800,8 @@ PyMethodDef methods[] = {method<bind, 2>("bind"),
                          method<int4_linear_backward, 9>("int4_linear_backward"),
                          method<norm_rope, 12>("norm_rope"),
                          method<norm_rope_backward, 17>("norm_rope_backward"),
-                         method<distill_loss, 10>("distill_loss"),
-                         method<distill_backward, 8>("distill_backward"),
+                         method<distill_loss, 11>("distill_loss"),
+                         method<distill_backward, 9>("distill_backward"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

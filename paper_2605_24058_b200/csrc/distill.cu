@@ -1,24 +1,40 @@
 // Distillation from a teacher's top logits: the loss of a row, its log-sum, and the gradient to the student's logits.
 //
 // Bound: HBM.  A row's logits are read once, and for the gradient written once, because the row stays in registers in
-// between: 64 KB of it in a CTA of 512 threads, and a row that is longer, or one of few, is shared by a cluster of up to eight
-// CTAs, which exchange their maxima and sums through distributed shared memory.  All of a thread's loads are on the way
-// before it looks at the first.  (What a row has beyond eight CTAs' registers is read again, from L2.)
+// between: eight 16-byte pieces a thread, all on the way before the first is looked at.  A row belongs to a CTA, or, where it is
+// long or rows are few, to a cluster of up to eight, which exchange maxima and sums through distributed shared memory.  A
+// thousand threads an SM, in CTAs as small as a row allows: while some wait for a row to arrive or for one another, others
+// calculate or write.  (What a row has beyond eight CTAs' registers is read again, from L2.)
 //
-// The exponentials are powers of two of  z log2(e)/temperature - m : one multiply-add and one instruction each.
+// Persistent CTAs that had the copy engine fetch rows ahead, with a row's exponentials kept in registers between the passes,
+// were slower (4096 x 131072 in bf16 1190 us, this 460; 2048 x 32000 128 and 68): a row is a chain of latencies for the warps that
+// share it, and what hides it is many rows at a time.
+//
+// Pieces lie on 16-byte boundaries whatever the row's alignment is: the first and last are masked, and results that lie
+// otherwise are joined from the pieces of neighbouring lanes.
+//
+// The exponentials are powers of two of  z log2(e)/temperature - m : a multiply-add (of two at a time) and one instruction each.
+//
+// The teacher's part of a row (softmax of the top entries, the student's logits there) is a chain of latencies too: for many rows a
+// kernel of its own goes through it first.
 #include <cstring>
+#include <type_traits>
 
 #include "block_checks.h"
-#include "block_common.cuh"
-#include "sm100.cuh"
+#include "product_internal.cuh"
 
 namespace lordba {
 namespace {
 
-constexpr int kMaxThreads = 512;
-constexpr int kMaxSplit = 8;
-constexpr int kMaxTop = LORDBA_DISTILL_MAX_TOP, kPerLane = kMaxTop / 32;
+using namespace sm100;
+
+constexpr int kHeld = 8;                  // pieces a thread keeps
+constexpr int kMaxSplit = 8, kMaxThreads = 512;
+// Rows up to which each does its teacher's part itself: a chain of accesses that wait for one another, 2 us where the GPU is
+// idle, but more than twice that among other rows' traffic, where a kernel of its own before (one more launch, 1.5 us) pays.
+constexpr int64_t kDistillAlone = 128;
 constexpr float kLn2 = 0.6931471805599453f;
+enum Mode { kLoss, kStep, kBack };
 
 struct DistillArgs {
     const void *logits, *ids, *teacher;
@@ -26,9 +42,12 @@ struct DistillArgs {
     float *loss, *lse;
     void *dlogits;
     int64_t ld_logits, ld_ids, ld_teacher, ld_dlogits, vocab;
-    int top, ids64, teacher_dtype, split;
-    float temperature, inverse, scale;        // scale: log2(e) / temperature
-    int vec_in, vec_out;
+    int top, ids64, teacher_dtype;
+    int split, split_log2, part;          // CTAs a row, a power of two; classes of one
+    int table;                            // entries of the hash table of classes: a power of two, at least twice `top`
+    float temperature, inverse, scale;    // scale: log2(e) / temperature
+    uint4 *entries;                       // of all rows, as the teacher's kernel leaves them, or null
+    uint2 *heads;
 };
 
 __device__ __forceinline__ float exp2_of(float x)
@@ -38,233 +57,480 @@ __device__ __forceinline__ float exp2_of(float x)
     return y;
 }
 
-// sum of 2^(scale (z - max)) and the max it is relative to
+// A sum of 2^(scale (z - max)) and the max it is relative to.
 struct Stat {
     float max, sum;
 };
-__device__ __forceinline__ Stat join(Stat a, Stat b, float scale)
+
+// One of the teacher's top classes: its probability there and the logarithm of it, the student's logit.
+struct __align__(16) Entry {
+    int id;
+    float p, log, z;
+};
+struct Head {
+    float sum;
+    int twice;
+};
+
+// Two floats in one register pair, worked on by one instruction.
+struct Two {
+    uint64_t v;
+};
+__device__ __forceinline__ Two two(float a, float b)
 {
-    // of an empty side (-inf, 0), or one of minus infinities only, nothing is taken; a NaN sum stays one
-    const float m = fmaxf(a.max, b.max), at = m == -INFINITY ? 0.0f : m;
-    return Stat{m, a.sum * exp2_of((a.max - at) * scale) + b.sum * exp2_of((b.max - at) * scale)};
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 halves(Two t)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(t.v));
+    return r;
+}
+__device__ __forceinline__ Two fma_two(Two a, Two b, Two c)
+{
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Two mul_two(Two a, Two b)
+{
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two add_two(Two a, Two b)
+{
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
 }
 
-template <typename E> constexpr int kHeld = sizeof(E) == 4 ? 4 : 8;        // groups of eight a thread keeps
-
-// STAT: max and sum are looked for (and loss and lse written); else lse is given.  GRAD: dlogits is written.
-template <typename E, bool STAT, bool GRAD>
-__global__ void __launch_bounds__(kMaxThreads, 2)
-distill_kernel(const __grid_constant__ DistillArgs A)
+// The logits of a piece.
+template <typename E>
+__device__ __forceinline__ void unpack_chunk(uint4 w, Two v[8 / sizeof(E)])
 {
-    __shared__ float top_p[kMaxTop], top_log[kMaxTop], top_z[kMaxTop];      // p, log p, the student's logit
-    __shared__ int top_id[kMaxTop];
-    __shared__ Stat part[kMaxThreads / 32], peers[kMaxSplit];
-    __shared__ float teacher_live;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
-    const int64_t t = blockIdx.x / A.split;
-    const int rank = blockIdx.x - (int)t * A.split;
-    const int groups = (int)((A.vocab + 7) / 8);
-    const int first = (int)((int64_t)groups * rank / A.split), last = (int)((int64_t)groups * (rank + 1) / A.split);
-    const int V = (int)A.vocab;
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i] = two(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2<E>(u[i]);
+            v[i] = two(f.x, f.y);
+        }
+    }
+}
+// What does not belong to the group's part of the row becomes minus infinity.
+template <typename E>
+__device__ __noinline__ uint4 mask_chunk(uint4 w, int chunk, int off, int count)
+{
+    constexpr int N = 16 / sizeof(E);
+    uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    const int base = chunk * N - off / (int)sizeof(E);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (base + i >= 0 && base + i < count) continue;
+        if (sizeof(E) == 4) u[i] = 0xff800000u;
+        else {
+            const uint32_t low = std::is_same_v<E, __half> ? 0xfc00u : 0xff80u;
+            u[i / 2] = i % 2 ? (u[i / 2] & 0xffffu) | low << 16 : (u[i / 2] & 0xffff0000u) | low;
+        }
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+// The larger of each entry, where one is NaN the other.
+template <typename E>
+__device__ __forceinline__ void top_of_chunk(uint4 w, uint32_t top[sizeof(E) == 4 ? 1 : 2])
+{
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[0] = __float_as_uint(fmaxf(__uint_as_float(top[0]), __uint_as_float(u[i])));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (std::is_same_v<E, __half>) asm("max.f16x2 %0, %0, %1;" : "+r"(top[i % 2]) : "r"(u[i]));
+            else asm("max.bf16x2 %0, %0, %1;" : "+r"(top[i % 2]) : "r"(u[i]));
+        }
+    }
+}
+
+template <typename E>
+__device__ __forceinline__ uint4 pack_chunk(const Two v[8 / sizeof(E)])
+{
+    const float2 a = halves(v[0]), b = halves(v[1]);
+    if constexpr (sizeof(E) == 4) return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+    else {
+        const float2 c = halves(v[2]), d = halves(v[3]);
+        return make_uint4(pack2<E>(a.x, a.y), pack2<E>(b.x, b.y), pack2<E>(c.x, c.y), pack2<E>(d.x, d.y));
+    }
+}
+// Bytes [from, to) of a piece to the address that its first byte has, element by element.
+template <typename E>
+__device__ __noinline__ void store_part(uint8_t *at, uint4 w, int from, int to)
+{
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 16 / (int)sizeof(E); ++i) {
+        const int b = i * (int)sizeof(E);
+        if (b < from || b >= to) continue;
+        if (sizeof(E) == 4) *reinterpret_cast<uint32_t *>(at + b) = u[i];
+        else *reinterpret_cast<uint16_t *>(at + b) = (uint16_t)(u[i / 2] >> 16 * (i % 2));
+    }
+}
+// A warp's 32 neighbouring pieces to memory.  `at`: where the lane's piece goes; by: at's distance from the last 16-byte
+// boundary, the same for all lanes; begin, end: the bytes of the piece that exist.  Off the boundaries a lane joins the end
+// of its piece and the beginning of its neighbour's.
+template <typename E>
+__device__ __forceinline__ void store_chunks(uint8_t *at, uint4 w, int by, int begin, int end, int lane)
+{
+    if (by == 0) {
+        if (begin == 0 && end == 16) *reinterpret_cast<uint4 *>(at) = w;
+        else if (begin < end) store_part<E>(at, w, begin, end);
+        return;
+    }
+    uint4 next;
+    next.x = __shfl_down_sync(0xffffffffu, w.x, 1); next.y = __shfl_down_sync(0xffffffffu, w.y, 1);
+    next.z = __shfl_down_sync(0xffffffffu, w.z, 1); next.w = __shfl_down_sync(0xffffffffu, w.w, 1);
+    const bool whole = begin == 0 && end == 16;
+    const unsigned all = __ballot_sync(0xffffffffu, whole);
+    const bool before = lane > 0 && (all >> (lane - 1) & 1u), after = lane < 31 && (all >> (lane + 1) & 1u);
+    if (whole && after) *reinterpret_cast<uint4 *>(at + 16 - by) = join_pieces(w, next, 16 - by);
+    // what no neighbour takes along
+    const int head = whole && before ? 16 - by : begin, tail = whole && after ? 16 - by : end;
+    if (head < tail) store_part<E>(at, w, head, tail);
+}
+
+// The teacher's entries of a row, by one warp, into shared memory.  sum: 0 where no entry has a chance; twice: whether a
+// class stands there twice (a hash table of `slots` classes says so).
+template <typename E>
+__device__ __forceinline__ Head teacher_of(const DistillArgs &A, int64_t t, Entry *top, int *table, int slots, int lane)
+{
     const E *z = static_cast<const E *>(A.logits) + t * A.ld_logits;
+    for (int i = lane; i < slots; i += 32) table[i] = -1;
+    __syncwarp();
+    float most = -INFINITY;
+    bool met = false;
+#pragma unroll 2
+    for (int j = lane; j < A.top; j += 32) {
+        const int64_t k = A.ids64 ? static_cast<const int64_t *>(A.ids)[t * A.ld_ids + j] : (int64_t)static_cast<const int32_t *>(A.ids)[t * A.ld_ids + j];
+        const int64_t at = t * A.ld_teacher + j;
+        float v = A.teacher_dtype == LORDBA_F32    ? static_cast<const float *>(A.teacher)[at]
+                  : A.teacher_dtype == LORDBA_BF16 ? to_float(static_cast<const __nv_bfloat16 *>(A.teacher)[at])
+                                                   : to_float(static_cast<const __half *>(A.teacher)[at]);
+        const bool in = k >= 0 && k < A.vocab;
+        if (!in) v = -INFINITY;
+        top[j] = Entry{in ? (int)k : -1, 0.0f, v, in ? to_float(z[k]) : 0.0f};
+        most = fmaxf(most, v);
+        for (uint32_t h = (uint32_t)k * 2654435769u; in; ++h) {
+            const int was = atomicCAS(&table[h & (slots - 1)], -1, (int)k);
+            met |= was == (int)k;
+            if (was == -1 || was == (int)k) break;
+        }
+    }
+    for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    float sum = 0.0f;                      // a NaN comes through here
+    for (int j = lane; j < A.top; j += 32) {
+        const float v = top[j].log, x = v == -INFINITY ? v : __fdiv_rn(v - most, A.temperature), e = expf(x);
+        top[j].log = x;
+        top[j].p = e;
+        sum += e;
+    }
+    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float log_sum = logf(sum), inverse = 1.0f / sum;
+    for (int j = lane; j < A.top; j += 32) {
+        top[j].p = top[j].log == -INFINITY ? 0.0f : top[j].p * inverse;
+        top[j].log -= log_sum;
+    }
+    const Head h{sum, (int)__any_sync(0xffffffffu, met)};
+    __syncwarp();
+    return h;
+}
+
+// The teacher's part of every row, a warp each, for the kernel below.
+template <typename E>
+__global__ void __launch_bounds__(128)
+distill_teacher_kernel(const __grid_constant__ DistillArgs A, int64_t T)
+{
+    extern __shared__ __align__(16) uint8_t own[];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int64_t t = (int64_t)blockIdx.x * 4 + warp;
+    Entry *top = reinterpret_cast<Entry *>(own) + warp * A.top;
+    int *table = reinterpret_cast<int *>(own + 4 * A.top * sizeof(Entry)) + warp * A.table;
     grid_wait();
     grid_release();
-    if (STAT && A.split > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");    // the peers run
-    const float weight = A.weight ? A.weight[t] : 1.0f;
-    constexpr int H = kHeld<E>;
-    Group8<E> held[H];
-    const bool wanted = STAT || weight != 0.0f;
-    if (wanted) {
-#pragma unroll
-        for (int i = 0; i < H; ++i) {
-            const int g = first + threadIdx.x + i * blockDim.x;
-            if (g < last) held[i] = load8(z, g, V, A.vec_in);
-        }
+    if (t >= T) return;
+    const Head h = teacher_of<E>(A, t, top, table, A.table, lane);
+    for (int j = lane; j < A.top; j += 32) A.entries[t * A.top + j] = *reinterpret_cast<const uint4 *>(top + j);
+    if (lane == 0) A.heads[t] = make_uint2(__float_as_uint(h.sum), (uint32_t)h.twice);
+}
+
+// Loss and lse of a row, by one warp.
+__device__ __forceinline__ void loss_of(const DistillArgs &A, int64_t t, const Entry *top, Stat all, float weight, bool live, int lane)
+{
+    // log p - log q from what is left of both maxima: neither lse nor a logit of its size enters
+    const float log_sum = logf(all.sum);
+    float loss = 0.0f;
+    for (int j = lane; j < A.top; j += 32)
+        if (top[j].p != 0.0f) loss += top[j].p * (top[j].log - ((top[j].z - all.max) * A.inverse - log_sum));
+    for (int o = 16; o; o /= 2) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+    if (lane == 0) {
+        A.lse[t] = all.max * A.inverse + log_sum;
+        A.loss[t] = live ? weight * A.temperature * A.temperature * loss : 0.0f;
     }
-    // the teacher: warp 0, entry lane + 32 i
-    if (warp == 0) {
-        float v[kPerLane], zt[kPerLane];
-        int id[kPerLane];
-        float most = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kPerLane; ++i) {
-            const int j = lane + 32 * i;
-            v[i] = -INFINITY; id[i] = -1; zt[i] = 0.0f;
-            if (j < A.top) {
-                const int64_t k = A.ids64 ? static_cast<const int64_t *>(A.ids)[t * A.ld_ids + j]
-                                          : (int64_t)static_cast<const int32_t *>(A.ids)[t * A.ld_ids + j];
-                if (k >= 0 && k < A.vocab) {
-                    id[i] = (int)k;
-                    const int64_t at = t * A.ld_teacher + j;
-                    v[i] = A.teacher_dtype == LORDBA_F32    ? static_cast<const float *>(A.teacher)[at]
-                           : A.teacher_dtype == LORDBA_BF16 ? to_float(static_cast<const __nv_bfloat16 *>(A.teacher)[at])
-                                                            : to_float(static_cast<const __half *>(A.teacher)[at]);
-                    // dlogits may be the logits: CTAs that share a row without a barrier read here only what they write themselves
-                    const bool own = k >= 8 * (int64_t)first && k < 8 * (int64_t)last;
-                    if (STAT || own) zt[i] = to_float(z[k]);
-                }
-            }
-            most = fmaxf(most, v[i]);
+}
+
+// The gradients of the teacher's entries, every `by`-th from `at` on, over what was put there.
+template <typename E>
+__device__ __forceinline__ void patch_row(const DistillArgs &A, int64_t t, int first, int count, const Entry *top, bool twice, float factor,
+                                          float shift, int at, int by = 32)
+{
+    E *dz = static_cast<E *>(A.dlogits) + t * A.ld_dlogits;
+    for (int j = at; j < A.top; j += by) {
+        const Entry e = top[j];
+        if (e.id < first || e.id >= first + count) continue;
+        float p = e.p;
+        if (twice) {                       // a class that stands there twice: both write the same value
+            p = 0.0f;
+            for (int k = 0; k < A.top; ++k) p += top[k].id == e.id ? top[k].p : 0.0f;
         }
-        for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        float total = 0.0f;                // 0 where no entry has a chance; a NaN comes through here
+        dz[e.id] = from_float<E>(factor * (exp2_of(fmaf(e.z, A.scale, -shift)) - p));
+    }
+}
+
+// The sides of LANES neighbouring lanes joined, in every one of them the same bits.
+template <int LANES>
+__device__ __forceinline__ Stat over_lanes(Stat s, float scale)
+{
+    float m = s.max;
+    if constexpr (LANES == 32) asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(s.max));
+    else
 #pragma unroll
-        for (int i = 0; i < kPerLane; ++i) {
-            if (v[i] != -INFINITY) v[i] = __fdiv_rn(v[i] - most, A.temperature);
-            total += expf(v[i]);
-        }
-        for (int o = 16; o; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
-        const float log_total = logf(total), inverse = 1.0f / total;
+        for (int o = LANES / 2; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float sum = s.sum * exp2_of((s.max - (m == -INFINITY ? 0.0f : m)) * scale);
 #pragma unroll
-        for (int i = 0; i < kPerLane; ++i) {
-            const int j = lane + 32 * i;
-            if (j < A.top) {
-                top_p[j] = v[i] == -INFINITY ? 0.0f : expf(v[i]) * inverse;
-                top_log[j] = v[i] - log_total;
-                top_z[j] = zt[i];
-                top_id[j] = id[i];
-            }
+    for (int o = LANES / 2; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return Stat{m, sum};
+}
+
+
+// ALONE: the row's first warp does the teacher's part itself; otherwise distill_teacher_kernel has done it for all rows.
+template <typename E, int MODE, int THREADS, bool ALONE>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
+distill_kernel(const __grid_constant__ DistillArgs A)
+{
+    extern __shared__ __align__(16) uint8_t own[];
+    constexpr int N = 16 / (int)sizeof(E), kWarps = THREADS / 32;
+    constexpr uint32_t kLow = sizeof(E) == 4 ? 0xff800000u : std::is_same_v<E, __half> ? 0xfc00fc00u : 0xff80ff80u;
+    __shared__ Stat part[kWarps], peers[kMaxSplit];
+    __shared__ Head head;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int64_t t = blockIdx.x >> A.split_log2;
+    const int rank = blockIdx.x & (A.split - 1);
+    Entry *top = reinterpret_cast<Entry *>(own);
+
+    // the CTA's part of the row, and the 16-byte pieces that hold it
+    const int first = rank * A.part, count = (int)A.vocab - first < A.part ? (int)A.vocab - first : A.part;
+    const uintptr_t row = reinterpret_cast<uintptr_t>(static_cast<const E *>(A.logits) + t * A.ld_logits + first);
+    const int off = (int)(row & 15), last = off + count * (int)sizeof(E), chunks = (last + 15) / 16;
+    const uint4 *in = reinterpret_cast<const uint4 *>(row - off) + tid;
+    const int pieces = (chunks - (tid - lane) + THREADS - 1) / THREADS;      // of the warp's first lane
+    const bool edges = off || last % 16;
+    auto mask = [&](uint4 w, int c) {
+        if (edges && (c == 0 || c == chunks - 1)) w = mask_chunk<E>(w, c, off, count);
+        return w;
+    };
+    // The teacher's kernel lets this one start only once it has itself seen the end of everything before it, so the logits are
+    // there (in L2); what that kernel makes, and what may be written over, waits for its end.
+    if (ALONE) grid_wait();
+    if (MODE != kBack && A.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // this CTA runs
+    uint4 raw[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        raw[i] = make_uint4(kLow, kLow, kLow, kLow);
+        if (tid + THREADS * i < chunks) raw[i] = __ldcg(in + THREADS * i);
+    }
+    if (!ALONE) grid_wait();
+    grid_release();
+    const float weight = A.weight ? A.weight[t] : 1.0f;
+    if constexpr (ALONE) {
+        if (warp == 0) {
+            const Head h = teacher_of<E>(A, t, top, reinterpret_cast<int *>(top + A.top), A.table, lane);
+            if (lane == 0) head = h;
         }
-        if (lane == 0) teacher_live = total;
+    } else {
+        for (int j = tid; j < A.top; j += THREADS) *reinterpret_cast<uint4 *>(top + j) = __ldcg(A.entries + t * A.top + j);
+        if (tid == 0) {
+            const uint2 h = __ldcg(A.heads + t);
+            head = Head{__uint_as_float(h.x), (int)h.y};
+        }
     }
     Stat all = {0.0f, 1.0f};
-    if (STAT) {
-        Stat s = {-INFINITY, 0.0f};
-        auto top_of = [&](const Group8<E> &h, int g) {
-            float v[8];
-            unpack_group<E>(h, v);
-            const int left = V - 8 * g;
+    if (MODE != kBack) {
+        uint32_t most[2] = {kLow, kLow};
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < left) s.max = fmaxf(s.max, v[j]);
-        };
-        auto add = [&](const Group8<E> &h, int g, float minus) {
-            float v[8];
-            unpack_group<E>(h, v);
-            const int left = V - 8 * g;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < left) s.sum += exp2_of(fmaf(v[j], A.scale, minus));
-        };
-#pragma unroll
-        for (int i = 0; i < H; ++i) {
-            const int g = first + threadIdx.x + i * blockDim.x;
-            if (g < last) top_of(held[i], g);
+        for (int i = 0; i < kHeld; ++i) {
+            if (i >= pieces) break;
+            raw[i] = mask(raw[i], tid + THREADS * i);
+            top_of_chunk<E>(raw[i], most);
         }
-        for (int g = first + threadIdx.x + H * blockDim.x; g < last; g += blockDim.x) top_of(load8(z, g, V, A.vec_in), g);
+        for (int c = tid + THREADS * kHeld; c < chunks; c += THREADS) top_of_chunk<E>(mask(in[c - tid], c), most);
+        Stat s;
+        if constexpr (sizeof(E) == 4) s.max = __uint_as_float(most[0]);
+        else {
+            const float2 x = unpack2<E>(most[0]), y = unpack2<E>(most[1]);
+            s.max = fmaxf(fmaxf(x.x, x.y), fmaxf(y.x, y.y));
+        }
         const float minus = s.max == -INFINITY ? 0.0f : -s.max * A.scale;
+        const Two scales = two(A.scale, A.scale), minuses = two(minus, minus);
+        Two sums[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
+        auto add = [&](uint4 w) {
+            Two v[N / 2];
+            unpack_chunk<E>(w, v);
 #pragma unroll
-        for (int i = 0; i < H; ++i) {
-            const int g = first + threadIdx.x + i * blockDim.x;
-            if (g < last) add(held[i], g, minus);
+            for (int j = 0; j < N / 2; ++j) {
+                const float2 x = halves(fma_two(v[j], scales, minuses));
+                sums[j % 2] = add_two(sums[j % 2], two(exp2_of(x.x), exp2_of(x.y)));
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            if (i >= pieces) break;
+            add(raw[i]);
         }
-        for (int g = first + threadIdx.x + H * blockDim.x; g < last; g += blockDim.x) add(load8(z, g, V, A.vec_in), g, minus);
-        for (int o = 16; o; o /= 2)
-            s = join(s, Stat{__shfl_xor_sync(0xffffffffu, s.max, o), __shfl_xor_sync(0xffffffffu, s.sum, o)}, A.scale);
+        for (int c = tid + THREADS * kHeld; c < chunks; c += THREADS) add(mask(in[c - tid], c));
+        const float2 sum = halves(add_two(sums[0], sums[1]));
+        s.sum = sum.x + sum.y;
+        s = over_lanes<32>(s, A.scale);
         if (lane == 0) part[warp] = s;
         __syncthreads();
-        if (A.split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (warp == 0) {
-            s = lane < warps ? part[lane] : Stat{-INFINITY, 0.0f};
-            for (int o = 16; o; o /= 2)
-                s = join(s, Stat{__shfl_xor_sync(0xffffffffu, s.max, o), __shfl_xor_sync(0xffffffffu, s.sum, o)}, A.scale);
-            if (A.split == 1) {
-                if (lane == 0) peers[0] = s;
-            } else if (lane < A.split) {
-                const uint32_t to = sm100::peer_addr(sm100::smem_addr(&peers[rank]), lane);
-                sm100::store_peer(to, __float_as_uint(s.max));
-                sm100::store_peer(to + 4, __float_as_uint(s.sum));
+        s = over_lanes<kWarps>(part[lane % kWarps], A.scale);
+        if (A.split > 1) {
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (warp == 0 && lane < A.split) {
+                const uint32_t to = peer_addr(smem_addr(&peers[rank]), lane);
+                store_peer(to, __float_as_uint(s.max));
+                store_peer(to + 4, __float_as_uint(s.sum));
             }
             __syncwarp();
+            // what the first warps have pushed is all that the peers must see
+            if (warp == 0) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            else asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            s = over_lanes<kMaxSplit>(lane % kMaxSplit < A.split ? peers[lane % kMaxSplit] : Stat{-INFINITY, 0.0f}, A.scale);
         }
-        if (A.split > 1) sm100::cluster_sync();
-        else __syncthreads();
-        all = peers[0];
-        for (int r = 1; r < A.split; ++r) all = join(all, peers[r], A.scale);
+        all = s;
     } else {
         __syncthreads();
     }
-    const bool live = weight != 0.0f && teacher_live != 0.0f;
+    const bool live = weight != 0.0f && head.sum != 0.0f;
+    if (MODE != kBack && rank == 0 && warp == 0) loss_of(A, t, top, all, weight, live, lane);
+    if (MODE == kLoss) return;
     // logits less `shift` powers are the student's probabilities
-    const float shift = STAT ? all.max * A.scale + log2f(all.sum) : A.lse[t] * (1.0f / kLn2);
-    if (STAT && rank == 0 && warp == 0) {
-        // log p - log q from what is left of both maxima: neither lse nor a logit of its size enters
-        const float log_sum = logf(all.sum);
-        float loss = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kPerLane; ++i) {
-            const int j = lane + 32 * i;
-            if (j < A.top && top_p[j] != 0.0f) loss += top_p[j] * (top_log[j] - ((top_z[j] - all.max) * A.inverse - log_sum));
-        }
-        for (int o = 16; o; o /= 2) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-        if (lane == 0) {
-            A.lse[t] = all.max * A.inverse + log_sum;
-            A.loss[t] = live ? weight * A.temperature * A.temperature * loss : 0.0f;
-        }
-    }
-    if (!GRAD) return;
-    E *dz = static_cast<E *>(A.dlogits) + t * A.ld_dlogits;
+    const float shift = MODE != kBack ? all.max * A.scale + log2f(all.sum) : A.lse[t] * (1.0f / kLn2);
     const float factor = weight * A.temperature;
-    auto put = [&](const Group8<E> &h, int g) {
-        float v[8];
-        unpack_group<E>(h, v);
+    const Two times = two(factor, factor), scales = two(A.scale, A.scale), shifts = two(-shift, -shift);
+    uint8_t *to = reinterpret_cast<uint8_t *>(static_cast<E *>(A.dlogits) + t * A.ld_dlogits + first) - off + 16 * tid;
+    const int by = (int)(reinterpret_cast<uintptr_t>(to) & 15);
+    const bool plain = by == 0 && !edges;             // whole pieces alone
+    auto put = [&](uint4 w, int c) {
+        Two v[N / 2];
+        unpack_chunk<E>(w, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = live ? factor * exp2_of(fmaf(v[j], A.scale, -shift)) : 0.0f;
-        store8(dz, g, V, A.vec_out, v);
+        for (int j = 0; j < N / 2; ++j) {
+            const float2 x = halves(fma_two(v[j], scales, shifts));
+            v[j] = mul_two(two(exp2_of(x.x), exp2_of(x.y)), times);
+        }
+        w = pack_chunk<E>(v);
+        if (!live) w = make_uint4(0, 0, 0, 0);                        // whatever stood there
+        uint8_t *at = to + 16 * (c - tid);
+        if (plain) {
+            if (c < chunks) *reinterpret_cast<uint4 *>(at) = w;
+        } else {
+            store_chunks<E>(at, w, by, c == 0 ? off : 0, last - 16 * c < 16 ? last - 16 * c : 16, lane);
+        }
     };
 #pragma unroll
-    for (int i = 0; i < H; ++i) {
-        const int g = first + threadIdx.x + i * blockDim.x;
-        if (g < last) put(held[i], g);
+    for (int i = 0; i < kHeld; ++i) {
+        if (i >= pieces) break;
+        put(raw[i], tid + THREADS * i);
     }
-    for (int g = first + threadIdx.x + H * blockDim.x; g < last; g += blockDim.x) put(wanted ? load8(z, g, V, A.vec_in) : held[0], g);
+    for (int c0 = tid - lane + THREADS * kHeld; c0 < chunks; c0 += THREADS)
+        put(c0 + lane < chunks ? in[c0 + lane - tid] : make_uint4(kLow, kLow, kLow, kLow), c0 + lane);
     if (!live) return;
-    __syncthreads();                       // the top entries' gradients are written over what was put there
-    for (int j = threadIdx.x; j < A.top; j += blockDim.x) {
-        const int id = top_id[j];
-        if (id < 8 * first || id >= 8 * last) continue;
-        float p = 0.0f;                    // an index that stands there twice: both write the same value
-        for (int k = 0; k < A.top; ++k) p += top_id[k] == id ? top_p[k] : 0.0f;
-        dz[id] = from_float<E>(factor * (exp2_of(fmaf(top_z[j], A.scale, -shift)) - p));
-    }
+    __syncthreads();                       // the teacher's entries' gradients go over what was put there
+    if (warp * 32 < A.top) patch_row<E>(A, t, first, count, top, head.twice, factor, shift, tid, THREADS);
 }
 
-template <typename E, bool STAT, bool GRAD>
-int launch_distill_typed(DistillArgs A, int64_t T, cudaStream_t stream)
+template <typename E, int MODE, bool ALONE>
+const void *kernel_of(int threads)
 {
-    const int64_t groups = (A.vocab + 7) / 8;
-    constexpr int H = kHeld<E>;
-    // As many CTAs a row as hold it, more while there are SMs without one and a CTA keeps a kilobyte or so.
+    return threads == 64    ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 64, ALONE>)
+           : threads == 128 ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 128, ALONE>)
+           : threads == 256 ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 256, ALONE>)
+                            : reinterpret_cast<const void *>(&distill_kernel<E, MODE, 512, ALONE>);
+}
+
+template <typename E, int MODE>
+int launch_held(DistillArgs &A, int64_t T, cudaStream_t stream)
+{
+    // As many CTAs of at most kMaxThreads a row as hold it, more while there are SMs without one and a CTA keeps a few kilobytes; then
+    // the smallest CTA that holds its part.
+    const int64_t pieces = (A.vocab * (int64_t)sizeof(E) + 30) / 16;
     int split = 1;
-    while (split < kMaxSplit && (groups > (int64_t)split * kMaxThreads * H || (T * split < 148 && groups >= 256 * split))) split *= 2;
-    const int64_t mine = (groups + split - 1) / split;
-    int threads = 128;
-    while (threads < kMaxThreads && mine > (int64_t)threads * (H / 2)) threads *= 2;
-    A.split = split;
+    while (split < kMaxSplit && (pieces > (int64_t)split * kMaxThreads * kHeld || (T * split * 2 <= sm_count() && pieces >= 256 * split))) split *= 2;
     if (T * split > 0x7fffffff) return LORDBA_EUNSUPPORTED;
+    A.split = split;
+    A.split_log2 = 0;
+    while ((1 << A.split_log2) < split) ++A.split_log2;
+    A.part = (int)((A.vocab + 8 * split - 1) / (8 * split) * 8);
+    const int64_t mine = (A.part * (int64_t)sizeof(E) + 14) / 16;
+    int threads = 64;
+    while (threads < kMaxThreads && mine > (int64_t)threads * kHeld) threads *= 2;
+    const bool alone = T <= kDistillAlone;
     LaunchRec rec;
     std::memset(&rec, 0, sizeof(rec));
-    rec.func = reinterpret_cast<const void *>(&distill_kernel<E, STAT, GRAD>);
+    rec.func = alone ? kernel_of<E, MODE, true>(threads) : kernel_of<E, MODE, false>(threads);
     rec.grid[0] = (unsigned)(T * split);
     rec.grid[1] = rec.grid[2] = 1;
     rec.block = (uint32_t)threads;
-    rec.cluster = STAT ? (uint32_t)split : 1;
+    rec.smem = (uint32_t)(A.top * sizeof(Entry) + (alone ? 4 * A.table : 0));
+    rec.cluster = MODE == kBack ? 1 : (uint32_t)split;
     rec.pdl = 1;
     rec.n_args = 1;
     rec.arg_bytes[0] = sizeof(DistillArgs);
     return launch_record(rec, &A, nullptr, stream);
 }
 
-template <typename E>
-int launch_distill_mode(const DistillArgs &A, int64_t T, bool stat, cudaStream_t stream)
+template <typename E, int MODE>
+int launch_mode(DistillArgs &A, int64_t T, cudaStream_t stream)
 {
-    if (!stat) return launch_distill_typed<E, false, true>(A, T, stream);
-    return A.dlogits ? launch_distill_typed<E, true, true>(A, T, stream) : launch_distill_typed<E, true, false>(A, T, stream);
+    if (T > kDistillAlone) {
+        const unsigned smem = 4u * (unsigned)(A.top * sizeof(Entry) + 4 * A.table);
+        const int rc = launch_kernel(distill_teacher_kernel<E>, dim3((unsigned)((T + 3) / 4), 1, 1), 128, smem, stream, A, T);
+        if (rc != LORDBA_OK) return rc;
+    }
+    return launch_held<E, MODE>(A, T, stream);
+}
+
+template <typename E>
+int launch_typed(DistillArgs &A, int64_t T, bool backward, cudaStream_t stream)
+{
+    if (backward) return launch_mode<E, kBack>(A, T, stream);
+    return A.dlogits ? launch_mode<E, kStep>(A, T, stream) : launch_mode<E, kLoss>(A, T, stream);
 }
 
 }  // namespace
 
-int launch_distill(const lordba_distill &d, int64_t T, int dtype, bool backward, cudaStream_t stream)
+size_t distill_bytes(const lordba_distill &d, int64_t T)
+{
+    return T <= kDistillAlone ? 0 : ((size_t)T * ((size_t)d.top * sizeof(Entry) + sizeof(uint2)) + 255) / 256 * 256;
+}
+
+int launch_distill(const lordba_distill &d, int64_t T, int dtype, bool backward, void *workspace, cudaStream_t stream)
 {
     DistillArgs A;
     std::memset(&A, 0, sizeof(A));
@@ -275,16 +541,17 @@ int launch_distill(const lordba_distill &d, int64_t T, int dtype, bool backward,
     A.top = (int)d.top;
     A.ids64 = d.flags & LORDBA_DISTILL_IDS_64;
     A.teacher_dtype = d.teacher_dtype;
+    A.entries = static_cast<uint4 *>(workspace);
+    A.heads = reinterpret_cast<uint2 *>(A.entries + T * d.top);
+    A.table = 32;
+    while (A.table < 2 * A.top) A.table *= 2;
     A.temperature = d.temperature;
     A.inverse = 1.0f / d.temperature;
     A.scale = (float)(1.4426950408889634 / (double)d.temperature);
-    const size_t e = elt(dtype);
-    A.vec_in = aligned(d.logits, 16) && (d.ld_logits * e) % 16 == 0;
-    A.vec_out = aligned(d.dlogits, 16) && (d.ld_dlogits * e) % 16 == 0;
     switch (dtype) {
-        case LORDBA_BF16: return launch_distill_mode<__nv_bfloat16>(A, T, !backward, stream);
-        case LORDBA_F16: return launch_distill_mode<__half>(A, T, !backward, stream);
-        default: return launch_distill_mode<float>(A, T, !backward, stream);
+        case LORDBA_BF16: return launch_typed<__nv_bfloat16>(A, T, backward, stream);
+        case LORDBA_F16: return launch_typed<__half>(A, T, backward, stream);
+        default: return launch_typed<float>(A, T, backward, stream);
     }
 }
 

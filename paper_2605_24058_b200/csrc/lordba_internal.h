@@ -152,7 +152,8 @@ size_t norm_rope_backward_bytes(const lordba_norm_rope_grad_args &a, int64_t T);
 int launch_norm_rope_backward(const lordba_norm_rope_grad_args &a, int64_t T, int dtype, void *workspace, cudaStream_t stream);
 
 // --- distill.cu --------------------------------------------------------------
-int launch_distill(const lordba_distill &d, int64_t T, int dtype, bool backward, cudaStream_t stream);
+size_t distill_bytes(const lordba_distill &d, int64_t T);
+int launch_distill(const lordba_distill &d, int64_t T, int dtype, bool backward, void *workspace, cudaStream_t stream);
 
 // --- product.cu --------------------------------------------------------------
 // D[m,n] = sum_k A[m,k] B[n,k], then an epilogue.  An operand is a row-major matrix; its rows run along m

@@ -154,8 +154,9 @@ _SIGNATURES = {
     "lordba_norm_rope": (ctypes.c_int, [ctypes.POINTER(NormRope), _i64, ctypes.c_int, _vp]),
     "lordba_norm_rope_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(NormRopeGrad), _i64]),
     "lordba_norm_rope_backward": (ctypes.c_int, [ctypes.POINTER(NormRopeGrad), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
-    "lordba_distill_loss": (ctypes.c_int, [ctypes.POINTER(Distill), _i64, ctypes.c_int, _vp]),
-    "lordba_distill_backward": (ctypes.c_int, [ctypes.POINTER(Distill), _i64, ctypes.c_int, _vp]),
+    "lordba_distill_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Distill), _i64]),
+    "lordba_distill_loss": (ctypes.c_int, [ctypes.POINTER(Distill), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "lordba_distill_backward": (ctypes.c_int, [ctypes.POINTER(Distill), _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
     "lordba_adapter_bits": (_i64, [_i64, _i64, ctypes.c_int, ctypes.c_int]),
     "lordba_set_variant": (ctypes.c_int, [ctypes.c_int]),
     "lordba_get_variant": (ctypes.c_int, []),
@@ -620,7 +621,8 @@ def norm_rope_backward(dq_out, dk_out, q, k, positions, inv_freq, w_q=None, w_k=
 
 
 def distill_loss(logits, ids, teacher, temperature: float = 1.0, weight: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None,
-                 lse: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, grad: bool = False, stream=None):
+                 lse: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, grad: bool = False,
+                 workspace: Optional[torch.Tensor] = None, stream=None):
     """(loss, lse, dlogits): the divergence of the student's distribution from the teacher's, of which the largest logits
     were kept.
 
@@ -631,13 +633,14 @@ def distill_loss(logits, ids, teacher, temperature: float = 1.0, weight: Optiona
 
     grad=True (or dlogits given) makes the gradient of sum(loss) in the same pass over the logits; dlogits may be the logits.
     Otherwise dlogits comes back as None, and distill_backward makes it from lse."""
-    return _native().distill_loss(logits, ids, teacher, temperature, weight, loss, lse, dlogits, grad, stream)
+    return _native().distill_loss(logits, ids, teacher, temperature, weight, loss, lse, dlogits, grad, workspace, stream)
 
 
-def distill_backward(dloss, logits, ids, teacher, lse, temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+def distill_backward(dloss, logits, ids, teacher, lse, temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The gradient to the logits from those of the losses (dloss, T float32; times the weight, where distill_loss had one) and
     the lse that distill_loss returned.  dlogits may be the logits."""
-    return _native().distill_backward(dloss, logits, ids, teacher, lse, temperature, dlogits, stream)
+    return _native().distill_backward(dloss, logits, ids, teacher, lse, temperature, dlogits, workspace, stream)
 
 
 def adapter_bits(d_in: int, d_out: int, r: int, ell: int = 1) -> int:

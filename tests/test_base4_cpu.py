@@ -143,8 +143,11 @@ def test_distill_arguments(lib, backward):
     from paper_2605_24058_b200 import lordba
     before = lordba.launch_count()
     f = lib.lordba_distill_backward if backward else lib.lordba_distill_loss
-    call = lambda T=4, dt=lordba.BF16, **kw: f(ctypes.byref(make(lordba.Distill, DISTILL, **kw)), T, dt, None)
-    assert f(None, 4, lordba.BF16, None) == EINVAL
+    call = lambda T=4, dt=lordba.BF16, ws=None, nbytes=0, **kw: f(ctypes.byref(make(lordba.Distill, DISTILL, **kw)), T, dt, ws, nbytes, None)
+    assert f(None, 4, lordba.BF16, None, 0, None) == EINVAL
+    need = lib.lordba_distill_workspace_bytes(ctypes.byref(make(lordba.Distill, DISTILL)), 3000)
+    assert need > 0 and lib.lordba_distill_workspace_bytes(None, 4) == 0 and lib.lordba_distill_workspace_bytes(ctypes.byref(make(lordba.Distill, DISTILL)), 4) == 0
+    assert call(T=3000) == EINVAL and call(T=3000, ws=20 * FAR, nbytes=need - 1) == EINVAL and call(T=3000, ws=20 * FAR + 8, nbytes=need) == EALIGN
     assert call(T=0) == 0 and call(T=0, logits=0) == 0
     assert call(T=-1) == EINVAL and call(vocab=0) == EINVAL and call(flags=2) == EINVAL and call(dt=8) == EUNSUP and call(teacher_dtype=8) == EUNSUP
     assert call(top=0) == EINVAL and call(top=lordba.DISTILL_MAX_TOP + 1, ld_ids=300, ld_teacher=300) == EUNSUP
