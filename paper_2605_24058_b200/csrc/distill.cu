@@ -72,41 +72,6 @@ struct Head {
     int twice;
 };
 
-// Two floats in one register pair, worked on by one instruction.
-struct Two {
-    uint64_t v;
-};
-__device__ __forceinline__ Two two(float a, float b)
-{
-    Two r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 halves(Two t)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(t.v));
-    return r;
-}
-__device__ __forceinline__ Two fma_two(Two a, Two b, Two c)
-{
-    Two r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-__device__ __forceinline__ Two mul_two(Two a, Two b)
-{
-    Two r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Two add_two(Two a, Two b)
-{
-    Two r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-
 // The logits of a piece.
 template <typename E>
 __device__ __forceinline__ void unpack_chunk(uint4 w, Two v[8 / sizeof(E)])

@@ -280,6 +280,186 @@ norm_rope_kernel(const __grid_constant__ RopeArgs A)
     }
 }
 
+// ---- head vectors that are rotated whole and fill their lanes --------------------------------------------------------
+// d = 16 WIDTH entries, all rotated, all on 16-byte boundaries: what models have.  Nothing is looked at per entry, and two entries
+// are worked on by one instruction.
+template <typename E, bool INTERLEAVED>
+__device__ __forceinline__ void unpack_pairs(const Raw<E, true> &raw, Two a[4], Two b[4])
+{
+    float v[16];
+    unpack_group<E>(raw.r[0], v);
+    unpack_group<E>(raw.r[1], v + 8);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        a[j] = INTERLEAVED ? two(v[4 * j], v[4 * j + 2]) : two(v[2 * j], v[2 * j + 1]);
+        b[j] = INTERLEAVED ? two(v[4 * j + 1], v[4 * j + 3]) : two(v[8 + 2 * j], v[9 + 2 * j]);
+    }
+}
+template <typename E, bool INTERLEAVED>
+__device__ __forceinline__ void store_pairs(E *p, int l, int second, const Two a[4], const Two b[4])
+{
+    float v[16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 x = halves(a[j]), y = halves(b[j]);
+        v[INTERLEAVED ? 4 * j : 2 * j] = x.x; v[INTERLEAVED ? 4 * j + 2 : 2 * j + 1] = x.y;
+        v[INTERLEAVED ? 4 * j + 1 : 8 + 2 * j] = y.x; v[INTERLEAVED ? 4 * j + 3 : 9 + 2 * j] = y.y;
+    }
+    store_group<E>(p, v);
+    store_group<E>(p + second, v + 8);
+}
+template <int WIDTH>
+__device__ __forceinline__ float over_lanes(Two t)
+{
+    const float2 h = halves(t);
+    float v = h.x + h.y;
+#pragma unroll
+    for (int o = WIDTH / 2; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+template <typename E, bool BACK, bool INTERLEAVED, bool NORM, int WIDTH>
+__global__ void __launch_bounds__(kThreads, BACK ? 2 : 3)
+norm_rope_full_kernel(const __grid_constant__ RopeArgs A)
+{
+    constexpr int D = 16 * WIDTH, PAIRS = D / 2, PER = 32 / WIDTH, SECOND = INTERLEAVED ? 8 : PAIRS;
+    __shared__ float2 table[kWarps][PAIRS + 1];
+    __shared__ float sums[BACK && NORM ? kWarps : 1][D];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % WIDTH, mine = lane / WIDTH;
+    const int at = INTERLEAVED ? 16 * l : 8 * l;             // the lane's first run of eight; the second is SECOND behind
+    const int which = (int)blockIdx.x >= A.side[0].blocks;
+    const Side &S = A.side[which];
+    const int block = blockIdx.x - (which ? A.side[0].blocks : 0);
+    grid_wait();
+    grid_release();
+    auto entry = [&](int j, int h, bool b) {                 // of pairs 2 j + h: the first or the second
+        return INTERLEAVED ? at + 4 * j + 2 * h + b : at + 2 * j + h + (b ? SECOND : 0);
+    };
+    Two wa[4], wb[4], da[4], db[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        wa[j] = wb[j] = two(1.0f, 1.0f);
+        if (NORM && S.w) {
+            wa[j] = two(weight_at(S.w, A.w_dtype, entry(j, 0, false)), weight_at(S.w, A.w_dtype, entry(j, 1, false)));
+            wb[j] = two(weight_at(S.w, A.w_dtype, entry(j, 0, true)), weight_at(S.w, A.w_dtype, entry(j, 1, true)));
+        }
+        da[j] = db[j] = two(0.0f, 0.0f);
+    }
+    auto load = [&](const E *p, bool in) {
+        Raw<E, true> v;
+        std::memset(&v, 0, sizeof(v));
+        if (in) {
+            v.r[0] = load_group(p);
+            v.r[1] = load_group(p + SECOND);
+        }
+        return v;
+    };
+    const int64_t units = A.T * S.chunks;
+    const int64_t x_step = PER * S.x_head, g_step = PER * S.g_head, out_step = PER * S.out_head;
+    for (int64_t u = (int64_t)block * kWarps + warp; u < units; u += (int64_t)S.blocks * kWarps) {
+        const int64_t t = S.chunks == 1 ? u : u / S.chunks;
+        const int s0 = (int)(u - t * S.chunks) * S.per_unit, s1 = s0 + S.per_unit < S.steps ? s0 + S.per_unit : S.steps;
+        int h = s0 * PER + mine;
+        const E *x = static_cast<const E *>(S.x) + t * S.x_token + h * S.x_head + at;
+        const E *g = static_cast<const E *>(S.g) + (BACK ? t * S.g_token + h * S.g_head + at : 0);
+        E *out = static_cast<E *>(S.out) + t * S.out_token + h * S.out_head + at;
+        // the first heads are on their way while the angles are worked out
+        Raw<E, true> rx = load(x, h < S.heads && (!BACK || NORM)), rg;
+        if (BACK) rg = load(g, h < S.heads);
+        const double turns_of = (double)A.positions[t] * 0.15915494309189533577;       // 1 / (2 pi)
+        __syncwarp();                                        // the table's last readers
+#pragma unroll
+        for (int i = 0; i < (PAIRS + 31) / 32; ++i) {
+            const int p = lane + 32 * i;
+            if (p < PAIRS) {
+                double turns = turns_of * (double)A.inv_freq[p];
+                turns -= rint(turns);
+                float sine, cosine;
+                sincospif(2.0f * (float)turns, &sine, &cosine);
+                table[warp][p] = make_float2(cosine, BACK ? -sine : sine);
+            }
+        }
+        __syncwarp();
+        Two c[4], s[4], minus[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 p = table[warp][8 * l + 2 * j], q = table[warp][8 * l + 2 * j + 1];
+            c[j] = two(p.x, q.x); s[j] = two(p.y, q.y); minus[j] = two(-p.y, -q.y);
+        }
+#pragma unroll 1
+        for (int step = s0; step < s1; ++step) {
+            const bool in = h < S.heads;
+            Two a[4], b[4], ga[4], gb[4];
+            unpack_pairs<E, INTERLEAVED>(rx, a, b);
+            if (BACK) unpack_pairs<E, INTERLEAVED>(rg, ga, gb);
+            h += PER;
+            x += x_step;
+            if (BACK) g += g_step;
+            const bool more = step + 1 < s1 && h < S.heads;   // the next heads' loads
+            rx = load(x, more && (!BACK || NORM));
+            if (BACK) rg = load(g, more);
+            float r = 1.0f;
+            if (NORM) {
+                Two q = mul_two(a[0], a[0]), q2 = mul_two(b[0], b[0]);
+#pragma unroll
+                for (int j = 1; j < 4; ++j) { q = fma_two(a[j], a[j], q); q2 = fma_two(b[j], b[j], q2); }
+                r = rsqrtf(over_lanes<WIDTH>(add_two(q, q2)) * A.inv_d + A.eps);
+            }
+            const Two rr = two(r, r);
+            if (!BACK) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const Two na = NORM ? mul_two(a[j], mul_two(rr, wa[j])) : a[j], nb = NORM ? mul_two(b[j], mul_two(rr, wb[j])) : b[j];
+                    a[j] = fma_two(na, c[j], mul_two(nb, minus[j]));
+                    b[j] = fma_two(nb, c[j], mul_two(na, s[j]));
+                }
+            } else {
+                Two dot = two(0.0f, 0.0f), dot2 = dot;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const Two ta = fma_two(ga[j], c[j], mul_two(gb[j], minus[j])), tb = fma_two(gb[j], c[j], mul_two(ga[j], s[j]));
+                    ga[j] = ta; gb[j] = tb;
+                    if (NORM) {
+                        a[j] = mul_two(a[j], rr); b[j] = mul_two(b[j], rr);
+                        da[j] = fma_two(ta, a[j], da[j]); db[j] = fma_two(tb, b[j], db[j]);
+                        ga[j] = mul_two(ta, wa[j]); gb[j] = mul_two(tb, wb[j]);
+                        dot = fma_two(ga[j], a[j], dot); dot2 = fma_two(gb[j], b[j], dot2);
+                    }
+                }
+                if (NORM) {
+                    const float d = -over_lanes<WIDTH>(add_two(dot, dot2)) * A.inv_d;
+                    const Two dd = two(d, d);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { ga[j] = mul_two(rr, fma_two(a[j], dd, ga[j])); gb[j] = mul_two(rr, fma_two(b[j], dd, gb[j])); }
+                }
+            }
+            if (in) store_pairs<E, INTERLEAVED>(out, l, SECOND, BACK ? ga : a, BACK ? gb : b);
+            out += out_step;
+        }
+    }
+    if (BACK && NORM && S.part) {
+        // lanes of one place, then warps, in a fixed order
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 x = halves(da[j]), y = halves(db[j]);
+            float v[4] = {x.x, x.y, y.x, y.y};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                for (int o = 16; o >= WIDTH; o /= 2) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+                if (mine == 0) sums[warp][entry(j, k % 2, k >= 2)] = v[k];
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < D; i += kThreads) {
+            float v = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) v += sums[BACK && NORM ? k : 0][i];
+            S.part[(int64_t)block * D + i] = v;
+        }
+    }
+}
+
 struct JoinArgs {
     const float *part[2];
     float *dw[2];
@@ -352,11 +532,23 @@ void take(Side &S, const lordba_heads &x, const lordba_heads &g, const lordba_he
     S.w = w;
 }
 
+template <typename E, bool BACK, bool INTERLEAVED, bool NORM>
+void (*full_kernel(int width))(const RopeArgs)
+{
+    return width == 4 ? norm_rope_full_kernel<E, BACK, INTERLEAVED, NORM, 4> : width == 8 ? norm_rope_full_kernel<E, BACK, INTERLEAVED, NORM, 8>
+                                                                             : norm_rope_full_kernel<E, BACK, INTERLEAVED, NORM, 16>;
+}
+
 template <typename E, bool BACK>
 int launch_typed(const RopeArgs &A, bool interleaved, bool vec, cudaStream_t stream)
 {
-    const auto kernel = interleaved ? (vec ? norm_rope_kernel<E, BACK, true, true> : norm_rope_kernel<E, BACK, true, false>)
-                                    : (vec ? norm_rope_kernel<E, BACK, false, true> : norm_rope_kernel<E, BACK, false, false>);
+    // heads of 64, 128 and 256 entries, rotated whole
+    const bool full = vec && A.d == 16 * A.width && 2 * A.half == A.d && A.width >= 4 && A.width <= 16;
+    const auto kernel =
+        full ? (interleaved ? (A.norm ? full_kernel<E, BACK, true, true>(A.width) : full_kernel<E, BACK, true, false>(A.width))
+                            : (A.norm ? full_kernel<E, BACK, false, true>(A.width) : full_kernel<E, BACK, false, false>(A.width)))
+        : interleaved ? (vec ? norm_rope_kernel<E, BACK, true, true> : norm_rope_kernel<E, BACK, true, false>)
+                      : (vec ? norm_rope_kernel<E, BACK, false, true> : norm_rope_kernel<E, BACK, false, false>);
     return launch_kernel(kernel, dim3((unsigned)(A.side[0].blocks + A.side[1].blocks), 1, 1), kThreads, 0, stream, A);
 }
 
