@@ -19,7 +19,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblordba.so")
 TESTHOOKS_LIB = os.path.join(PKG, "liblordba_testhooks.so")
-SOURCES = ("api.cu", "block_api.cu", "base4_api.cu", "elementwise.cu", "int4.cu", "int4_few.cu", "rope.cu", "distill.cu", "product.cu", "product_tile.cu", "product_stream.cu", "pack.cu", "fit.cu", "forward_fma.cu", "forward_tc.cu", "forward_mma.cu")
+SOURCES = ("api.cu", "block_api.cu", "base4_api.cu", "elementwise.cu", "int4.cu", "int4_few.cu", "int4_stream.cu", "rope.cu", "distill.cu", "product.cu", "product_tile.cu", "product_stream.cu", "pack.cu", "fit.cu", "forward_fma.cu", "forward_tc.cu", "forward_mma.cu")
 BINDING = os.path.join(PKG, "_block.so")       # Python module of csrc/binding.cpp
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Wno-deprecated-gpu-targets",

@@ -72,23 +72,36 @@ Product int4_product(const lordba_int4_proj &p, int64_t T, int dtype, bool backw
     return q;
 }
 
+// How a product is done: a few tokens, some tens of them, or many, for which the weights are laid out in 16 bits first.
+enum class Int4Way { kFew, kStream, kWide };
+
+Int4Way int4_way(const lordba_int4_proj &p, int64_t T, bool backward)
+{
+    if (!backward && T <= kInt4Few) return Int4Way::kFew;
+    const double us = int4_stream_estimate(p, T, backward);
+    return T <= kInt4Stream && us >= 0 ? Int4Way::kStream : Int4Way::kWide;
+}
+
 struct Int4Workspace {
-    size_t weights, bytes;       // of the weights in 16 bits; in all
-    int64_t ldw;
+    Int4Way way;
+    size_t first, bytes;         // of the weights in 16 bits, or of the activations on 16-byte boundaries where they are not; in all
+    int64_t ld;
 };
 
 Int4Workspace int4_workspace(const lordba_int4_proj &p, int64_t T, int dtype, bool backward)
 {
     Int4Workspace w = {};
-    if (!backward && T <= kInt4Few) {
-        // activations off 16-byte boundaries are copied first
-        if (!aligned(p.in, 16) || p.ld_in % 8) w.bytes = ((size_t)T * (size_t)((p.d_in + 7) / 8 * 8) * 2 + 255) / 256 * 256;
+    w.way = int4_way(p, T, backward);
+    if (w.way != Int4Way::kWide) {
+        w.ld = ((backward ? p.d_out : p.d_in) + 7) / 8 * 8;
+        if (!aligned(p.in, 16) || p.ld_in % 8) w.first = ((size_t)T * (size_t)w.ld * 2 + 255) / 256 * 256;
+        w.bytes = w.first;
         return w;
     }
-    w.ldw = (p.d_in + 7) / 8 * 8;
-    w.weights = ((size_t)p.d_out * (size_t)w.ldw * 2 + 255) / 256 * 256;
+    w.ld = (p.d_in + 7) / 8 * 8;
+    w.first = ((size_t)p.d_out * (size_t)w.ld * 2 + 255) / 256 * 256;
     // the weights' place says only that they lie aligned
-    w.bytes = w.weights + product_workspace_bytes(int4_product(p, T, dtype, backward, reinterpret_cast<const void *>(uintptr_t(256)), w.ldw));
+    w.bytes = w.first + product_workspace_bytes(int4_product(p, T, dtype, backward, reinterpret_cast<const void *>(uintptr_t(256)), w.ld));
     return w;
 }
 
@@ -106,24 +119,24 @@ int int4_call(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, 
     const Int4Workspace w = int4_workspace(*p, T, dtype, backward);
     rc = check_workspace(w.bytes, workspace, workspace_bytes);
     if (rc != LORDBA_OK) return rc;
-    lordba_int4_proj wide = *p;
-    if (!backward && T <= kInt4Few) {
-        if (w.bytes) {
-            wide.in = workspace;
-            wide.ld_in = (p->d_in + 7) / 8 * 8;
-            RepackList list = {};
-            list.item[list.n++] = RepackList::Item{p->in, workspace, p->ld_in * 2, wide.ld_in * 2, T, p->d_in * 2};
-            rc = launch_repack(list, static_cast<cudaStream_t>(stream));
-            if (rc != LORDBA_OK) return rc;
-        }
-        return launch_int4_few(wide, T, dtype, static_cast<cudaStream_t>(stream));
+    const cudaStream_t on = static_cast<cudaStream_t>(stream);
+    lordba_int4_proj call = *p;
+    if (w.way == Int4Way::kWide) {
+        call.out = workspace;
+        call.ld_out = w.ld;
+        rc = launch_int4_dequantize(call, dtype, on);
+        if (rc != LORDBA_OK) return rc;
+        return launch_product(int4_product(*p, T, dtype, backward, workspace, w.ld), static_cast<uint8_t *>(workspace) + w.first, on);
     }
-    wide.out = workspace;
-    wide.ld_out = w.ldw;
-    rc = launch_int4_dequantize(wide, dtype, static_cast<cudaStream_t>(stream));
-    if (rc != LORDBA_OK) return rc;
-    return launch_product(int4_product(*p, T, dtype, backward, workspace, w.ldw), static_cast<uint8_t *>(workspace) + w.weights,
-                          static_cast<cudaStream_t>(stream));
+    if (w.first) {
+        call.in = workspace;
+        call.ld_in = w.ld;
+        RepackList list = {};
+        list.item[list.n++] = RepackList::Item{p->in, workspace, p->ld_in * 2, w.ld * 2, T, (backward ? p->d_out : p->d_in) * 2};
+        rc = launch_repack(list, on);
+        if (rc != LORDBA_OK) return rc;
+    }
+    return w.way == Int4Way::kFew ? launch_int4_few(call, T, dtype, on) : launch_int4_stream(call, T, dtype, backward, on);
 }
 
 // ---- heads --------------------------------------------------------------------------------------------------------

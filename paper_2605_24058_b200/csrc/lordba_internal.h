@@ -143,8 +143,14 @@ int launch_int4_quantize(const void *w, int64_t ldw, int wdtype, uint8_t *q, int
 int launch_int4_dequantize(const lordba_int4_proj &p, int dtype, cudaStream_t stream);      // to p.out
 
 // --- int4_few.cu -------------------------------------------------------------
+constexpr int64_t kInt4Stream = 256;    // tokens up to which the weights are widened on their way
 constexpr int64_t kInt4Few = 16;        // tokens it takes at most
 int launch_int4_few(const lordba_int4_proj &p, int64_t T, int dtype, cudaStream_t stream);
+
+// --- int4_stream.cu ----------------------------------------------------------
+// Its time in microseconds, as far as choosing needs it; < 0: cannot be had.
+double int4_stream_estimate(const lordba_int4_proj &p, int64_t T, bool backward);
+int launch_int4_stream(const lordba_int4_proj &p, int64_t T, int dtype, bool backward, cudaStream_t stream);      // p.in: as above
 
 // --- rope.cu -----------------------------------------------------------------
 int launch_norm_rope(const lordba_norm_rope_args &f, int64_t T, int dtype, cudaStream_t stream);
