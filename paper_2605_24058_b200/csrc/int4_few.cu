@@ -16,7 +16,7 @@
 #include <type_traits>
 
 #include "int4_common.cuh"
-#include "sm100.cuh"
+#include "product_internal.cuh"
 
 namespace lordba {
 namespace {
@@ -277,10 +277,15 @@ int launch_grouped(const FewArgs &A, cudaStream_t stream)
 template <typename E>
 int launch_typed(const FewArgs &A, cudaStream_t stream)
 {
-    // more tokens, more weight rows a CTA: its activations come from L2 once for all of them
-    if (A.T == 1) return launch_grouped<E, 1, 1, 8, 4>(A, stream);
-    if (A.T <= 4) return launch_grouped<E, 2, 4, 8, 4>(A, stream);
-    return A.T <= 8 ? launch_grouped<E, 2, 8, 8, 3>(A, stream) : launch_grouped<E, 2, 16, 4, 3>(A, stream);
+    // More tokens, more weight rows a CTA: its activations come from L2 once for all of them.  Where the CTAs are one to an SM, each
+    // wants more warps and more on the way; where there are more, two that share an SM do better (11008 x 4096 and 4096 x 11008, of
+    // 128 and 344 CTAs: 16 tokens with eight warps 11.9 and 16.6 us, with four 12.9 and 13.9; 8 tokens with three slots a warp 9.9 and,
+    // groups of 64 with zeros, 15.6 us, with two 11.5 and 12.3; 4 tokens with eight warps 9.2 and 17.2 us, groups of 32, with four 10.2 and 10.8).
+    if (A.T == 1) return launch_grouped<E, 1, 1, 8, 3>(A, stream);
+    const bool alone = (A.d_out + 31) / 32 <= sm_count();
+    if (A.T <= 4) return alone ? launch_grouped<E, 2, 4, 8, 4>(A, stream) : launch_grouped<E, 2, 4, 4, 4>(A, stream);
+    if (A.T <= 8) return alone ? launch_grouped<E, 2, 8, 8, 3>(A, stream) : launch_grouped<E, 2, 8, 8, 2>(A, stream);
+    return alone ? launch_grouped<E, 2, 16, 8, 3>(A, stream) : launch_grouped<E, 2, 16, 4, 3>(A, stream);
 }
 
 }  // namespace

@@ -4,15 +4,18 @@
 //   forward     y[t,n]  = sum_k x[t,k] w[n,k]       a CTA's 128 MMA rows are weight rows, the contraction runs along them
 //   backward    dx[t,k] = sum_n dy[t,n] w[n,k]      they are 128 columns (a block of the carrier), the contraction runs over rows
 //
-// Eight warps fetch packed pieces of 16 bytes, several stages ahead in registers, widen them (u - zero, exactly; times the scale,
+// Sixteen warps fetch packed pieces of 16 bytes, several steps ahead in registers, widen them (u - zero, exactly; times the scale,
 // rounded once to the type of x) and write them as the swizzled tiles that the tensor core reads; the tokens come through the copy
 // engine.  The contraction is split over a cluster of up to eight CTAs, whose sums meet in distributed shared memory and are
 // added in rank order.
 //
-// Bound: the widening.  A piece takes a lane 152 operations (a pair a shift, a choice of bits, a subtraction and a product), 5 us
-// for 4096 x 11008 weights on all SMs, where they arrive in 3.5 us; it is done once for up to 128 tokens.
+// Bound: the widening.  A pair takes a shift, a choice of bits, a subtraction and a product, and the first two go at half the
+// rate: 8 us for 4096 x 11008 weights where nothing else is done (they arrive in 3.5 us).  It is done once for up to 128 tokens.
+// Measured, weights from HBM: 4096 x 4096, 17 / 64 / 128 tokens 11.8 / 12.6 / 15.0 us, 4096 x 11008 19.4 / 21.3 / 26.1 us (laid out in
+// 16 bits first 17.4 / 18.7 / 20.5 and 36.9 / 40.0 / 43.6 us; 256 tokens take both the same).  Rings of 4 ... 12 stages, one CTA an
+// SM, and half as many warps with two pieces each gained nothing.
 //
-//   warps 0-7 widen (0-3 also move the sums), warp 8 issues MMAs and warp 9 the tokens' copies (one thread each)
+//   warps 0-15 widen (0-3 also move the sums), warp 16 issues MMAs and warp 17 the tokens' copies (one thread each)
 #include <cstring>
 #include <mutex>
 
@@ -26,7 +29,7 @@ using namespace sm100;
 
 constexpr int kRows = 128;                     // MMA rows: weight rows, or columns
 constexpr int kTile = kRows * 128;             // bytes of a stage's weights: 64 contraction steps
-constexpr int kLoaders = 8, kThreads = 32 * (kLoaders + 2);
+constexpr int kLoaders = 16, kThreads = 32 * (kLoaders + 2);
 constexpr int kMaxStages = 6, kMaxSplit = 8;
 constexpr int kBarBytes = (2 * kMaxStages + 1) * 8 + 16;
 constexpr int kSmem = 113 * 1024;              // of a CTA: two share an SM
@@ -37,25 +40,45 @@ struct StreamArgs {
     const uint16_t *scale;
     const uint8_t *zero;
     void *out;
-    int64_t ldq, ld_scale, ld_zero, ld_out;
+    uint32_t ldq, ld_scale, ld_zero;
+    int64_t ld_out;
     int64_t T, N;            // of the output
     int rows, groups;        // of the weights
     int group_log2;
-    int blocks;              // stages in all
+    int steps;               // of 128 contraction steps
     int tokens, stages, split, tmem_columns, vec_out;
     int skip;                // -1; the test-hooks build can name a stage whose copy is left out
     int *status;
     uint32_t idesc;
 };
 
-// SPB: scales of a block and row, 1, 2 or 4.  A step of the loaders is a block of 128 columns of 128 rows, two stages (forward), or
-// of 64 rows, one stage (backward): PIECES of 16 bytes a thread.
+// Loads that are issued where they stand: left to itself the compiler puts them off until shortly before their use.
+__device__ __forceinline__ uint4 load_piece(const uint8_t *p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t load_now(const uint16_t *p)
+{
+    uint32_t v;
+    asm volatile("ld.global.nc.u16 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t load_now(const uint8_t *p)
+{
+    uint32_t v;
+    asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+
+// SPB: scales of a block and row, 1, 2 or 4.
 template <typename E, bool BACK, int SPB, bool ZERO>
 __global__ void __launch_bounds__(kThreads, 2)
 int4_stream_kernel(const __grid_constant__ StreamArgs P)
 {
     extern __shared__ uint8_t smem_raw[];
-    constexpr int PIECES = BACK ? 1 : 2, STAGES_A_STEP = BACK ? 1 : 2, DEPTH = (BACK ? 2 : 1) * (SPB == 4 ? 2 : SPB == 2 ? 3 : 4);
+    constexpr int DEPTH = SPB == 4 ? 2 : SPB == 2 ? 3 : 4;        // steps fetched ahead
     const uint32_t raw = smem_addr(smem_raw), bars = raw, base = (raw + kBarBytes + 1023u) & ~1023u;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (kMaxStages + s); };
@@ -68,19 +91,19 @@ int4_stream_kernel(const __grid_constant__ StreamArgs P)
     const int stage_bytes = kTile + P.tokens * 128;
     const int t0 = blockIdx.z * P.tokens, n0 = blockIdx.y * kRows;
     // the cluster's share of the steps, in whole ones
-    const int steps = P.blocks / STAGES_A_STEP, first = steps * rank / P.split, last = steps * (rank + 1) / P.split;
+    const int first = P.steps * rank / P.split, last = P.steps * (rank + 1) / P.split;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < P.stages; ++s) {
-            bar_init(full(s), kLoaders + 1);
+            bar_init(full(s), (BACK ? kLoaders / 2 : kLoaders) + 1);
             bar_init(empty(s), 1);
         }
         bar_init(sum_full, 1);
         *abort_flag = 0;
         bar_init_fence();
     }
-    if (warp == 8) tmem_alloc<1>(smem_addr(misc), P.tmem_columns);
-    if (warp == 9 && lane == 0) prefetch_map(&P.t);
+    if (warp == kLoaders) tmem_alloc<1>(smem_addr(misc), P.tmem_columns);
+    if (warp == kLoaders + 1 && lane == 0) prefetch_map(&P.t);
     fence_before();
     __syncthreads();
     fence_after();
@@ -88,70 +111,69 @@ int4_stream_kernel(const __grid_constant__ StreamArgs P)
     grid_wait();
     grid_release();
 
-    if (warp == 9) {
+    if (warp == kLoaders + 1) {
         if (lane == 0) {
             Ring r;
-            for (int kb = first * STAGES_A_STEP; kb < last * STAGES_A_STEP; ++kb) {
+            for (int kb = 2 * first; kb < 2 * last; ++kb) {
                 if (!bound.wait(empty(r.stage), r.phase ^ 1u, kDevTmaWaitTimeout)) break;
                 bar_expect(full(r.stage), P.tokens * 128);
-                if (kb - first * STAGES_A_STEP != P.skip) load_tile(base + r.stage * stage_bytes + kTile, &P.t, kb * 64, t0, full(r.stage));
+                if (kb - 2 * first != P.skip) load_tile(base + r.stage * stage_bytes + kTile, &P.t, kb * 64, t0, full(r.stage));
                 r.next(P.stages);
             }
         }
-    } else if (warp == 8) {
+    } else if (warp == kLoaders) {
         if (lane == 0) {
             Ring r;
             bool alive = true;
-            for (int kb = first * STAGES_A_STEP; kb < last * STAGES_A_STEP; ++kb) {
+            for (int kb = 2 * first; kb < 2 * last; ++kb) {
                 alive = bound.wait(full(r.stage), r.phase, kDevMmaWaitTimeout);
                 if (!alive) break;
                 fence_after();
                 const uint32_t sw = base + r.stage * stage_bytes;
                 const uint32_t w = desc_low(sw, BACK ? kTile / 2 : 0), t = desc_low(sw + kTile);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) mma<1, false>(tmem, w + j * (BACK ? 128 : 2), t + j * 2, P.idesc, kb - first * STAGES_A_STEP + j > 0);
+                for (int j = 0; j < 4; ++j) mma<1, false>(tmem, w + j * (BACK ? 128 : 2), t + j * 2, P.idesc, kb - 2 * first + j > 0);
                 mma_commit<1>(empty(r.stage));
                 r.next(P.stages);
             }
             if (alive) mma_commit<1>(sum_full);
         }
     } else {
-        // lanes of a warp: four pieces of a row; eight rows in an order in which eight neighbouring lanes write to different banks
-        const int t = lane % 4, row = 8 * warp + (lane / 8 + lane / 4 % 2 * 4);          // and, forward, 64 rows on
-        const int column = BACK ? n0 : 0;                    // where the tile's columns begin
-        uint4 ring[DEPTH][PIECES];
-        uint16_t s[DEPTH][PIECES][SPB];
-        uint8_t z[DEPTH][PIECES][SPB];
+        // A step is 128 contraction steps, two stages: a piece a thread.  Lanes of a warp hold the four pieces of eight rows, in an
+        // order in which eight neighbouring lanes write to different banks.  Forward, a piece's halves belong to the two stages;
+        // backward the first eight warps' rows are the one stage and the others' the other.
+        const int t = lane % 4, row = 8 * warp + (lane / 8 + lane / 4 % 2 * 4), own = BACK ? warp / 8 : 0;
+        uint4 ring[DEPTH];
+        uint32_t s[DEPTH][SPB];
+        uint32_t z[DEPTH][SPB];
+        // Behind the last row it is read again: forward what comes of it is not written, backward it meets zeros.
+        const int row0 = BACK ? row : n0 + row < P.rows ? n0 + row : P.rows - 1, end = P.rows - 1;
+        const uint8_t *q_at = P.q + (BACK ? n0 / 2 : (int64_t)row0 * P.ldq) + 16 * t;
+        const uint16_t *s_at = P.scale + (BACK ? 0 : (int64_t)row0 * P.ld_scale);
+        const uint8_t *z_at = P.zero + (BACK || !ZERO ? 0 : (int64_t)row0 * P.ld_zero);
+        auto group = [&](int block, int k) {                 // of the k-th part of a block; a block is as long as a group at least, or shorter
+            if (SPB == 1) return block >> (P.group_log2 - 7);
+            const int g = SPB * block + k;
+            return g < P.groups ? g : P.groups - 1;
+        };
+        int own_group[SPB];
+#pragma unroll
+        for (int k = 0; k < SPB; ++k) own_group[k] = group(n0 / 128, k);
         auto fetch = [&](int step, int slot) {
             if (step >= last) return;
+            const int n = 128 * step + row0 < end ? 128 * step + row0 : end;         // backward
+            ring[slot] = load_piece(q_at + (BACK ? (uint64_t)(uint32_t)n * P.ldq : (uint64_t)(64u * (uint32_t)step)));
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                const int64_t n = BACK ? 64 * (int64_t)step + row : (int64_t)n0 + row + 64 * i;
-                const int64_t c = BACK ? column : 128 * (int64_t)step;
-                ring[slot][i] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int k = 0; k < SPB; ++k) { s[slot][i][k] = 0; z[slot][i][k] = 0; }
-                if (n < P.rows) {
-                    ring[slot][i] = __ldg(reinterpret_cast<const uint4 *>(P.q + n * P.ldq + c / 2 + 16 * t));
-#pragma unroll
-                    for (int k = 0; k < SPB; ++k) {
-                        const int g = (int)((c + 128 / SPB * k) >> P.group_log2), at = g < P.groups ? g : P.groups - 1;
-                        s[slot][i][k] = __ldg(P.scale + n * P.ld_scale + at);
-                        if (ZERO) z[slot][i][k] = __ldg(P.zero + n * P.ld_zero + at);
-                    }
-                }
+            for (int k = 0; k < SPB; ++k) {
+                s[slot][k] = load_now(s_at + (BACK ? (uint64_t)(uint32_t)n * P.ld_scale + (uint32_t)own_group[k] : (uint64_t)(uint32_t)group(step, k)));
+                if (ZERO) z[slot][k] = load_now(z_at + (BACK ? (uint64_t)(uint32_t)n * P.ld_zero + (uint32_t)own_group[k] : (uint64_t)(uint32_t)group(step, k)));
             }
         };
-        // word j of piece i as eight columns in a tile
-        auto widen = [&](int slot, int i, int j, uint32_t to) {
-            const uint4 &x = ring[slot][i];
-            const uint32_t word = j == 0 ? x.x : j == 1 ? x.y : j == 2 ? x.z : x.w;
-            const uint32_t zero = int4_zero<E>(ZERO ? z[slot][i][j * SPB / 4] & 15u : 8u), one = s[slot][i][j * SPB / 4], scale = one | one << 16;
-            uint32_t v[4];
+        // where the piece's four words go in a stage
+        uint32_t place[4];
 #pragma unroll
-            for (int p = 0; p < 4; ++p) v[p] = int4_scaled<E>(int4_pair<E>(word, p, zero), scale);
-            store_shared_v4(to, make_uint4(v[0], v[1], v[2], v[3]));
-        };
+        for (int j = 0; j < 4; ++j)
+            place[j] = base + (BACK ? j / 2 * (kTile / 2) + row % 64 * 128 : row * 128) + 16 * ((4 * (j % 2) + t) ^ (row & 7));
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) fetch(first + d, d);
         Ring r;
@@ -160,23 +182,31 @@ int4_stream_kernel(const __grid_constant__ StreamArgs P)
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) {
                 if (!alive || step0 + d >= last) break;
+                int stage[2];
 #pragma unroll
-                for (int h = 0; h < STAGES_A_STEP; ++h) {
-                    alive = alive && __all_sync(0xffffffffu, bound.wait(empty(r.stage), r.phase ^ 1u, kDevTmaWaitTimeout));
-                    if (!alive) break;
-                    const uint32_t sw = base + r.stage * stage_bytes + row * 128;
-                    // row + 64 has the same place in the swizzle
-#pragma unroll
-                    for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-                        for (int j = 0; j < (BACK ? 4 : 2); ++j)
-                            widen(d, i, BACK ? j : 2 * h + j, sw + (BACK ? j / 2 * (kTile / 2) : i * 64 * 128) + 16 * ((4 * (j % 2) + t) ^ (row & 7)));
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(full(r.stage));
+                for (int h = 0; h < 2; ++h) {
+                    if (!BACK || h == own) alive = alive && bound.wait(empty(r.stage), r.phase ^ 1u, kDevTmaWaitTimeout);
+                    stage[h] = r.stage;
                     r.next(P.stages);
                 }
+                alive = __all_sync(0xffffffffu, alive);
+                if (!alive) break;
+                const uint32_t words[4] = {ring[d].x, ring[d].y, ring[d].z, ring[d].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t zero = int4_zero<E>(ZERO ? z[d][j * SPB / 4] & 15u : 8u), one = s[d][j * SPB / 4], scale = one | one << 16;
+                    uint32_t v[4];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) v[p] = int4_scaled<E>(int4_pair<E>(words[j], p, zero), scale);
+                    store_shared_v4(place[j] + (BACK ? (own ? stage[1] : stage[0]) : stage[j / 2]) * stage_bytes, make_uint4(v[0], v[1], v[2], v[3]));
+                }
                 fetch(step0 + d + DEPTH, d);
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    if (!BACK || !own) bar_arrive(full(stage[0]));
+                    if (!BACK || own) bar_arrive(full(stage[1]));
+                }
             }
         }
         // the partial sums go where the ring was: [token][128 rows]
@@ -203,7 +233,7 @@ int4_stream_kernel(const __grid_constant__ StreamArgs P)
     }
     __syncwarp();
     cluster_sync();
-    if (warp == 8) {
+    if (warp == kLoaders) {
         fence_after();
         tmem_free<1>(tmem, P.tmem_columns);
     }
@@ -278,7 +308,7 @@ bool allow(const void *func)
 }
 
 struct StreamPlan {
-    int tokens, stages, split, blocks;
+    int tokens, stages, split, steps;
     int64_t row_tiles, token_tiles;
     double us;
 };
@@ -288,17 +318,19 @@ StreamPlan plan_stream(const lordba_int4_proj &p, int64_t T, bool backward)
     StreamPlan s = {};
     const int64_t N = backward ? p.d_in : p.d_out;
     s.tokens = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
-    s.blocks = (int)(backward ? (p.d_out + 63) / 64 : (p.d_in + 127) / 128 * 2);
+    s.steps = (int)(((backward ? p.d_out : p.d_in) + 127) / 128);
     s.row_tiles = (N + kRows - 1) / kRows;
     s.token_tiles = (T + s.tokens - 1) / s.tokens;
     const int stage = kTile + s.tokens * 128, room = kSmem - kBarBytes - 1024;
     s.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
-    // Two CTAs an SM; a cluster of n takes what no other CTAs' clusters leave.
-    const int steps = backward ? s.blocks : s.blocks / 2;
-    for (int n = 1; n <= kMaxSplit && n <= steps; ++n) {
+    // Two CTAs share an SM.  A step takes one that is alone there 0.85 us, two at a time 1.25 us; around the steps 4 us, 0.4 us a CTA
+    // that the sums are exchanged with, and 3 to 6 us for 128 tokens' sums (4096 x 4096, 17 tokens, clusters of 1, 2, 4, 6 and 8: 29.5, 17.6,
+    // 11.8, 13.4 and 12.0 us; 4096 x 11008: 29.7, 24.8 and, of 3 and 4, 19.4 and 26.7 us).
+    for (int n = 1; n <= kMaxSplit && n <= s.steps; ++n) {
         const int64_t fit = 2 * sm_count() / n, work = s.row_tiles * s.token_tiles;
-        const double rounds = (double)((work + fit - 1) / fit), each = (double)((steps + n - 1) / n) * (backward ? 0.5 : 1.0);
-        const double us = 3.0 + rounds * (1.0 + each * 0.45 + s.tokens / 128.0 * (2.0 + 1.0 / n) + 0.19 * (n - 1));
+        const double rounds = (double)((work + fit - 1) / fit), steps = (double)((s.steps + n - 1) / n);
+        const bool alone = work * n <= sm_count();
+        const double us = 4.0 + rounds * (steps * (alone ? 0.85 : 1.25) + 0.4 * n + s.tokens / 128.0 * (alone ? 3.2 : 6.5));
         if (s.split == 0 || us < s.us) { s.split = n; s.us = us; }
     }
     return s;
@@ -309,7 +341,8 @@ StreamPlan plan_stream(const lordba_int4_proj &p, int64_t T, bool backward)
 double int4_stream_estimate(const lordba_int4_proj &p, int64_t T, bool backward)
 {
     const StreamPlan s = plan_stream(p, T, backward);
-    return s.row_tiles <= 65535 && s.token_tiles <= 65535 ? s.us : -1.0;
+    constexpr int64_t kFar = int64_t(1) << 31;           // pitches are multiplied in 32 bits
+    return s.row_tiles <= 65535 && s.token_tiles <= 65535 && p.ldq < kFar && p.ld_scale < kFar && (!p.zero || p.ld_zero < kFar) ? s.us : -1.0;
 }
 
 int launch_int4_stream(const lordba_int4_proj &p, int64_t T, int dtype, bool backward, cudaStream_t stream)
@@ -320,13 +353,13 @@ int launch_int4_stream(const lordba_int4_proj &p, int64_t T, int dtype, bool bac
     const int64_t K = backward ? p.d_out : p.d_in;
     if (!encode_map(&a.t, p.in, T, K, p.ld_in, 2, plan.tokens)) return LORDBA_ECUDA;
     a.q = p.q; a.scale = static_cast<const uint16_t *>(p.scale); a.zero = p.zero; a.out = p.out;
-    a.ldq = p.ldq; a.ld_scale = p.ld_scale; a.ld_zero = p.ld_zero; a.ld_out = p.ld_out;
+    a.ldq = (uint32_t)p.ldq; a.ld_scale = (uint32_t)p.ld_scale; a.ld_zero = (uint32_t)p.ld_zero; a.ld_out = p.ld_out;
     a.T = T;
     a.N = backward ? p.d_in : p.d_out;
     a.rows = (int)p.d_out;
     a.groups = (int)((p.d_in + p.group - 1) / p.group);
     while ((int64_t(1) << a.group_log2) < p.group) ++a.group_log2;
-    a.blocks = plan.blocks;
+    a.steps = plan.steps;
     a.tokens = plan.tokens;
     a.stages = plan.stages;
     a.split = plan.split;
