@@ -144,7 +144,7 @@ int launch_int4_dequantize(const lordba_int4_proj &p, int dtype, cudaStream_t st
 
 // --- int4_few.cu -------------------------------------------------------------
 constexpr int64_t kInt4Stream = 256;    // tokens up to which the weights are widened on their way
-constexpr int64_t kInt4Few = 16;        // tokens it takes at most
+constexpr int64_t kInt4Few = 32;        // tokens it takes at most
 int launch_int4_few(const lordba_int4_proj &p, int64_t T, int dtype, cudaStream_t stream);
 
 // --- int4_stream.cu ----------------------------------------------------------
