@@ -2,8 +2,8 @@
 //
 //   y[t,n] = sum over groups of  scale[n,g] * sum_{k in g} x[t,k] (u[n,k] - zero[n,g])
 //
-// Bound: HBM, half a byte a weight.  A CTA holds 16 or 32 weight rows, its eight warps every eighth block of 128 columns
-// each.  A lane's 16 bytes of a block are four runs of eight columns, 32 apart, so that the four lanes of a row and one word
+// Bound: HBM, half a byte a weight.  A CTA holds 16 or 32 weight rows, each of its four or eight warps every fourth or eighth block
+// of 128 columns.  A lane's 16 bytes of a block are four runs of eight columns, 32 apart, so that the four lanes of a row and one word
 // of each make 32 neighbouring columns: two matrix instructions (weights are the 16 rows, tokens the 8 columns), whose
 // order of columns is the carrier's and needs no exchange, and never more than one group's.  The integers go in as they are
 // (exact in 16 bits); a group's sum is scaled in float32.  The warps' sums meet in shared memory, in a fixed order.
@@ -108,14 +108,15 @@ int4_few_kernel(const __grid_constant__ FewArgs A)
         mine[i] = 2 * i + lane / 16 < A.T;
         x[i] = static_cast<const uint8_t *>(A.x) + (2 * i + lane / 16) * A.ldx * 2 + 256 * warp + 16 * (lane % 16);
     }
-    const int end = (int)(2 * A.d_in) - 16 * (lane % 16);           // bytes of a token's row from its piece of block 0 on
+    const int left = (int)(2 * (A.d_in - 128 * (int64_t)(A.blocks - 1))) - 16 * (lane % 16);           // bytes of a token's row from its piece of
+    const int tail = left < 0 ? 0 : left < 16 ? left : 16;                                             // the last block on, and of the piece
     const uint32_t weights_to = ring + 16 * lane, tokens_to = ring + 1024 * ROWS + kTokenBytes * (lane / 16) + 16 * (lane % 16);
     // block b, which lies `on` blocks of the warp's behind the pointers, into a slot
     auto fetch = [&](int b, int on, int slot) {
         if (b < A.blocks) {
 #pragma unroll
             for (int h = 0; h < 2 * ROWS; ++h) fetch_part(weights_to + slot * kSlot + 512 * h, q[h] + 64 * WARPS * on, 16);
-            const int left = end - 256 * b, bytes = left < 0 ? 0 : left < 16 ? left : 16;
+            const int bytes = b + 1 < A.blocks ? 16 : tail;
 #pragma unroll
             for (int i = 0; i < kShare; ++i)
                 if (mine[i]) fetch_part(tokens_to + slot * kSlot + 2 * kTokenBytes * i, x[i] + 256 * WARPS * on, bytes);

@@ -341,8 +341,8 @@ StreamPlan plan_stream(const lordba_int4_proj &p, int64_t T, bool backward)
 double int4_stream_estimate(const lordba_int4_proj &p, int64_t T, bool backward)
 {
     const StreamPlan s = plan_stream(p, T, backward);
-    constexpr int64_t kFar = int64_t(1) << 31;           // pitches are multiplied in 32 bits
-    return s.row_tiles <= 65535 && s.token_tiles <= 65535 && p.ldq < kFar && p.ld_scale < kFar && (!p.zero || p.ld_zero < kFar) ? s.us : -1.0;
+    constexpr int64_t kFar = int64_t(1) << 31;           // pitches, and rows and columns with a tile's on top, are 32 bits
+    return p.d_in < kFar / 2 && p.d_out < kFar / 2 && s.row_tiles <= 65535 && s.token_tiles <= 65535 && p.ldq < kFar && p.ld_scale < kFar && (!p.zero || p.ld_zero < kFar) ? s.us : -1.0;
 }
 
 int launch_int4_stream(const lordba_int4_proj &p, int64_t T, int dtype, bool backward, cudaStream_t stream)

@@ -292,3 +292,29 @@ def test_refusals():
     with pytest.raises(lordba.LordbaError):
         lordba.int4_linear(matrix(rng, 300, 256, "bf16")[0], big.q, big.scale, group=64, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert call(x=x[:0]).shape == (0, 64)
+
+
+@pytest.mark.parametrize("T", [1, 3])
+def test_rows_of_more_than_two_gigabytes(T):
+    """Columns whose byte offsets pass 31 bits; nearly all of x is zero, so that the sums are exact."""
+    d_in, d_out, group = (1 << 30) + 200, 2, 1 << 16
+    x = torch.zeros(T, d_in + 56, dtype=torch.float16, device="cuda")
+    q = torch.randint(0, 256, (d_out, lordba.int4_row_bytes(d_in)), dtype=torch.uint8, device="cuda")
+    scale = torch.full((d_out, -(-d_in // group)), 0.25, dtype=torch.float16, device="cuda")
+    at = [0, 5, 127, 128, (1 << 29) + 3, (1 << 30) - 1, 1 << 30, d_in - 1]
+    want = np.zeros((T, d_out))
+    host = {}
+    for c in at:
+        block, col = divmod(c, 128)
+        j, rest = divmod(col, 32)
+        t, e = divmod(rest, 8)
+        words = q[:, 64 * block + 4 * (4 * t + j):64 * block + 4 * (4 * t + j) + 4].cpu().numpy().copy().view(np.uint32)[:, 0]
+        host[c] = (words >> np.uint32(4 * (e // 2) + 16 * (e % 2))) & 15
+    for i, c in enumerate(at):
+        for token in {0, T - 1}:
+            x[token, c] = i + 1 + token
+            want[token] += (i + 1 + token) * 0.25 * (host[c].astype(np.float64) - 8)
+    x[:, d_in:] = math.nan
+    y = lordba.int4_linear(x[:, :d_in], q, scale, None, group)
+    assert np.array_equal(f64(y), want)
+    clean()
