@@ -1,13 +1,13 @@
 // Distillation from a teacher's top logits: the loss of a row, its log-sum, and the gradient to the student's logits.
 //
-// Bound: HBM.  A row's logits are read once, and for the gradient written once, because the row stays in registers in
-// between: eight 16-byte pieces a thread, all on the way before the first is looked at.  A row belongs to a CTA, or, where it is
-// long or rows are few, to a cluster of up to eight, which exchange maxima and sums through distributed shared memory.  A
-// thousand threads an SM, in CTAs as small as a row allows: while some wait for a row to arrive or for one another, others
-// calculate or write.  (What a row has beyond eight CTAs' registers is read again, from L2.)
+// Bound: HBM.  A row's logits are read once, and for the gradient written once.  Eight 16-byte pieces a thread are on the way before
+// the first is looked at.  A row that fits stays in a CTA's registers in between, or, where rows are few, in those of a cluster of
+// up to eight, which exchange maxima and sums through distributed shared memory; a longer one goes by against a running maximum,
+// and for the gradient comes a second time, from L2.  A thousand threads an SM, in CTAs as small as a row allows: while some
+// wait for a row to arrive or for one another, others calculate or write.
 //
 // Persistent CTAs that had the copy engine fetch rows ahead, with a row's exponentials kept in registers between the passes,
-// were slower (4096 x 131072 in bf16 1190 us, this 460; 2048 x 32000 128 and 68): a row is a chain of latencies for the warps that
+// were slower (4096 x 131072 in bf16 1190 us, this 422; 2048 x 32000 128 and 68): a row is a chain of latencies for the warps that
 // share it, and what hides it is many rows at a time.
 //
 // Pieces lie on 16-byte boundaries whatever the row's alignment is: the first and last are masked, and results that lie
@@ -29,7 +29,7 @@ namespace {
 using namespace sm100;
 
 constexpr int kHeld = 8;                  // pieces a thread keeps
-constexpr int kMaxSplit = 8, kMaxThreads = 512;
+constexpr int kMaxSplit = 8, kMaxThreads = 512, kPassThreads = 512;
 // Rows up to which each does its teacher's part itself: a chain of accesses that wait for one another, 2 us where the GPU is
 // idle, but more than twice that among other rows' traffic, where a kernel of its own before (one more launch, 1.5 us) pays.
 constexpr int64_t kDistillAlone = 128;
@@ -282,13 +282,15 @@ __device__ __forceinline__ Stat over_lanes(Stat s, float scale)
 }
 
 
-// ALONE: the row's first warp does the teacher's part itself; otherwise distill_teacher_kernel has done it for all rows.
-template <typename E, int MODE, int THREADS, bool ALONE>
+// ALONE: the row's first warp does the teacher's part itself; otherwise distill_teacher_kernel has done it for all rows.  HELD:
+// the registers have room for the CTA's part of the row; otherwise it goes by, half of the pieces at a time, whose successors are asked
+// for at once, against a running maximum, and for the gradient once more (it comes from L2 then).
+template <typename E, int MODE, int THREADS, bool ALONE, bool HELD>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 distill_kernel(const __grid_constant__ DistillArgs A)
 {
     extern __shared__ __align__(16) uint8_t own[];
-    constexpr int N = 16 / (int)sizeof(E), kWarps = THREADS / 32;
+    constexpr int N = 16 / (int)sizeof(E), kWarps = THREADS / 32, kHalf = kHeld / 2;
     constexpr uint32_t kLow = sizeof(E) == 4 ? 0xff800000u : std::is_same_v<E, __half> ? 0xfc00fc00u : 0xff80ff80u;
     __shared__ Stat part[kWarps], peers[kMaxSplit];
     __shared__ Head head;
@@ -312,12 +314,12 @@ distill_kernel(const __grid_constant__ DistillArgs A)
     // there (in L2); what that kernel makes, and what may be written over, waits for its end.
     if (ALONE) grid_wait();
     if (MODE != kBack && A.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // this CTA runs
+    auto piece = [&](int i) { return tid + THREADS * i < chunks ? __ldcg(in + THREADS * i) : make_uint4(kLow, kLow, kLow, kLow); };
+    // for the last time: other rows may take its place in L2
+    auto last_piece = [&](int i) { return MODE != kStep ? piece(i) : tid + THREADS * i < chunks ? __ldcs(in + THREADS * i) : make_uint4(kLow, kLow, kLow, kLow); };
     uint4 raw[kHeld];
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-        raw[i] = make_uint4(kLow, kLow, kLow, kLow);
-        if (tid + THREADS * i < chunks) raw[i] = __ldcg(in + THREADS * i);
-    }
+    for (int i = 0; i < kHeld; ++i) raw[i] = piece(i);
     if (!ALONE) grid_wait();
     grid_release();
     const float weight = A.weight ? A.weight[t] : 1.0f;
@@ -336,22 +338,15 @@ distill_kernel(const __grid_constant__ DistillArgs A)
     Stat all = {0.0f, 1.0f};
     if (MODE != kBack) {
         uint32_t most[2] = {kLow, kLow};
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            if (i >= pieces) break;
-            raw[i] = mask(raw[i], tid + THREADS * i);
-            top_of_chunk<E>(raw[i], most);
-        }
-        for (int c = tid + THREADS * kHeld; c < chunks; c += THREADS) top_of_chunk<E>(mask(in[c - tid], c), most);
         Stat s;
-        if constexpr (sizeof(E) == 4) s.max = __uint_as_float(most[0]);
-        else {
-            const float2 x = unpack2<E>(most[0]), y = unpack2<E>(most[1]);
-            s.max = fmaxf(fmaxf(x.x, x.y), fmaxf(y.x, y.y));
-        }
-        const float minus = s.max == -INFINITY ? 0.0f : -s.max * A.scale;
-        const Two scales = two(A.scale, A.scale), minuses = two(minus, minus);
-        Two sums[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
+        auto largest = [&] {
+            if constexpr (sizeof(E) == 4) return __uint_as_float(most[0]);
+            else {
+                const float2 x = unpack2<E>(most[0]), y = unpack2<E>(most[1]);
+                return fmaxf(fmaxf(x.x, x.y), fmaxf(y.x, y.y));
+            }
+        };
+        Two scales = two(A.scale, A.scale), minuses, sums[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
         auto add = [&](uint4 w) {
             Two v[N / 2];
             unpack_chunk<E>(w, v);
@@ -361,12 +356,50 @@ distill_kernel(const __grid_constant__ DistillArgs A)
                 sums[j % 2] = add_two(sums[j % 2], two(exp2_of(x.x), exp2_of(x.y)));
             }
         };
+        if constexpr (!HELD) {
+            s.max = -INFINITY;
+            for (int base = 0; base < pieces; base += kHeld) {
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            if (i >= pieces) break;
-            add(raw[i]);
+                for (int h = 0; h < kHeld; h += kHalf) {
+                    if (base + h >= pieces) break;
+#pragma unroll
+                    for (int i = h; i < h + kHalf; ++i) {
+                        raw[i] = mask(raw[i], tid + THREADS * (base + i));
+                        top_of_chunk<E>(raw[i], most);
+                    }
+                    const float was = s.max;
+                    s.max = largest();
+                    const float minus = s.max == -INFINITY ? 0.0f : -s.max * A.scale, kept = exp2_of(fmaf(was, A.scale, minus));
+                    minuses = two(minus, minus);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) sums[j] = mul_two(sums[j], two(kept, kept));
+#pragma unroll
+                    for (int i = h; i < h + kHalf; ++i) {
+                        add(raw[i]);
+                        raw[i] = piece(base + kHeld + i);
+                    }
+                }
+            }
+            if (MODE == kStep) {
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i) raw[i] = last_piece(i);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) {
+                if (i >= pieces) break;
+                raw[i] = mask(raw[i], tid + THREADS * i);
+                top_of_chunk<E>(raw[i], most);
+            }
+            s.max = largest();
+            const float minus = s.max == -INFINITY ? 0.0f : -s.max * A.scale;
+            minuses = two(minus, minus);
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) {
+                if (i >= pieces) break;
+                add(raw[i]);
+            }
         }
-        for (int c = tid + THREADS * kHeld; c < chunks; c += THREADS) add(mask(in[c - tid], c));
         const float2 sum = halves(add_two(sums[0], sums[1]));
         s.sum = sum.x + sum.y;
         s = over_lanes<32>(s, A.scale);
@@ -413,52 +446,74 @@ distill_kernel(const __grid_constant__ DistillArgs A)
         if (!live) w = make_uint4(0, 0, 0, 0);                        // whatever stood there
         uint8_t *at = to + 16 * (c - tid);
         if (plain) {
-            if (c < chunks) *reinterpret_cast<uint4 *>(at) = w;
+            if (c < chunks) __stcs(reinterpret_cast<uint4 *>(at), w);
         } else {
             store_chunks<E>(at, w, by, c == 0 ? off : 0, last - 16 * c < 16 ? last - 16 * c : 16, lane);
         }
     };
+    for (int base = 0; base < (HELD ? 1 : pieces); base += kHeld) {
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-        if (i >= pieces) break;
-        put(raw[i], tid + THREADS * i);
+        for (int i = 0; i < kHeld; ++i) {
+            if (base + i >= pieces) break;
+            put(raw[i], tid + THREADS * (base + i));
+            if (!HELD) raw[i] = last_piece(base + kHeld + i);
+        }
     }
-    for (int c0 = tid - lane + THREADS * kHeld; c0 < chunks; c0 += THREADS)
-        put(c0 + lane < chunks ? in[c0 + lane - tid] : make_uint4(kLow, kLow, kLow, kLow), c0 + lane);
     if (!live) return;
     __syncthreads();                       // the teacher's entries' gradients go over what was put there
     if (warp * 32 < A.top) patch_row<E>(A, t, first, count, top, head.twice, factor, shift, tid, THREADS);
 }
 
 template <typename E, int MODE, bool ALONE>
-const void *kernel_of(int threads)
+const void *kernel_of(int threads, bool held)
 {
-    return threads == 64    ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 64, ALONE>)
-           : threads == 128 ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 128, ALONE>)
-           : threads == 256 ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 256, ALONE>)
-                            : reinterpret_cast<const void *>(&distill_kernel<E, MODE, 512, ALONE>);
+    constexpr bool HELD = MODE != kLoss;
+    if (HELD && !held) return reinterpret_cast<const void *>(&distill_kernel<E, MODE, kPassThreads, ALONE, false>);
+    return threads == 64    ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 64, ALONE, HELD>)
+           : threads == 128 ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 128, ALONE, HELD>)
+           : threads == 256 ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 256, ALONE, HELD>)
+                            : reinterpret_cast<const void *>(&distill_kernel<E, MODE, 512, ALONE, HELD>);
 }
 
 template <typename E, int MODE>
-int launch_held(DistillArgs &A, int64_t T, cudaStream_t stream)
+int launch_row(DistillArgs &A, int64_t T, cudaStream_t stream)
 {
-    // As many CTAs of at most kMaxThreads a row as hold it, more while there are SMs without one and a CTA keeps a few kilobytes; then
-    // the smallest CTA that holds its part.
-    const int64_t pieces = (A.vocab * (int64_t)sizeof(E) + 30) / 16;
+    // Of a row, or a CTA's part (whole 16 bytes of it): one more where it begins inside a piece.
+    const bool inside = reinterpret_cast<uintptr_t>(A.logits) % 16 || (T > 1 && A.ld_logits * sizeof(E) % 16);
+    auto part_of = [&](int split) { return (A.vocab + 8 * split - 1) / (8 * split) * 8; };
+    auto pieces_of = [&](int split) {
+        const int64_t part = part_of(split);
+        return ((part < A.vocab ? part : A.vocab) * (int64_t)sizeof(E) + 15) / 16 + inside;
+    };
+    // With a row for every SM, one CTA each (two an SM, 512 threads) goes over rows that it cannot hold, as long as all of these stay in L2
+    // for the second pass; longer ones are held by a cluster that they fill, and so are fewer rows.  Steps of 4096 x 131072 in bf16 422 us,
+    // held by clusters 440; 1500 x 160000 217, held (not filled) 310; 2048 x 50257 105 and 118; 1024 x 131072 in f32 (512 KB a row) 257, held
+    // 235.  Backward, which takes one pass: 343, held 388; 171 and 231; 79 and 100.
+    constexpr int64_t kRoom = kMaxThreads * kHeld;
+    const bool many = T >= sm_count(), stays = 2 * sm_count() * A.vocab * (int64_t)sizeof(E) <= (int64_t)112 << 20;
     int split = 1;
-    while (split < kMaxSplit && (pieces > (int64_t)split * kMaxThreads * kHeld || (T * split * 2 <= sm_count() && pieces >= 256 * split))) split *= 2;
+    while (split < kMaxSplit && pieces_of(split) > kRoom) split *= 2;
+    const bool filled = MODE == kStep && !stays && pieces_of(split) * 8 >= kRoom * 7;
+    const bool held = MODE != kLoss && pieces_of(split) <= kRoom && (split == 1 || !many || filled);
+    if (!held && (MODE == kLoss || many)) split = 1;
+    // more CTAs a row while there are SMs without one and a CTA keeps a few kilobytes
+    while (split < kMaxSplit && T * split * 2 <= sm_count() && pieces_of(1) >= 256 * split) split *= 2;
     if (T * split > 0x7fffffff) return LORDBA_EUNSUPPORTED;
     A.split = split;
     A.split_log2 = 0;
     while ((1 << A.split_log2) < split) ++A.split_log2;
-    A.part = (int)((A.vocab + 8 * split - 1) / (8 * split) * 8);
-    const int64_t mine = (A.part * (int64_t)sizeof(E) + 14) / 16;
+    A.part = (int)part_of(split);
+    const int64_t mine = pieces_of(split);
+    // The smallest CTA that holds its part; for the loss of many rows, which holds nothing, small ones of several rounds (2048 x 32000 38 us, of
+    // one round 46; 4096 x 131072 177, with 512 threads 190).
+    const int rounds = MODE == kLoss && many ? 4 : 1, most = MODE == kLoss && many ? kMaxThreads / 2 : kMaxThreads;
     int threads = 64;
-    while (threads < kMaxThreads && mine > (int64_t)threads * kHeld) threads *= 2;
+    while (threads < most && mine > (int64_t)threads * kHeld * rounds) threads *= 2;
+    if (MODE != kLoss && !held) threads = kPassThreads;
     const bool alone = T <= kDistillAlone;
     LaunchRec rec;
     std::memset(&rec, 0, sizeof(rec));
-    rec.func = alone ? kernel_of<E, MODE, true>(threads) : kernel_of<E, MODE, false>(threads);
+    rec.func = alone ? kernel_of<E, MODE, true>(threads, held) : kernel_of<E, MODE, false>(threads, held);
     rec.grid[0] = (unsigned)(T * split);
     rec.grid[1] = rec.grid[2] = 1;
     rec.block = (uint32_t)threads;
@@ -478,7 +533,7 @@ int launch_mode(DistillArgs &A, int64_t T, cudaStream_t stream)
         const int rc = launch_kernel(distill_teacher_kernel<E>, dim3((unsigned)((T + 3) / 4), 1, 1), 128, smem, stream, A, T);
         if (rc != LORDBA_OK) return rc;
     }
-    return launch_held<E, MODE>(A, T, stream);
+    return launch_row<E, MODE>(A, T, stream);
 }
 
 template <typename E>
