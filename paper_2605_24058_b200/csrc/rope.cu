@@ -74,21 +74,51 @@ struct Place {
     }
 };
 
+// Eight entries side by side.  Input that lies off the 16-byte boundaries is fetched as the aligned pieces that hold it, and shifted when it is used: the
+// pieces of the next heads are on their way meanwhile like any other (4096 tokens 22 us, gradients 40 us, half of a head rotated 35 and
+// 78 us; entry by entry 62 and 125 us).
+template <typename E, bool ALIGNED> struct Run;
+template <typename E> struct Run<E, true> {
+    Group8<E> g;
+    __device__ __forceinline__ void load(const E *p) { g = load_group(p); }
+    __device__ __forceinline__ Group8<E> get() const { return g; }
+};
+template <typename E> struct Run<E, false> {
+    static constexpr int kWhole = sizeof(Group8<E>) / 16;
+    uint4 piece[kWhole + 1];
+    uint32_t by;
+    __device__ __forceinline__ void load(const E *p)
+    {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        const uint4 *q = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
+        by = (uint32_t)at & 15u;
+#pragma unroll
+        for (int i = 0; i < kWhole; ++i) piece[i] = q[i];
+        piece[kWhole] = q[by ? kWhole : 0];         // all of them hold bytes of the run
+    }
+    __device__ __forceinline__ Group8<E> get() const
+    {
+        Group8<E> g;
+        g.w = join_pieces(piece[0], piece[1], by);
+        if constexpr (sizeof(E) == 4) g.w2 = join_pieces(piece[1], piece[2], by);
+        return g;
+    }
+};
 // What a lane holds of a head vector, as it lies in memory.
-template <typename E, bool VEC> struct Raw;
-template <typename E> struct Raw<E, true> { Group8<E> r[2]; };
-template <typename E> struct Raw<E, false> { E a[8], b[8]; };
+template <typename E, bool VEC, bool ALIGNED> struct Raw;
+template <typename E, bool ALIGNED> struct Raw<E, true, ALIGNED> { Run<E, ALIGNED> r[2]; };
+template <typename E, bool ALIGNED> struct Raw<E, false, ALIGNED> { E a[8], b[8]; };
 
-template <typename E, bool INTERLEAVED, bool VEC>
-__device__ __forceinline__ Raw<E, VEC> load_heads(const E *p, const Place<INTERLEAVED, VEC> &at, bool in)
+template <typename E, bool ALIGNED, bool INTERLEAVED, bool VEC>
+__device__ __forceinline__ Raw<E, VEC, ALIGNED> load_heads(const E *p, const Place<INTERLEAVED, VEC> &at, bool in)
 {
-    Raw<E, VEC> v;
+    Raw<E, VEC, ALIGNED> v;
     std::memset(&v, 0, sizeof(v));
     if (!in) return v;
     if constexpr (VEC) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
-            if (at.run(r) < at.d) v.r[r] = load_group(p + at.run(r));
+            if (at.run(r) < at.d) v.r[r].load(p + at.run(r));
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -99,13 +129,13 @@ __device__ __forceinline__ Raw<E, VEC> load_heads(const E *p, const Place<INTERL
     return v;
 }
 
-template <typename E, bool INTERLEAVED, bool VEC>
-__device__ __forceinline__ void unpack(const Raw<E, VEC> &v, float a[8], float b[8])
+template <typename E, bool INTERLEAVED, bool VEC, bool ALIGNED>
+__device__ __forceinline__ void unpack(const Raw<E, VEC, ALIGNED> &v, float a[8], float b[8])
 {
     if constexpr (VEC) {
         float x[16];
-        unpack_group<E>(v.r[0], x);
-        unpack_group<E>(v.r[1], x + 8);
+        unpack_group<E>(v.r[0].get(), x);
+        unpack_group<E>(v.r[1].get(), x + 8);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             a[j] = x[INTERLEAVED ? 2 * j : j];
@@ -163,7 +193,7 @@ __device__ __forceinline__ float over_head(float v, int width)
     return v;
 }
 
-template <typename E, bool BACK, bool INTERLEAVED, bool VEC>
+template <typename E, bool BACK, bool INTERLEAVED, bool VEC, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, BACK ? 2 : 3)
 norm_rope_kernel(const __grid_constant__ RopeArgs A)
 {
@@ -194,8 +224,8 @@ norm_rope_kernel(const __grid_constant__ RopeArgs A)
         // the first heads are on their way while the angles are worked out
         int h = s0 * per + mine;
         bool in = h < S.heads && at.has(0);
-        Raw<E, VEC> rx = load_heads<E>(x + h * S.x_head, at, in && (!BACK || A.norm)), rg;
-        if (BACK) rg = load_heads<E>(g + h * S.g_head, at, in);
+        Raw<E, VEC, ALIGNED> rx = load_heads<E, ALIGNED>(x + h * S.x_head, at, in && (!BACK || A.norm)), rg;
+        if (BACK) rg = load_heads<E, ALIGNED>(g + h * S.g_head, at, in);
         if (A.half) {
             const double turns_of = (double)A.positions[t] * 0.15915494309189533577;       // 1 / (2 pi)
             __syncwarp();                                   // the table's last readers
@@ -223,8 +253,8 @@ norm_rope_kernel(const __grid_constant__ RopeArgs A)
             if (step + 1 < s1) {                            // the next heads' loads
                 h += per;
                 in = h < S.heads && at.has(0);
-                rx = load_heads<E>(x + h * S.x_head, at, in && (!BACK || A.norm));
-                if (BACK) rg = load_heads<E>(g + h * S.g_head, at, in);
+                rx = load_heads<E, ALIGNED>(x + h * S.x_head, at, in && (!BACK || A.norm));
+                if (BACK) rg = load_heads<E, ALIGNED>(g + h * S.g_head, at, in);
             }
             float r = 1.0f;
             if (A.norm) {
@@ -294,40 +324,9 @@ norm_rope_kernel(const __grid_constant__ RopeArgs A)
 // ---- head vectors that are rotated whole and fill their lanes --------------------------------------------------------
 // d = 16 WIDTH entries, all rotated, results on 16-byte boundaries: what models have.  Nothing is looked at per entry, and two entries
 // are worked on by one instruction (4096 tokens 19.7 us, by the kernel for any heads 26 us).
-//
-// Input that lies off the 16-byte boundaries is fetched as the aligned pieces that hold it, and shifted when it is used: the
-// pieces of the next heads are on their way meanwhile like any other (4096 tokens 22 us, gradients 40 us; entry by entry 62 and 125 us).
-template <typename E, bool ALIGNED> struct Run;
-template <typename E> struct Run<E, true> {
-    Group8<E> g;
-    __device__ __forceinline__ void load(const E *p) { g = load_group(p); }
-    __device__ __forceinline__ Group8<E> get() const { return g; }
-};
-template <typename E> struct Run<E, false> {
-    static constexpr int kWhole = sizeof(Group8<E>) / 16;
-    uint4 piece[kWhole + 1];
-    uint32_t by;
-    __device__ __forceinline__ void load(const E *p)
-    {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-        const uint4 *q = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
-        by = (uint32_t)at & 15u;
-#pragma unroll
-        for (int i = 0; i < kWhole; ++i) piece[i] = q[i];
-        piece[kWhole] = q[by ? kWhole : 0];         // all of them hold bytes of the run
-    }
-    __device__ __forceinline__ Group8<E> get() const
-    {
-        Group8<E> g;
-        g.w = join_pieces(piece[0], piece[1], by);
-        if constexpr (sizeof(E) == 4) g.w2 = join_pieces(piece[1], piece[2], by);
-        return g;
-    }
-};
-template <typename E, bool ALIGNED> struct Pieces { Run<E, ALIGNED> r[2]; };
 
 template <typename E, bool INTERLEAVED, bool ALIGNED>
-__device__ __forceinline__ void unpack_pairs(const Pieces<E, ALIGNED> &raw, Two a[4], Two b[4])
+__device__ __forceinline__ void unpack_pairs(const Raw<E, true, ALIGNED> &raw, Two a[4], Two b[4])
 {
     float v[16];
     unpack_group<E>(raw.r[0].get(), v);
@@ -389,7 +388,7 @@ norm_rope_full_kernel(const __grid_constant__ RopeArgs A)
         da[j] = db[j] = two(0.0f, 0.0f);
     }
     auto load = [&](const E *p, bool in) {
-        Pieces<E, ALIGNED> v;
+        Raw<E, true, ALIGNED> v;
         std::memset(&v, 0, sizeof(v));
         if (in) {
             v.r[0].load(p);
@@ -407,7 +406,7 @@ norm_rope_full_kernel(const __grid_constant__ RopeArgs A)
         const E *g = static_cast<const E *>(S.g) + (BACK ? t * S.g_token + h * S.g_head + at : 0);
         E *out = static_cast<E *>(S.out) + t * S.out_token + h * S.out_head + at;
         // the first heads are on their way while the angles are worked out
-        Pieces<E, ALIGNED> rx = load(x, h < S.heads && (!BACK || NORM)), rg;
+        Raw<E, true, ALIGNED> rx = load(x, h < S.heads && (!BACK || NORM)), rg;
         if (BACK) rg = load(g, h < S.heads);
         const double turns_of = (double)A.positions[t] * 0.15915494309189533577;       // 1 / (2 pi)
         __syncwarp();                                        // the table's last readers
@@ -595,11 +594,12 @@ template <typename E, bool BACK>
 int launch_typed(const RopeArgs &A, bool interleaved, bool vec_shape, bool vec_in, bool vec_out, cudaStream_t stream)
 {
     // heads of 64, 128 and 256 entries, rotated whole
-    const bool full = vec_out && A.d == 16 * A.width && 2 * A.half == A.d && A.width >= 4 && A.width <= 16, vec = vec_shape && vec_in && vec_out;
+    const bool full = vec_out && A.d == 16 * A.width && 2 * A.half == A.d && A.width >= 4 && A.width <= 16, vec = vec_shape && vec_out;
     RopeKernel kernel;
     if (full) kernel = vec_in ? full_kernel<E, BACK, true>(A, interleaved) : full_kernel<E, BACK, false>(A, interleaved);
-    else if (interleaved) kernel = vec ? norm_rope_kernel<E, BACK, true, true> : norm_rope_kernel<E, BACK, true, false>;
-    else kernel = vec ? norm_rope_kernel<E, BACK, false, true> : norm_rope_kernel<E, BACK, false, false>;
+    else if (vec && vec_in) kernel = interleaved ? norm_rope_kernel<E, BACK, true, true, true> : norm_rope_kernel<E, BACK, false, true, true>;
+    else if (vec) kernel = interleaved ? norm_rope_kernel<E, BACK, true, true, false> : norm_rope_kernel<E, BACK, false, true, false>;
+    else kernel = interleaved ? norm_rope_kernel<E, BACK, true, false, true> : norm_rope_kernel<E, BACK, false, false, true>;
     return launch_kernel(kernel, dim3((unsigned)(A.side[0].blocks + A.side[1].blocks), 1, 1), kThreads, 0, stream, A);
 }
 

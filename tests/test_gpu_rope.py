@@ -71,7 +71,8 @@ SHAPES = [  # T, heads_q, heads_k, d, rotary, interleaved, pad, lead
     (1, 1, 1, 2, 2, False, 0, 0), (1, 32, 32, 128, 128, False, 0, 0), (1, 5, 0, 64, 64, True, 0, 0), (3, 4, 1, 1, 0, False, 0, 0), (2, 3, 2, 7, 4, False, 0, 0),
     (7, 8, 2, 128, 128, False, 0, 0), (9, 6, 3, 64, 32, False, 8, 0), (17, 2, 2, 80, 80, True, 0, 0), (33, 5, 1, 80, 40, False, 0, 0), (65, 4, 4, 96, 96, False, 5, 1),
     (40, 3, 1, 512, 512, False, 0, 0), (12, 2, 1, 511, 510, True, 0, 0), (21, 4, 2, 256, 64, True, 64, 0), (200, 16, 4, 128, 128, False, 1024, 8), (500, 32, 8, 64, 64, False, 0, 0),
-    (300, 1, 1, 24, 16, False, 0, 0), (130, 2, 1, 33, 32, False, 3, 0), (1000, 7, 3, 128, 64, True, 0, 0), (50, 40, 40, 16, 16, False, 0, 0), (19, 2, 2, 72, 48, False, 0, 0)]
+    (300, 1, 1, 24, 16, False, 0, 0), (130, 2, 1, 33, 32, False, 3, 0), (1000, 7, 3, 128, 64, True, 0, 0), (50, 40, 40, 16, 16, False, 0, 0), (19, 2, 2, 72, 48, False, 0, 0),
+    (77, 4, 2, 128, 128, False, 5, 1), (30, 2, 1, 64, 64, True, 3, 0), (26, 3, 2, 256, 256, False, 1, 7), (44, 5, 2, 128, 64, False, 5, 3), (31, 2, 2, 80, 80, True, 7, 0)]
 
 
 @pytest.mark.parametrize("T,hq,hk,d,R,interleaved,pad,lead", SHAPES)
