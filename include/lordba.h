@@ -504,10 +504,10 @@ int lordba_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr
  * a zero's byte the low four bits count.
  *
  * dtype: LORDBA_BF16 or LORDBA_F16, the type of the activations, the results and the scales (LORDBA_F32 is
- * LORDBA_EUNSUPPORTED).  Every sum is float32, results are rounded once.  A call of few tokens multiplies
- * the integers themselves (they are exact in 16 bits) and scales the sum of each group; one of many tokens
- * multiplies weights that were rounded to the type of x, because that is what the tensor cores take (the
- * error of y is then up to 1.4 times that of rounding y alone).  A scale that is not finite spoils its
+ * LORDBA_EUNSUPPORTED).  Every sum is float32, results are rounded once.  A forward call of few tokens
+ * (now up to 32) multiplies the integers themselves (they are exact in 16 bits) and scales the sum of each
+ * group; others multiply weights that were rounded to the type of x, because that is what the tensor cores
+ * take (the error of y is then up to 1.4 times that of rounding y alone).  A scale that is not finite spoils its
  * row of y (of dx: the columns of its group) and nothing else.  T = 0 is a no-op.
  */
 typedef struct lordba_int4_proj {

@@ -29,7 +29,7 @@ namespace {
 using namespace sm100;
 
 constexpr int kHeld = 8;                  // pieces a thread keeps
-constexpr int kMaxSplit = 8, kMaxThreads = 512, kPassThreads = 512;
+constexpr int kMaxSplit = 8, kMaxThreads = 512;
 // Rows up to which each does its teacher's part itself: a chain of accesses that wait for one another, 2 us where the GPU is
 // idle, but more than twice that among other rows' traffic, where a kernel of its own before (one more launch, 1.5 us) pays.
 constexpr int64_t kDistillAlone = 128;
@@ -464,15 +464,21 @@ distill_kernel(const __grid_constant__ DistillArgs A)
     if (warp * 32 < A.top) patch_row<E>(A, t, first, count, top, head.twice, factor, shift, tid, THREADS);
 }
 
-template <typename E, int MODE, bool ALONE>
-const void *kernel_of(int threads, bool held)
+template <typename E, int MODE, bool ALONE, bool HELD>
+const void *kernel_of(int threads)
 {
-    constexpr bool HELD = MODE != kLoss;
-    if (HELD && !held) return reinterpret_cast<const void *>(&distill_kernel<E, MODE, kPassThreads, ALONE, false>);
     return threads == 64    ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 64, ALONE, HELD>)
            : threads == 128 ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 128, ALONE, HELD>)
            : threads == 256 ? reinterpret_cast<const void *>(&distill_kernel<E, MODE, 256, ALONE, HELD>)
                             : reinterpret_cast<const void *>(&distill_kernel<E, MODE, 512, ALONE, HELD>);
+}
+template <typename E, int MODE, bool ALONE>
+const void *kernel_of(int threads, bool held)
+{
+    if constexpr (MODE == kLoss) return kernel_of<E, MODE, ALONE, false>(threads);
+    else if (held) return kernel_of<E, MODE, ALONE, true>(threads);
+    else if constexpr (MODE == kBack && !ALONE) return kernel_of<E, MODE, ALONE, false>(threads);
+    else return reinterpret_cast<const void *>(&distill_kernel<E, MODE, kMaxThreads, ALONE, false>);
 }
 
 template <typename E, int MODE>
@@ -485,17 +491,21 @@ int launch_row(DistillArgs &A, int64_t T, cudaStream_t stream)
         const int64_t part = part_of(split);
         return ((part < A.vocab ? part : A.vocab) * (int64_t)sizeof(E) + 15) / 16 + inside;
     };
-    // With a row for every SM, one CTA each (two an SM, 512 threads) goes over rows that it cannot hold, as long as all of these stay in L2
-    // for the second pass; longer ones are held by a cluster that they fill, and so are fewer rows.  Steps of 4096 x 131072 in bf16 422 us,
-    // held by clusters 440; 1500 x 160000 217, held (not filled) 310; 2048 x 50257 105 and 118; 1024 x 131072 in f32 (512 KB a row) 257, held
-    // 235.  Backward, which takes one pass: 343, held 388; 171 and 231; 79 and 100.
+    // With a row for every SM, one CTA each (two an SM, 512 threads) goes over rows that it cannot hold, as long as all of these stay
+    // in L2 for the second pass; longer ones are held by a cluster that they fill, and so are fewer rows.  Steps of 4096 x 131072 in
+    // bf16 422 us, held by clusters 440; 1500 x 160000 217, held (not filled) 310; 2048 x 50257 105 and 118; 1024 x 131072 in f32
+    // (512 KB a row) 257, held 235.  Backward, which takes one pass: 343, held 388; 171 and 231; 79 and 100; rows
+    // that a CTA could hold go by small CTAs as well where there are many of 16 KB and more (2048 x 32000 58 and 61; 8192 x 4000 35 and
+    // 32, 256 x 32000 16.5 and 13.7, which are held).
     constexpr int64_t kRoom = kMaxThreads * kHeld;
-    const bool many = T >= sm_count(), stays = 2 * sm_count() * A.vocab * (int64_t)sizeof(E) <= (int64_t)112 << 20;
+    const bool many = T >= sm_count() && T > kDistillAlone, stays = 2 * sm_count() * A.vocab * (int64_t)sizeof(E) <= (int64_t)112 << 20;
     int split = 1;
     while (split < kMaxSplit && pieces_of(split) > kRoom) split *= 2;
     const bool filled = MODE == kStep && !stays && pieces_of(split) * 8 >= kRoom * 7;
-    const bool held = MODE != kLoss && pieces_of(split) <= kRoom && (split == 1 || !many || filled);
+    const bool small = MODE == kBack && T >= 4 * sm_count() && pieces_of(1) > 1024;
+    const bool held = MODE != kLoss && pieces_of(split) <= kRoom && (!many || filled || (split == 1 && !small));
     if (!held && (MODE == kLoss || many)) split = 1;
+    while (split < kMaxSplit && pieces_of(split) > 1 << 26) split *= 2;          // a part's bytes are counted in 32 bits
     // more CTAs a row while there are SMs without one and a CTA keeps a few kilobytes
     while (split < kMaxSplit && T * split * 2 <= sm_count() && pieces_of(1) >= 256 * split) split *= 2;
     if (T * split > 0x7fffffff) return LORDBA_EUNSUPPORTED;
@@ -504,12 +514,11 @@ int launch_row(DistillArgs &A, int64_t T, cudaStream_t stream)
     while ((1 << A.split_log2) < split) ++A.split_log2;
     A.part = (int)part_of(split);
     const int64_t mine = pieces_of(split);
-    // The smallest CTA that holds its part; for the loss of many rows, which holds nothing, small ones of several rounds (2048 x 32000 38 us, of
-    // one round 46; 4096 x 131072 177, with 512 threads 190).
-    const int rounds = MODE == kLoss && many ? 4 : 1, most = MODE == kLoss && many ? kMaxThreads / 2 : kMaxThreads;
+    // The smallest CTA that holds its part.  Of many rows that nothing of is held, small ones of several rounds: the loss of 2048 x 32000
+    // 38 us, of one round 46; of 4096 x 131072 177, with 512 threads 190.
+    const int rounds = !many || held ? 1 : MODE == kLoss ? 4 : 2, most = MODE == kLoss && many ? kMaxThreads / 2 : kMaxThreads;
     int threads = 64;
     while (threads < most && mine > (int64_t)threads * kHeld * rounds) threads *= 2;
-    if (MODE != kLoss && !held) threads = kPassThreads;
     const bool alone = T <= kDistillAlone;
     LaunchRec rec;
     std::memset(&rec, 0, sizeof(rec));

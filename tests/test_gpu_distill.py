@@ -78,7 +78,7 @@ class Case:
 SIZES = [  # T, V, top, pad, lead
     (1, 1, 1, 0, 0), (1, 8, 3, 0, 0), (3, 33, 5, 0, 0), (2, 1000, 20, 5, 1), (1, 32000, 64, 0, 0), (7, 32003, 20, 1, 0), (40, 1023, 256, 1, 0), (5, 4096, 100, 8, 0),
     (64, 2050, 33, 0, 3), (150, 5000, 8, 0, 0), (9, 50257, 50, 0, 0), (3, 131072, 32, 0, 0), (160, 33000, 16, 0, 0), (2, 300001, 7, 0, 0), (1, 700000, 10, 0, 0), (300, 128, 4, 0, 0),
-    (150, 120000, 16, 5, 1)]
+    (150, 120000, 16, 5, 1), (600, 9001, 8, 0, 0)]
 
 
 @pytest.mark.parametrize("T,V,top,pad,lead", SIZES)
