@@ -7,7 +7,7 @@
 // wait for a row to arrive or for one another, others calculate or write.
 //
 // Persistent CTAs that had the copy engine fetch rows ahead, with a row's exponentials kept in registers between the passes,
-// were slower (4096 x 131072 in bf16 1190 us, this 422; 2048 x 32000 128 and 68): a row is a chain of latencies for the warps that
+// were slower (4096 x 131072 in bf16 1190 us, this 452; 2048 x 32000 128 and 68): a row is a chain of latencies for the warps that
 // share it, and what hides it is many rows at a time.
 //
 // Pieces lie on 16-byte boundaries whatever the row's alignment is: the first and last are masked, and results that lie
@@ -491,20 +491,21 @@ int launch_row(DistillArgs &A, int64_t T, cudaStream_t stream)
         const int64_t part = part_of(split);
         return ((part < A.vocab ? part : A.vocab) * (int64_t)sizeof(E) + 15) / 16 + inside;
     };
-    // With a row for every SM, one CTA each (two an SM, 512 threads) goes over rows that it cannot hold, as long as all of these stay
-    // in L2 for the second pass; longer ones are held by a cluster that they fill, and so are fewer rows.  Steps of 4096 x 131072 in
-    // bf16 422 us, held by clusters 440; 1500 x 160000 217, held (not filled) 310; 2048 x 50257 105 and 118; 1024 x 131072 in f32
-    // (512 KB a row) 257, held 235.  Backward, which takes one pass: 343, held 388; 171 and 231; 79 and 100; rows
+    // With a row for every SM, one CTA each (two an SM, 512 threads) goes over rows that it cannot hold, unless a cluster holds them and
+    // is filled: in CTAs of 256 threads then, where eight are enough.  Steps of 4096 x 131072 in bf16, inputs that change from call to
+    // call, 452 us, gone by 465, held in CTAs of 512 threads 468; of 1500 x 160000 gone by 217, held (not filled) 310; of 2048 x 50257
+    // 105 and 118; of 1024 x 131072 in f32 held 236, gone by 257.  Backward, which takes one pass: 343, held 388; 171 and 231; 79 and 100; rows
     // that a CTA could hold go by small CTAs as well where there are many of 16 KB and more (2048 x 32000 58 and 61; 8192 x 4000 35 and
     // 32, 256 x 32000 16.5 and 13.7, which are held).
     constexpr int64_t kRoom = kMaxThreads * kHeld;
-    const bool many = T >= sm_count() && T > kDistillAlone, stays = 2 * sm_count() * A.vocab * (int64_t)sizeof(E) <= (int64_t)112 << 20;
+    const bool many = T >= sm_count() && T > kDistillAlone;
     int split = 1;
     while (split < kMaxSplit && pieces_of(split) > kRoom) split *= 2;
-    const bool filled = MODE == kStep && !stays && pieces_of(split) * 8 >= kRoom * 7;
+    const bool filled = MODE == kStep && pieces_of(split) * 8 >= kRoom * 7;
     const bool small = MODE == kBack && T >= 4 * sm_count() && pieces_of(1) > 1024;
     const bool held = MODE != kLoss && pieces_of(split) <= kRoom && (!many || filled || (split == 1 && !small));
     if (!held && (MODE == kLoss || many)) split = 1;
+    if (held && many && split > 1 && split < kMaxSplit) split *= 2;
     while (split < kMaxSplit && pieces_of(split) > 1 << 26) split *= 2;          // a part's bytes are counted in 32 bits
     // more CTAs a row while there are SMs without one and a CTA keeps a few kilobytes
     while (split < kMaxSplit && T * split * 2 <= sm_count() && pieces_of(1) >= 256 * split) split *= 2;
