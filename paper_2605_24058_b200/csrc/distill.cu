@@ -13,7 +13,9 @@
 // Pieces lie on 16-byte boundaries whatever the row's alignment is: the first and last are masked, and results that lie
 // otherwise are joined from the pieces of neighbouring lanes.
 //
-// The exponentials are powers of two of  z log2(e)/temperature - m : a multiply-add (of two at a time) and one instruction each.
+// The exponentials are powers of two of  (z - max) log2(e)/temperature : a difference and a product (of two at a time) and one
+// instruction each.  The difference comes first: a product of max and the factor, subtracted in one multiply-add, would leave its rounding
+// in every exponent, and of very low numbers (a mask's) an infinity.
 //
 // The teacher's part of a row (softmax of the top entries, the student's logits there) is a chain of latencies too: for many rows a
 // kernel of its own goes through it first.
@@ -346,13 +348,20 @@ distill_kernel(const __grid_constant__ DistillArgs A)
                 return fmaxf(fmaxf(x.x, x.y), fmaxf(y.x, y.y));
             }
         };
-        Two scales = two(A.scale, A.scale), minuses, sums[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
+        const Two scales = two(A.scale, A.scale);
+        Two minuses, sums[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
+        // sums are relative to the largest logit so far itself, or to 0 where that is minus infinity
+        auto relative_to = [&](float max) {
+            const float minus = max == -INFINITY ? 0.0f : -max;
+            minuses = two(minus, minus);
+            return minus;
+        };
         auto add = [&](uint4 w) {
             Two v[N / 2];
             unpack_chunk<E>(w, v);
 #pragma unroll
             for (int j = 0; j < N / 2; ++j) {
-                const float2 x = halves(fma_two(v[j], scales, minuses));
+                const float2 x = halves(mul_two(add_two(v[j], minuses), scales));
                 sums[j % 2] = add_two(sums[j % 2], two(exp2_of(x.x), exp2_of(x.y)));
             }
         };
@@ -369,8 +378,7 @@ distill_kernel(const __grid_constant__ DistillArgs A)
                     }
                     const float was = s.max;
                     s.max = largest();
-                    const float minus = s.max == -INFINITY ? 0.0f : -s.max * A.scale, kept = exp2_of(fmaf(was, A.scale, minus));
-                    minuses = two(minus, minus);
+                    const float kept = exp2_of((was + relative_to(s.max)) * A.scale);          // 1 where the maximum stays
 #pragma unroll
                     for (int j = 0; j < 2; ++j) sums[j] = mul_two(sums[j], two(kept, kept));
 #pragma unroll
@@ -392,8 +400,7 @@ distill_kernel(const __grid_constant__ DistillArgs A)
                 top_of_chunk<E>(raw[i], most);
             }
             s.max = largest();
-            const float minus = s.max == -INFINITY ? 0.0f : -s.max * A.scale;
-            minuses = two(minus, minus);
+            relative_to(s.max);
 #pragma unroll
             for (int i = 0; i < kHeld; ++i) {
                 if (i >= pieces) break;
