@@ -35,7 +35,7 @@ constexpr int kMaxSplit = 8, kMaxThreads = 512;
 // Rows up to which each does its teacher's part itself: a chain of accesses that wait for one another, 2 us where the GPU is
 // idle, but more than twice that among other rows' traffic, where a kernel of its own before (one more launch, 1.5 us) pays.
 constexpr int64_t kDistillAlone = 128;
-constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLog2E = 1.4426950408889634f;
 enum Mode { kLoss, kStep, kBack };
 
 struct DistillArgs {
@@ -250,10 +250,10 @@ __device__ __forceinline__ void loss_of(const DistillArgs &A, int64_t t, const E
     }
 }
 
-// The gradients of the teacher's entries, every `by`-th from `at` on, over what was put there.
-template <typename E>
+// The gradients of the teacher's entries, every `by`-th from `at` on, over what was put there.  probability: the student's, of a logit.
+template <typename E, typename F>
 __device__ __forceinline__ void patch_row(const DistillArgs &A, int64_t t, int first, int count, const Entry *top, bool twice, float factor,
-                                          float shift, int at, int by = 32)
+                                          F probability, int at, int by)
 {
     E *dz = static_cast<E *>(A.dlogits) + t * A.ld_dlogits;
     for (int j = at; j < A.top; j += by) {
@@ -264,7 +264,7 @@ __device__ __forceinline__ void patch_row(const DistillArgs &A, int64_t t, int f
             p = 0.0f;
             for (int k = 0; k < A.top; ++k) p += top[k].id == e.id ? top[k].p : 0.0f;
         }
-        dz[e.id] = from_float<E>(factor * (exp2_of(fmaf(e.z, A.scale, -shift)) - p));
+        dz[e.id] = from_float<E>(factor * (probability(e.z) - p));
     }
 }
 
@@ -434,10 +434,16 @@ distill_kernel(const __grid_constant__ DistillArgs A)
     const bool live = weight != 0.0f && head.sum != 0.0f;
     if (MODE != kBack && rank == 0 && warp == 0) loss_of(A, t, top, all, weight, live, lane);
     if (MODE == kLoss) return;
-    // logits less `shift` powers are the student's probabilities
-    const float shift = MODE != kBack ? all.max * A.scale + log2f(all.sum) : A.lse[t] * (1.0f / kLn2);
+    // The student's probabilities: 2^((z - max) log2(e)/temperature - log2(sum)), or from lse 2^((z/temperature - lse) log2(e)).  As in the sums the
+    // large numbers meet first, and what is left of them is scaled.
+    const float less = MODE != kBack ? -all.max : -A.lse[t], log_sum = MODE != kBack ? -log2f(all.sum) : 0.0f;
+    auto exponents = [&](Two v) {
+        if constexpr (MODE != kBack) return fma_two(add_two(v, two(less, less)), two(A.scale, A.scale), two(log_sum, log_sum));
+        else return mul_two(fma_two(v, two(A.inverse, A.inverse), two(less, less)), two(kLog2E, kLog2E));
+    };
+    auto probability = [&](float z) { return exp2_of(halves(exponents(two(z, z))).x); };
     const float factor = weight * A.temperature;
-    const Two times = two(factor, factor), scales = two(A.scale, A.scale), shifts = two(-shift, -shift);
+    const Two times = two(factor, factor);
     uint8_t *to = reinterpret_cast<uint8_t *>(static_cast<E *>(A.dlogits) + t * A.ld_dlogits + first) - off + 16 * tid;
     const int by = (int)(reinterpret_cast<uintptr_t>(to) & 15);
     const bool plain = by == 0 && !edges;             // whole pieces alone
@@ -446,7 +452,7 @@ distill_kernel(const __grid_constant__ DistillArgs A)
         unpack_chunk<E>(w, v);
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) {
-            const float2 x = halves(fma_two(v[j], scales, shifts));
+            const float2 x = halves(exponents(v[j]));
             v[j] = mul_two(two(exp2_of(x.x), exp2_of(x.y)), times);
         }
         w = pack_chunk<E>(v);
@@ -468,7 +474,7 @@ distill_kernel(const __grid_constant__ DistillArgs A)
     }
     if (!live) return;
     __syncthreads();                       // the teacher's entries' gradients go over what was put there
-    if (warp * 32 < A.top) patch_row<E>(A, t, first, count, top, head.twice, factor, shift, tid, THREADS);
+    if (warp * 32 < A.top) patch_row<E>(A, t, first, count, top, head.twice, factor, probability, tid, THREADS);
 }
 
 template <typename E, int MODE, bool ALONE, bool HELD>

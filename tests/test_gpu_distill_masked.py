@@ -82,3 +82,43 @@ def test_rows_masked_throughout_are_even(kind, dtype, T, V):
     for got in (lordba.distill_loss(z, ids, teacher, 1.0, weight), lordba.distill_loss(z, ids, teacher, 1.0, weight, grad=True)):
         within(got[0], loss, tol_loss, "f32", "loss")
         within(got[1], lse, tol_lse, "f32", "lse")
+
+
+@everything
+def test_gradients_beside_masked_classes(place, kind, dtype, T, V, tau):
+    z, ids, teacher, weight, masked, left = masked_case(place, kind, dtype, T, V)
+    _, _, dz, _, _, tol_dz, tol_back = definition(z[:, ~masked], left, teacher, weight, tau)
+    step = lordba.distill_loss(z, ids, teacher, tau, weight, grad=True)
+    back = lordba.distill_backward(weight, z, ids, teacher, step[1], tau)
+    for g, tol in ((step[2], tol_dz), (back, tol_back)):
+        within(g[:, ~masked], dz, tol, dtype, "dlogits")
+        assert (g[:, masked] == 0).all()
+
+
+@throughout
+def test_gradients_of_rows_masked_throughout(kind, dtype, T, V):
+    z, ids, teacher, weight = even_case(kind, dtype, T, V)
+    _, _, dz, _, _, tol_dz, _ = definition(z, ids, teacher, weight, 1.0)
+    _, lse, got = lordba.distill_loss(z, ids, teacher, 1.0, weight, grad=True)
+    within(got, dz, tol_dz, dtype, "dlogits")
+    # the way back knows lse in float32 alone, which has no room for log V beside such a number: the formula's value for the lse given
+    back = lordba.distill_backward(weight, z, ids, teacher, lse)
+    q = (z.double() - lse.double()[:, None]).exp()
+    want = weight.double()[:, None] * q.scatter_add(1, ids, -teacher.double().softmax(1))
+    # z - lse is rounded once (float16's is of some tens; the others' 0), the power's argument twice more
+    within(back, want, weight.double()[:, None] * (q + 1) * 2.0 ** -18, dtype, "dlogits of distill_backward")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V", [(3, 512), (200, 32000), (200, 140000)])
+def test_a_masked_class_of_the_teacher(dtype, T, V):
+    """The teacher names a class that the student masks: a very large loss (float32 holds it), gradient -p there."""
+    z, ids, teacher, weight = case(T, V, dtype, 7 * V + T, torch.arange(V // 2, V, device="cuda"))
+    z[:, :V // 2] = -1e30
+    ids[:, 2] = 7
+    loss, lse, dz, tol_loss, tol_lse, tol_dz, _ = definition(z, ids, teacher, weight, 1.0)
+    got = lordba.distill_loss(z, ids, teacher, 1.0, weight, grad=True)
+    assert (loss > 1e20).all()
+    within(got[0], loss, tol_loss, "f32", "loss")
+    within(got[1], lse, tol_lse, "f32", "lse")
+    within(got[2], dz, tol_dz, dtype, "dlogits")

@@ -89,3 +89,12 @@ def test_losses_of_offset_rows(kind, dtype, T, V, tau, offset):
     for got in (lordba.distill_loss(z, ids, teacher, tau, weight), lordba.distill_loss(z, ids, teacher, tau, weight, grad=True)):
         within(got[0], loss, tol_loss, "f32", "loss")
         within(got[1], lse, tol_lse, "f32", "lse")
+
+
+@everything
+def test_gradients_of_offset_rows(kind, dtype, T, V, tau, offset):
+    z, ids, teacher, tau, weight = case(kind, dtype, T, V, tau, offset)
+    _, lse, dz, _, _, tol_dz, tol_back = definition(z, ids, teacher, weight, tau)
+    within(lordba.distill_loss(z, ids, teacher, tau, weight, grad=True)[2], dz, tol_dz, dtype, "dlogits")
+    lse = lordba.distill_loss(z, ids, teacher, tau, weight)[1]
+    within(lordba.distill_backward(weight, z, ids, teacher, lse, tau), dz, tol_back, dtype, "dlogits of distill_backward")
