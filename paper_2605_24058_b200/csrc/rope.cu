@@ -261,7 +261,8 @@ norm_rope_kernel(const __grid_constant__ RopeArgs A)
                 float q = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) q += a[j] * a[j] + b[j] * b[j];
-                r = rsqrtf(over_head(q, A.width) * A.inv_d + A.eps);
+                q = over_head(q, A.width) * A.inv_d + A.eps;
+                r = !BACK || h_now < S.heads ? rsqrtf(q) : 0.0f;          // where no head is, zeros enter the sums of dw, without an epsilon too
             }
             if (!BACK) {
 #pragma unroll
@@ -444,7 +445,8 @@ norm_rope_full_kernel(const __grid_constant__ RopeArgs A)
                 Two q = mul_two(a[0], a[0]), q2 = mul_two(b[0], b[0]);
 #pragma unroll
                 for (int j = 1; j < 4; ++j) { q = fma_two(a[j], a[j], q); q2 = fma_two(b[j], b[j], q2); }
-                r = rsqrtf(over_lanes<WIDTH>(add_two(q, q2)) * A.inv_d + A.eps);
+                const float mean = over_lanes<WIDTH>(add_two(q, q2)) * A.inv_d + A.eps;
+                r = !BACK || in ? rsqrtf(mean) : 0.0f;                    // where no head is, zeros enter the sums of dw, without an epsilon too
             }
             const Two rr = two(r, r);
             if (!BACK) {
