@@ -312,9 +312,10 @@ distill_kernel(const __grid_constant__ DistillArgs A)
         if (edges && (c == 0 || c == chunks - 1)) w = mask_chunk<E>(w, c, off, count);
         return w;
     };
-    // The teacher's kernel lets this one start only once it has itself seen the end of everything before it, so the logits are
-    // there (in L2); what that kernel makes, and what may be written over, waits for its end.
-    if (ALONE) grid_wait();
+    // Logits too wait for the end of all kernels before.  Reading them while the teacher's kernel still runs gained a microsecond for the loss of
+    // 2048 x 32000 and lost ten of 4096 x 131072 with gradient.
+    grid_wait();
+    grid_release();
     if (MODE != kBack && A.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // this CTA runs
     auto piece = [&](int i) { return tid + THREADS * i < chunks ? __ldcg(in + THREADS * i) : make_uint4(kLow, kLow, kLow, kLow); };
     // for the last time: other rows may take its place in L2
@@ -322,8 +323,6 @@ distill_kernel(const __grid_constant__ DistillArgs A)
     uint4 raw[kHeld];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) raw[i] = piece(i);
-    if (!ALONE) grid_wait();
-    grid_release();
     const float weight = A.weight ? A.weight[t] : 1.0f;
     if constexpr (ALONE) {
         if (warp == 0) {
