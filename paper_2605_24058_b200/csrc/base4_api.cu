@@ -36,6 +36,7 @@ int check_carrier_pointers(const Carrier &c)
 {
     int rc = check_matrix(c.q);
     if (rc == LORDBA_OK) rc = check_matrix(c.scale);
+    if (rc == LORDBA_OK && too_far(c.zero)) rc = LORDBA_EINVAL;
     if (rc != LORDBA_OK) return rc;
     return aligned(c.q.p, 16) && c.q.ld % 16 == 0 ? LORDBA_OK : LORDBA_EALIGN;
 }
@@ -141,7 +142,7 @@ int int4_call(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, 
 
 // ---- heads --------------------------------------------------------------------------------------------------------
 // Head vectors as a matrix: a row a token (or, head by head, a row a head), from the first entry to the last.  One that is
-// neither, such as heads that share their entries, is a single row.  clear: no two vectors share an entry.
+// neither, such as heads that share their entries, is a single row.  clear: no two vectors share an entry.  Sizes have been looked at (far_heads).
 struct Heads {
     Matrix m;
     bool clear;
@@ -155,6 +156,13 @@ Heads heads_of(const lordba_heads &h, int64_t T, int64_t heads, int64_t d, size_
     if ((T == 1 || token >= d) && (heads == 1 || head >= by_head)) return Heads{Matrix{h.p, heads, by_head, heads > 1 ? head : by_head, e}, true};
     const int64_t all = (T - 1) * token + (heads - 1) * head + d;
     return Heads{Matrix{h.p, 1, all, all, e}, false};
+}
+
+// Whether head vectors reach further than any memory does.
+bool far_heads(const lordba_heads &h, int64_t T, int64_t heads, size_t e)
+{
+    const int64_t most = kMostBytes / 4 / (int64_t)e;
+    return (T > 1 && h.token > most / (T - 1)) || (heads > 1 && h.head > most / (heads - 1));
 }
 
 bool same_heads(const lordba_heads &a, const lordba_heads &b, int64_t T, int64_t heads)
@@ -189,10 +197,10 @@ struct RopeCall {
 int check_heads(const RopeCall &c, const lordba_norm_rope_args &a, int64_t T, int dtype, float *const *dw)
 {
     const size_t e = elt(dtype), ew = elt(a.w_dtype);
-    constexpr int64_t kFar = int64_t(1) << 40;            // keeps every product of sizes inside 64 bits
     for (int i = 0; i < c.n_in + c.n_out; ++i) {
-        const lordba_heads &h = i < c.n_in ? *c.in[i].h : *c.out[i - c.n_in].h;
-        if (!h.p || h.token < 0 || h.head < 0 || h.token > kFar || h.head > kFar) return LORDBA_EINVAL;
+        const RopeCall::Item &item = i < c.n_in ? c.in[i] : c.out[i - c.n_in];
+        const lordba_heads &h = *item.h;
+        if (!h.p || h.token < 0 || h.head < 0 || far_heads(h, T, item.heads, e)) return LORDBA_EINVAL;
         if (!aligned(h.p, e)) return LORDBA_EALIGN;
     }
     if (!a.positions || (a.rotary && !a.inv_freq)) return LORDBA_EINVAL;
@@ -294,7 +302,7 @@ int lordba_int4_pack(const uint8_t *values, int64_t ldv, uint8_t *q, int64_t ldq
     if (bad_size(d_out, d_in) || ldv < d_in || ldq < carrier_bytes(d_in)) return LORDBA_EINVAL;
     if (d_out == 0) return LORDBA_OK;
     const Matrix v{values, d_out, d_in, ldv, 1}, c{q, d_out, carrier_bytes(d_in), ldq, 1};
-    if (!v.p || !c.p) return LORDBA_EINVAL;
+    if (!v.p || !c.p || too_far(v) || too_far(c)) return LORDBA_EINVAL;
     if (!aligned(q, 16) || ldq % 16) return LORDBA_EALIGN;
     if (meet(v, c)) return LORDBA_EINVAL;
     return launch_int4_pack(values, ldv, q, ldq, d_out, d_in, static_cast<cudaStream_t>(stream));

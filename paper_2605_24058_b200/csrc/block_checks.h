@@ -32,9 +32,19 @@ inline bool meet(const Matrix &a, const Matrix &b)
 
 inline bool same(const Matrix &a, const Matrix &b) { return a.p == b.p && a.ld == b.ld && a.e == b.e && a.cols == b.cols; }
 
+// No range of addresses is longer, and sizes within it can be multiplied out in 64 bits.
+constexpr int64_t kMostBytes = int64_t(1) << 56;
+inline bool too_far(const Matrix &m)
+{
+    if (!m.p) return false;
+    const int64_t most = kMostBytes / (int64_t)m.e;
+    return m.ld > most || m.cols > most || (m.rows > 1 && m.ld > (most - m.cols) / (m.rows - 1));
+}
+
+// Of each matrix that a call is given, before `meet` looks at it.
 inline int check_matrix(const Matrix &m)
 {
-    if (!m.p) return LORDBA_EINVAL;
+    if (!m.p || too_far(m)) return LORDBA_EINVAL;
     if (!aligned(m.p, m.e)) return LORDBA_EALIGN;
     return LORDBA_OK;
 }
