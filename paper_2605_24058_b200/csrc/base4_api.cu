@@ -2,6 +2,7 @@
 // distillation.  Argument checks on the host, then launches; include/lordba.h states every contract.
 #include <cmath>
 #include <cstring>
+#include <numeric>
 
 #include "block_checks.h"
 
@@ -165,6 +166,22 @@ bool far_heads(const lordba_heads &h, int64_t T, int64_t heads, size_t e)
     return (T > 1 && h.token > most / (T - 1)) || (heads > 1 && h.head > most / (heads - 1));
 }
 
+// Whether two sets of head vectors share an entry's bytes.  Beyond what `meet` sees: where all distances are multiples of one, such as in
+// a joint projection's output that holds a head's query, key and value side by side, vectors that do not meet within it do not meet.
+bool meet_heads(const lordba_heads &a, int64_t heads_a, const lordba_heads &b, int64_t heads_b, int64_t T, int64_t d, size_t e)
+{
+    if (!meet(heads_of(a, T, heads_a, d, e).m, heads_of(b, T, heads_b, d, e).m)) return false;
+    int64_t step = 0;
+    if (T > 1) step = std::gcd(a.token, b.token);
+    if (heads_a > 1) step = std::gcd(step, a.head);
+    if (heads_b > 1) step = std::gcd(step, b.head);
+    if (step == 0) return true;
+    const size_t pitch = (size_t)step * e, bytes = (size_t)d * e;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+    const size_t shift = pb >= pa ? (pb - pa) % pitch : (pitch - (pa - pb) % pitch) % pitch;
+    return !(bytes <= shift && shift + bytes <= pitch);
+}
+
 bool same_heads(const lordba_heads &a, const lordba_heads &b, int64_t T, int64_t heads)
 {
     return a.p == b.p && (T <= 1 || a.token == b.token) && (heads <= 1 || a.head == b.head);
@@ -217,9 +234,11 @@ int check_heads(const RopeCall &c, const lordba_norm_rope_args &a, int64_t T, in
         for (int j = 0; j < c.n_in; ++j) {
             // an input of the same side may be the output's very place
             if (c.in[j].side == c.out[i].side && same_heads(*c.out[i].h, *c.in[j].h, T, c.out[i].heads)) continue;
-            if (meet(h.m, heads_of(*c.in[j].h, T, c.in[j].heads, a.d, e).m)) return LORDBA_EINVAL;
+            if (meet_heads(*c.out[i].h, c.out[i].heads, *c.in[j].h, c.in[j].heads, T, a.d, e)) return LORDBA_EINVAL;
         }
     }
+    if (n == 2 && meet_heads(*c.out[0].h, c.out[0].heads, *c.out[1].h, c.out[1].heads, T, a.d, e)) return LORDBA_EINVAL;
+    const int vectors = n;
     for (int i = 0; dw && i < 2; ++i)
         if (dw[i]) {
             if (!aligned(dw[i], 4)) return LORDBA_EALIGN;
@@ -229,7 +248,7 @@ int check_heads(const RopeCall &c, const lordba_norm_rope_args &a, int64_t T, in
             outs[n++] = m;
         }
     for (int i = 0; i < n; ++i) {
-        for (int j = i + 1; j < n; ++j)
+        for (int j = i + 1 < vectors ? vectors : i + 1; j < n; ++j)
             if (meet(outs[i], outs[j])) return LORDBA_EINVAL;
         for (const Matrix &m : flat)
             if (meet(outs[i], m)) return LORDBA_EINVAL;
