@@ -256,6 +256,16 @@ int check_heads(const RopeCall &c, const lordba_norm_rope_args &a, int64_t T, in
     return LORDBA_OK;
 }
 
+// The arguments, without what would belong to keys where there are none: nothing of it is looked at.
+lordba_norm_rope_args without_absent_keys(lordba_norm_rope_args a)
+{
+    if (a.heads_k == 0) {
+        a.k = a.k_out = lordba_heads{};
+        a.w_k = nullptr;
+    }
+    return a;
+}
+
 int check_rope_grad(const lordba_norm_rope_grad_args &a, int64_t T, int dtype)
 {
     const int rc = check_norm_rope(a.f, T, dtype);
@@ -377,9 +387,10 @@ int lordba_int4_linear_backward(const lordba_int4_proj *p, int64_t T, int dtype,
     return int4_call(p, T, dtype, workspace, workspace_bytes, stream, true);
 }
 
-int lordba_norm_rope(const lordba_norm_rope_args *a, int64_t T, int dtype, void *stream)
+int lordba_norm_rope(const lordba_norm_rope_args *given, int64_t T, int dtype, void *stream)
 {
-    if (!a) return LORDBA_EINVAL;
+    if (!given) return LORDBA_EINVAL;
+    const lordba_norm_rope_args own = without_absent_keys(*given), *a = &own;
     int rc = check_norm_rope(*a, T, dtype);
     if (rc != LORDBA_OK || T == 0) return rc;
     const int sides = a->heads_k ? 2 : 1;
@@ -388,15 +399,20 @@ int lordba_norm_rope(const lordba_norm_rope_args *a, int64_t T, int dtype, void 
     return rc != LORDBA_OK ? rc : launch_norm_rope(*a, T, dtype, static_cast<cudaStream_t>(stream));
 }
 
-size_t lordba_norm_rope_backward_workspace_bytes(const lordba_norm_rope_grad_args *a, int64_t T)
+size_t lordba_norm_rope_backward_workspace_bytes(const lordba_norm_rope_grad_args *given, int64_t T)
 {
-    if (!a || check_rope_grad(*a, T, LORDBA_F32) != LORDBA_OK || T == 0) return 0;
-    return norm_rope_backward_bytes(*a, T);
+    if (!given) return 0;
+    lordba_norm_rope_grad_args a = *given;
+    a.f = without_absent_keys(a.f);
+    return check_rope_grad(a, T, LORDBA_F32) != LORDBA_OK || T == 0 ? 0 : norm_rope_backward_bytes(a, T);
 }
 
-int lordba_norm_rope_backward(const lordba_norm_rope_grad_args *a, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+int lordba_norm_rope_backward(const lordba_norm_rope_grad_args *given, int64_t T, int dtype, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!a) return LORDBA_EINVAL;
+    if (!given) return LORDBA_EINVAL;
+    lordba_norm_rope_grad_args own = *given;
+    own.f = without_absent_keys(own.f);
+    const lordba_norm_rope_grad_args *a = &own;
     int rc = check_rope_grad(*a, T, dtype);
     if (rc != LORDBA_OK) return rc;
     const lordba_norm_rope_args &f = a->f;
