@@ -96,7 +96,7 @@ Int4Workspace int4_workspace(const lordba_int4_proj &p, int64_t T, int dtype, bo
     w.way = int4_way(p, T, backward);
     if (w.way != Int4Way::kWide) {
         w.ld = ((backward ? p.d_out : p.d_in) + 7) / 8 * 8;
-        if (!aligned(p.in, 16) || p.ld_in % 8) w.first = ((size_t)T * (size_t)w.ld * 2 + 255) / 256 * 256;
+        if (!aligned(p.in, 16) || (T > 1 && p.ld_in % 8)) w.first = ((size_t)T * (size_t)w.ld * 2 + 255) / 256 * 256;
         w.bytes = w.first;
         return w;
     }
@@ -130,6 +130,7 @@ int int4_call(const lordba_int4_proj *p, int64_t T, int dtype, void *workspace, 
         if (rc != LORDBA_OK) return rc;
         return launch_product(int4_product(*p, T, dtype, backward, workspace, w.ld), static_cast<uint8_t *>(workspace) + w.first, on);
     }
+    if (T == 1) call.ld_in = w.ld;              // a single row has no pitch of its own
     if (w.first) {
         call.in = workspace;
         call.ld_in = w.ld;
