@@ -561,8 +561,8 @@ int lordba_int4_linear_backward(const lordba_int4_proj *p, int64_t T, int dtype,
  *     y_a = n_a cos(f) - n_b sin(f),  y_b = n_b cos(f) + n_a sin(f),    f = positions[t] * inv_freq[i]
  *
  * for the pairs (a, b) = (i, i + rotary/2), or (2 i, 2 i + 1) with LORDBA_ROPE_INTERLEAVED, i < rotary/2;
- * y = n from entry `rotary` on.  rotary = 0 is the norm alone.  The angle is the exact product, reduced in
- * 64 bits: positions of any size are good.  Everything else is float32, y is rounded once.
+ * y = n from entry `rotary` on.  rotary = 0 is the norm alone.  The angle is the product of any 64-bit position and a frequency (up to
+ * 16 in size) less its whole turns, good to 2^-40 of a turn.  Everything else is float32, y is rounded once.
  *
  * Tensors are [token][head][entry] with any distances between tokens and between heads and the entries
  * side by side (slices of a joint projection's output are read in place).  q_out may be q and k_out may be
