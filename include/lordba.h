@@ -507,8 +507,9 @@ int lordba_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr
  * LORDBA_EUNSUPPORTED).  Every sum is float32, results are rounded once.  A forward call of few tokens
  * (now up to 32) multiplies the integers themselves (they are exact in 16 bits) and scales the sum of each
  * group; others multiply weights that were rounded to the type of x, because that is what the tensor cores
- * take (the error of y is then up to 1.4 times that of rounding y alone).  A scale that is not finite spoils its
- * row of y (of dx: the columns of its group) and nothing else.  T = 0 is a no-op.
+ * take (the error of y is then up to 1.4 times that of rounding y alone).  So a float16 weight beyond 65504 (a scale above 65504 / 15 can
+ * make one) is infinite in gradients and for many tokens, as it is for lordba_int4_dequantize, though not for few.  A scale that is not
+ * finite spoils its row of y (of dx: the columns of its group) and nothing else.  T = 0 is a no-op.
  */
 typedef struct lordba_int4_proj {
     const void    *in;          /* [device] x, T x d_in  (backward: dy, T x d_out), pitch ld_in                  */
@@ -621,7 +622,10 @@ int lordba_norm_rope_backward(const lordba_norm_rope_grad_args *a, int64_t T, in
  * An entry is present where 0 <= ids[t,j] < vocab; an index may stand in a row more than once.  An entry
  * of teacher logit minus infinity has p = 0 and adds nothing, whatever the student's logit.  A row without
  * an entry of p > 0, and one of weight 0, has loss 0 and gradient 0, whatever stands in its logits.  A
- * student's logit of minus infinity has probability 0.  Sums and exponents are float32.
+ * student's logit of minus infinity, or of any number so low that its power is nothing beside the row's largest, has probability 0.
+ * Sums and exponents are float32, and relative to the row's largest logit: loss and the gradient of lordba_distill_loss do not
+ * depend on how far from zero a row lies.  lse is float32 too (infinite where logits / temperature pass its range), and the gradient made
+ * from it is off by its rounding.
  *
  * lordba_distill_loss writes loss and lse and, where dlogits is not NULL, the gradient in the same pass
  * over the logits (the weights of the rows, such as 1 over the number of tokens, are then the gradients of

@@ -74,14 +74,20 @@ Product int4_product(const lordba_int4_proj &p, int64_t T, int dtype, bool backw
     return q;
 }
 
-// How a product is done: a few tokens, some tens of them, or many, for which the weights are laid out in 16 bits first.
+// How a product is done: a few tokens, some tens of them, or many, for which the weights are laid out in 16 bits first.  Up to 256 tokens,
+// whatever the weights' size, widening them on the way (once for each 128 tokens) is as quick or quicker than laying them out, groups of 128, bf16:
+//   tokens                     48             129             256
+//   512 x 512             5.3 and 6.5     6.7 and 8.6     6.7 and 8.7 us      gradient 5.3 and 7.1,  6.7 and 8.6,  6.7 and 8.6
+//   4096 x 4096            12 and 18       22 and 22       22 and 24           13 and 19,   20 and 24,   20 and 26
+//   4096 -> 11008          21 and 39       46 and 48       49 and 49           22 and 42,   38 and 53,   38 and 56
+//   4096 -> 32000          47 and 114     103 and 125     105 and 133          44 and 116,  88 and 139,  88 and 144
+// (4096 -> 1024, 256 tokens, is the one shape measured that loses: 14.4 and 13.5).
 enum class Int4Way { kFew, kStream, kWide };
 
 Int4Way int4_way(const lordba_int4_proj &p, int64_t T, bool backward)
 {
     if (!backward && T <= kInt4Few) return Int4Way::kFew;
-    const double us = int4_stream_estimate(p, T, backward);
-    return T <= kInt4Stream && us >= 0 ? Int4Way::kStream : Int4Way::kWide;
+    return T <= kInt4Stream && int4_stream_takes(p, T, backward) ? Int4Way::kStream : Int4Way::kWide;
 }
 
 struct Int4Workspace {

@@ -11,8 +11,8 @@
 //
 // Bound: the widening.  A pair takes a shift, a choice of bits, a subtraction and a product, and the first two go at half the
 // rate: 8 us for 4096 x 11008 weights where nothing else is done (they arrive in 3.5 us).  It is done once for up to 128 tokens.
-// Measured, weights from HBM: 4096 x 4096, 17 / 64 / 128 tokens 11.8 / 12.6 / 15.0 us, 4096 x 11008 19.4 / 21.3 / 26.1 us (laid out in
-// 16 bits first 17.4 / 18.7 / 20.5 and 36.9 / 40.0 / 43.6 us; 256 tokens take both the same).  Rings of 4 ... 12 stages, one CTA an
+// Measured, weights from HBM: 4096 x 4096, 64 / 128 / 256 tokens 12.6 / 14.9 / 22.2 us, 4096 x 11008 21.4 / 26.0 / 48.9 us (int4_way in
+// base4_api.cu has the other way beside them).  Rings of 4 ... 12 stages, one CTA an
 // SM, and half as many warps with two pieces each gained nothing.
 //
 //   warps 0-15 widen (0-3 also move the sums), warp 16 issues MMAs and warp 17 the tokens' copies (one thread each)
@@ -350,11 +350,11 @@ StreamPlan plan_stream(const lordba_int4_proj &p, int64_t T, bool backward)
 
 }  // namespace
 
-double int4_stream_estimate(const lordba_int4_proj &p, int64_t T, bool backward)
+bool int4_stream_takes(const lordba_int4_proj &p, int64_t T, bool backward)
 {
     const StreamPlan s = plan_stream(p, T, backward);
     constexpr int64_t kFar = int64_t(1) << 31;           // pitches, and rows and columns with a tile's on top, are 32 bits
-    return p.d_in < kFar / 2 && p.d_out < kFar / 2 && s.row_tiles <= 65535 && s.token_tiles <= 65535 && p.ldq < kFar && p.ld_scale < kFar && (!p.zero || p.ld_zero < kFar) ? s.us : -1.0;
+    return p.d_in < kFar / 2 && p.d_out < kFar / 2 && s.row_tiles <= 65535 && s.token_tiles <= 65535 && p.ldq < kFar && p.ld_scale < kFar && (!p.zero || p.ld_zero < kFar);
 }
 
 int launch_int4_stream(const lordba_int4_proj &p, int64_t T, int dtype, bool backward, cudaStream_t stream)

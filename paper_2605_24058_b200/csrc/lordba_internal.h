@@ -148,8 +148,7 @@ constexpr int64_t kInt4Few = 32;        // tokens it takes at most
 int launch_int4_few(const lordba_int4_proj &p, int64_t T, int dtype, cudaStream_t stream);
 
 // --- int4_stream.cu ----------------------------------------------------------
-// Its time in microseconds, as far as choosing needs it; < 0: cannot be had.
-double int4_stream_estimate(const lordba_int4_proj &p, int64_t T, bool backward);
+bool int4_stream_takes(const lordba_int4_proj &p, int64_t T, bool backward);         // whether its counters have room for the sizes
 int launch_int4_stream(const lordba_int4_proj &p, int64_t T, int dtype, bool backward, cudaStream_t stream);      // p.in: as above
 
 // --- rope.cu -----------------------------------------------------------------
