@@ -15,7 +15,7 @@
 #include <cstring>
 
 #include "block_checks.h"
-#include "block_common.cuh"
+#include "product_internal.cuh"
 
 namespace lordba {
 namespace {
@@ -549,8 +549,6 @@ norm_rope_join_kernel(const __grid_constant__ JoinArgs J)
     }
 }
 
-constexpr int kBackBlocks = 148 * 2;       // at most, of both sides: what is resident at once
-
 // How a call's heads are dealt out: blocks of both sides, units.
 void plan(RopeArgs &A, const lordba_norm_rope_args &f, int64_t T, bool back)
 {
@@ -567,8 +565,9 @@ void plan(RopeArgs &A, const lordba_norm_rope_args &f, int64_t T, bool back)
         S.steps = (S.heads + per - 1) / per;
         all += S.steps;
     }
-    // a unit is a token's heads, or fewer of them while the GPU has idle warps (16 an SM are enough)
-    const int64_t warps = 148 * 16, most_blocks = back ? kBackBlocks : 148 * 16;
+    // a unit is a token's heads, or fewer of them while the GPU has idle warps (16 an SM are enough); backward two blocks an SM, what is
+    // resident at once: each leaves a row of partial sums
+    const int64_t warps = 16 * sm_count(), most_blocks = (back ? 2 : 16) * sm_count();
     for (int i = 0; i < 2; ++i) {
         Side &S = A.side[i];
         if (S.steps == 0) continue;
