@@ -7,8 +7,9 @@
 // wait for a row to arrive or for one another, others calculate or write.
 //
 // Persistent CTAs that had the copy engine fetch rows ahead, with a row's exponentials kept in registers between the passes,
-// were slower (4096 x 131072 in bf16 1190 us, this 452; 2048 x 32000 128 and 68): a row is a chain of latencies for the warps that
-// share it, and what hides it is many rows at a time.
+// were slower (4096 x 131072 in bf16 1190 us, this 438; 2048 x 32000 128 and 68): a row is a chain of latencies for the warps that
+// share it, and what hides it is many rows at a time.  The fullest unit is the one of the exponentials (59 % of its rate, 2048 x 32000), and warps
+// wait most for a row to arrive; no unit alone bounds it.
 //
 // Pieces lie on 16-byte boundaries whatever the row's alignment is: the first and last are masked, and results that lie
 // otherwise are joined from the pieces of neighbouring lanes.
@@ -505,10 +506,9 @@ int launch_row(DistillArgs &A, int64_t T, cudaStream_t stream)
     };
     // With a row for every SM, one CTA each (two an SM, 512 threads) goes over rows that it cannot hold, unless a cluster holds them and
     // is filled: in CTAs of 256 threads then, where eight are enough.  Steps of 4096 x 131072 in bf16, inputs that change from call to
-    // call, 452 us, gone by 465, held in CTAs of 512 threads 468; of 1500 x 160000 gone by 217, held (not filled) 310; of 2048 x 50257
-    // 105 and 118; of 1024 x 131072 in f32 held 236, gone by 257.  Backward, which takes one pass: 343, held 388; 171 and 231; 79 and 100; rows
-    // that a CTA could hold go by small CTAs as well where there are many of 16 KB and more (2048 x 32000 58 and 61; 8192 x 4000 35 and
-    // 32, 256 x 32000 16.5 and 13.7, which are held).
+    // call, 438 us, gone by 429, held in CTAs of 512 threads 474; of 1024 x 131072 in f32 held 220, gone by 248; of 1500 x 160000 gone by
+    // 215, held (not filled) 288; of 2048 x 50257 109 and 113.  Backward, which takes one pass, rows go by: 346, held 339; f32 182 and 170; 166 and 180;
+    // 79 and 83; rows that a CTA could hold go by small CTAs as well where there are many of 16 KB and more (2048 x 32000 58 and 61).
     constexpr int64_t kRoom = kMaxThreads * kHeld;
     const bool many = T >= sm_count() && T > kDistillAlone;
     int split = 1;
@@ -527,8 +527,8 @@ int launch_row(DistillArgs &A, int64_t T, cudaStream_t stream)
     while ((1 << A.split_log2) < split) ++A.split_log2;
     A.part = (int)part_of(split);
     const int64_t mine = pieces_of(split);
-    // The smallest CTA that holds its part.  Of many rows that nothing of is held, small ones of several rounds: the loss of 2048 x 32000
-    // 38 us, of one round 46; of 4096 x 131072 177, with 512 threads 190.
+    // The smallest CTA that holds its part.  Of many rows that nothing of is held, small ones of several rounds: the gradient from lse of 2048 x 32000
+    // 58 us, of one round 69, its loss 41 and 43; the loss of 4096 x 131072 182, with 512 threads 197.
     const int rounds = !many || held ? 1 : MODE == kLoss ? 4 : 2, most = MODE == kLoss && many ? kMaxThreads / 2 : kMaxThreads;
     int threads = 64;
     while (threads < most && mine > (int64_t)threads * kHeld * rounds) threads *= 2;

@@ -1,7 +1,8 @@
 // The 4-bit carrier: packing, quantisation and its way back to 16-bit weights.
 //
-// All three are bound by bytes and are no part of a decoding step: packing and quantising happen once a weight,
-// and the way back stands before products of many tokens, which take the weights as a 16-bit matrix (int4_linear).
+// Packing and quantising happen once a weight and are no part of a step; the way back stands before products of many tokens, which take the
+// weights as a 16-bit matrix (int4_linear).  11008 x 4096, floors by bytes in brackets: way back 21.7 us (17.3), pack 25.5 (10.3: a byte an
+// access), quantise from bf16 116 us (17.3), from f32 113 (31): the exact quotients take it, a division and its check a weight.
 #include "int4_common.cuh"
 
 namespace lordba {

@@ -9,8 +9,10 @@
 // engine.  The contraction is split over a cluster of up to eight CTAs, whose sums meet in distributed shared memory and are
 // added in rank order.
 //
-// Bound: the widening.  A pair takes a shift, a choice of bits, a subtraction and a product, and the first two go at half the
-// rate: 8 us for 4096 x 11008 weights where nothing else is done (they arrive in 3.5 us).  It is done once for up to 128 tokens.
+// Bound: latency, and the hand-over of stages.  A step takes a lone CTA 0.85 us (plan_stream), of which the widening's instructions are a
+// quarter (a pair: a shift, a choice of bits, a subtraction and a product); 64 tokens through 4096 x 11008 keep the integer pipe 32 % and
+// the issue slots 44 % busy, and the warps wait for weights, for one another at the stages' barriers, and for shared memory.  It is done once
+// for up to 128 tokens.
 // Measured, weights from HBM: 4096 x 4096, 64 / 128 / 256 tokens 12.6 / 14.9 / 22.2 us, 4096 x 11008 21.4 / 26.0 / 48.9 us (int4_way in
 // base4_api.cu has the other way beside them).  Rings of 4 ... 12 stages, one CTA an
 // SM, and half as many warps with two pieces each gained nothing.

@@ -10,8 +10,9 @@
 // 131072, one in 64 bits by 2^-17 of a turn at 2^40: frequencies are taken as turns in two doubles, products with what their rounding left,
 // and positions in halves of 32 bits, so that what is left of a turn is good to 2^-40 for any position and frequencies up to 16.
 //
-// Measured in bf16, 32 + 8 heads of 128: 8192 tokens 36 us (168 MB, 4.7 TB/s), gradients of 4096 tokens 33 us (126 MB, 3.9 TB/s), one
-// token 2.5 us.
+// Measured in bf16, 32 + 8 heads of 128: 8192 tokens 37 us (168 MB, 4.6 TB/s), gradients of 4096 tokens 32 us (126 MB, 3.9 TB/s), one
+// token 2.6 us.  No unit is full: issue slots 55 and 49 %, the integer pipe 40 and 38 %; the warps that registers leave room for (24 and 16 an SM)
+// wait for their loads first.
 #include <cstring>
 
 #include "block_checks.h"

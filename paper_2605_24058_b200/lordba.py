@@ -588,7 +588,8 @@ def int4_linear(x, q, scale, zero=None, group: int = 128, y: Optional[torch.Tens
                 stream=None) -> torch.Tensor:
     """y[t, n] = sum_k x[t, k] w[n, k] with the 4-bit weights w[n, k] = scale[n, k // group] (u[n, k] - zero[n, k // group]): the
     frozen base projection that an adapter's term is added to.  x (T, d_in), scale and y are bfloat16 or float16; y is
-    overwritten and returned.  workspace: a uint8 CUDA tensor of lordba_int4_linear_workspace_bytes(), made here if absent."""
+    overwritten and returned.  For more than 32 tokens, and in the gradient, weights are rounded to the type of x first (float16 ones
+    beyond 65504 are infinite then).  workspace: a uint8 CUDA tensor of lordba_int4_linear_workspace_bytes(), made here if absent."""
     return _native().int4_linear(x, q, scale, zero, group, y, workspace, stream)
 
 
@@ -603,7 +604,7 @@ def norm_rope(q, k, positions, inv_freq, w_q=None, w_k=None, eps: float = 1e-6, 
     """(q_out, k_out): queries (T, heads, d) and keys (T, key heads, d), each head vector divided by its root mean square and
     multiplied by w_q or w_k (ones if absent; norm=False leaves the vectors as they are), then rotated by position.
 
-    positions (T): int64.  inv_freq (rotary / 2): float32; pair i of a head, entries (i, i + rotary / 2) or, interleaved, (2 i,
+    positions (T): int64, of any size.  inv_freq (rotary / 2): float32; pair i of a head, entries (i, i + rotary / 2) or, interleaved, (2 i,
     2 i + 1), turns by positions[t] * inv_freq[i]; entries from ``rotary`` on are not rotated.  Tokens and heads may lie any
     distance apart (slices of a joint projection's output), entries side by side.  k may be None (k_out is then None).  q_out
     and k_out may be q and k."""
